@@ -38,6 +38,7 @@
 #ifndef ISAM_H
 #define ISAM_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -437,6 +438,139 @@ int isam_gru_plan_info(int layers, int batch, int hidden, int reset_before, int 
  */
 int isam_gru_plan_for(int layers, int batch, int hidden, int reset_before, int num_sms, int smem_optin,
                       int *out);
+
+/* Element types of the gated linear recurrence's gates and states. */
+enum { ISAM_F32 = 0, ISAM_BF16 = 1 };
+
+/*
+ * Gated linear recurrence: the GRU's state update with gates that do not read
+ * the state, so that it can be evaluated in parallel over time and trained.
+ * (The paper schedules recurrent nets step by step, Section 3.6; this form
+ * removes the product between the steps.)
+ *
+ *   z_t = sigmoid(g_z), n_t = g_n,  h_t = z_t h_{t-1} + (1 - z_t) n_t
+ *
+ *   g       [T][batch][2*hidden], rows z then n: what isam_gemm writes for a
+ *           stacked weight matrix [2*hidden][D]; fp32 or bf16 (g_type)
+ *   h0      [batch][hidden] fp32, or NULL for zeros
+ *   lengths [batch] int32 on the device, or NULL (every sequence has T
+ *           steps); values are clamped to [0, T].  Steps t >= lengths[b] are
+ *           padding: whatever g holds there is not used, h_out is zero and the
+ *           state stays.
+ *   h_out   [T][batch][hidden], fp32 or bf16 (h_type): every step's state
+ *   h_last  [batch][hidden] fp32 or NULL: the state after lengths[b] steps
+ *           (h0 where that is none); may be h0 itself.
+ *
+ * Gates, products and states are evaluated and carried in fp32; only h_out is
+ * rounded.  Results do not depend on timing (no atomics).
+ * Any T, batch, hidden >= 1 with T * batch * 2 * hidden below 2^40; pointers
+ * aligned to their element.  ISAM_ERR_INVALID_ARG for sizes < 1, null
+ * pointers or unknown types; ISAM_ERR_UNSUPPORTED beyond the size limit or
+ * for misaligned pointers.  Asynchronous on the stream set by
+ * isam_set_stream; no workspace.
+ */
+int isam_glr_forward(int T, int batch, int hidden, int g_type, const void *g, const float *h0,
+                     const int32_t *lengths, int h_type, void *h_out, float *h_last);
+
+/*
+ * Its backward pass.  With d_t the whole gradient of h_t,
+ *   d_t = dh_out_t + z_{t+1} d_{t+1}   (dh_last takes the place of the last
+ *                                       step's second term),
+ *   dg_z = d_t (h_{t-1} - n_t) z_t (1 - z_t),  dg_n = d_t (1 - z_t),
+ *   dh0 = z_1 d_1.
+ * g, h0, lengths and h_out are the forward call's arguments and result
+ * (h_{t-1} is read from h_out, as rounded there).
+ *   dh_out  [T][batch][hidden], h_type, or NULL for zeros; not used in padding
+ *   dh_last [batch][hidden] fp32, or NULL for zeros
+ *   dg      [T][batch][2*hidden], g_type; zero in padding
+ *   dh0     [batch][hidden] fp32, or NULL if not wanted; may be dh_last itself
+ * Limits, status codes and execution as isam_glr_forward.
+ */
+int isam_glr_backward(int T, int batch, int hidden, int g_type, const void *g, const float *h0,
+                      const int32_t *lengths, int h_type, const void *h_out, const void *dh_out,
+                      const float *dh_last, void *dg, float *dh0);
+
+/*
+ * One token of the recurrence for `batch` sequences whose states sit in a
+ * cache of `slots` rows:
+ *   new_state[slot] = h[b] = z state[slot] + (1 - z) n,  slot = slot_ids[b].
+ *   g          [batch][2*hidden] (g_type)
+ *   slot_ids   [batch] int32 on the device, distinct where they are valid, or
+ *              NULL for slot b (batch <= slots).  An id outside [0, slots)
+ *              marks a padding row: h is zero and no state is touched.
+ *   state      [slots][hidden] fp32
+ *   new_state  the same shape; `state` itself (updated in place) or another
+ *              buffer, of which only the rows of slot_ids are written
+ *   h          [batch][hidden] (h_type)
+ * Status codes and execution as isam_glr_forward.
+ */
+int isam_glr_step(int batch, int hidden, int slots, int g_type, const void *g, const int32_t *slot_ids,
+                  const float *state, float *new_state, int h_type, void *h);
+
+/* Activations of the gated feed-forward product (GELU with the error function). */
+enum { ISAM_ACT_SILU = 0, ISAM_ACT_GELU = 1, ISAM_ACT_RELU = 2, ISAM_ACT_SIGMOID = 3 };
+
+/*
+ * Gated feed-forward product: both projections of a feed-forward block, the
+ * activation and the product in one kernel,
+ *   h = act(x Wg^T) * (x Wu^T),   W = [Wg; Wu].
+ *   x  [T][D] bf16,  W  [2*F][D] bf16 (the F gate rows, then the F up rows),
+ *   h  [T][F] bf16.
+ * Two of Listing 4's matrix products share x, and the element-wise statements
+ * after them run on the accumulators (fp32): neither projection reaches
+ * memory.  The block's output projection is isam_gemm on h.
+ * Any T, F >= 1, D a multiple of 8, x and W 16-byte aligned, h 2-byte
+ * aligned; else ISAM_ERR_UNSUPPORTED.  ISAM_ERR_INVALID_ARG for sizes < 1, null
+ * pointers or an unknown act.  Asynchronous on the stream set by
+ * isam_set_stream.
+ */
+int isam_glu_forward(int T, int D, int F, int act, const isam_bf16 *x, const isam_bf16 *W, isam_bf16 *h);
+
+/* Bytes of isam_glu_backward's workspace (host arithmetic only). */
+int isam_glu_backward_workspace(int T, int D, int F, size_t *bytes);
+
+/*
+ * Its backward pass from dh [T][F] bf16.  The projections are computed again
+ * (the forward call keeps nothing): with g = x Wg^T, u = x Wu^T in fp32,
+ *   d = [dh u act'(g) | dh act(g)]  (rounded to bf16, in the workspace),
+ *   dx = d W  [T][D] bf16,   dW = d^T x  [2*F][D] bf16,
+ * sums in fp32.  dx or dW may be NULL if not wanted.
+ *   workspace: isam_glu_backward_workspace bytes of device memory, 16-byte
+ *   aligned, owned by the caller and free again when the call has completed on
+ *   its stream (calls on several streams need one each).
+ * F a multiple of 8 too (the second products read rows of 2F elements);
+ * dh, dx and dW 16-byte aligned.  Other limits, status codes and execution as
+ * isam_glu_forward.
+ */
+int isam_glu_backward(int T, int D, int F, int act, const isam_bf16 *x, const isam_bf16 *W,
+                      const isam_bf16 *dh, void *workspace, isam_bf16 *dx, isam_bf16 *dW);
+
+/*
+ * Products of a few tokens with 4-bit weights and group scales, for serving:
+ *   y[m][n] = sum_k x[m][k] s[n][k / group] (q[n][k] - 8),
+ * q in 0..15, one bf16 scale per `group` (32, 64 or 128) consecutive k of a
+ * row; x [M][K] bf16, y [M][N] fp32.  Weights are read once, in a tiled order
+ * that isam_w4_pack lays out (16 rows x 128 k a tile; padding has weight 0):
+ *   tiled:  [ceil(N/16)][ceil(K/128)][2][8][4][4] 32-bit words; word j of
+ *           (half, r, t) holds row 16 nb + 8 half + r, k = 128 kb + 32 j +
+ *           8 t + {0, 2, 4, 6, 1, 3, 5, 7} from its lowest nibble up.
+ *   tiled_scales: [ceil(N/16)][ceil(K/128)][16][128/group] bf16
+ * (a warp's lane 4 r + t reads 16 consecutive bytes of rows r and 8 + r).
+ *
+ * isam_w4_pack: from codes [N][K/2] (byte k/2 of a row holds q of an even k in
+ * its low half and of k + 1 in its high half) and scales [N][ceil(K/group)].
+ *
+ * 1 <= M <= 32, N >= 1, K >= 8 a multiple of 8; x, tiled and tiled_scales
+ * 16-byte aligned, y 4-byte aligned, scales 2-byte aligned; else
+ * ISAM_ERR_UNSUPPORTED.  ISAM_ERR_INVALID_ARG for sizes < 1, another group or
+ * null pointers.  (q - 8) is exact in bf16, sums are fp32, and each group's sum
+ * is multiplied by its scale in fp32.  Asynchronous on the stream set by
+ * isam_set_stream.
+ */
+int isam_w4_pack(int N, int K, int group, const uint8_t *codes, const isam_bf16 *scales, uint8_t *tiled,
+                 isam_bf16 *tiled_scales);
+int isam_gemv_w4(int M, int N, int K, int group, const isam_bf16 *x, const uint8_t *tiled,
+                 const isam_bf16 *tiled_scales, float *y);
 
 #ifdef __cplusplus
 }

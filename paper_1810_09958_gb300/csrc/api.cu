@@ -569,4 +569,157 @@ int isam_gru_plan_for(int layers, int batch, int hidden, int reset_before, int n
     return gru_plan_out(layers, batch, hidden, reset_before, num_sms, smem_optin, out);
 }
 
+namespace {
+
+bool aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1u)) == 0; }
+
+// Argument checks common to the gated linear recurrence's entries.
+int glr_validate(const char *name, int64_t T, int64_t batch, int64_t hidden, int g_type, int h_type, const void *g,
+                 const void *h) {
+    if (T < 1 || batch < 1 || hidden < 1) return set_error(ISAM_ERR_INVALID_ARG, "%s: sizes must be >= 1", name);
+    if ((g_type != ISAM_F32 && g_type != ISAM_BF16) || (h_type != ISAM_F32 && h_type != ISAM_BF16))
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: types must be ISAM_F32 or ISAM_BF16", name);
+    if (!g || !h) return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
+    if (batch * hidden > (int64_t{1} << 40) / (2 * T))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: more than 2^40 gate values", name);
+    if (!aligned(g, g_type == ISAM_F32 ? 4 : 2) || !aligned(h, h_type == ISAM_F32 ? 4 : 2))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: a pointer is not aligned to its element", name);
+    return ISAM_OK;
+}
+
+int glu_validate(const char *name, int T, int D, int F, int act, const void *x, const void *W) {
+    if (T < 1 || D < 1 || F < 1) return set_error(ISAM_ERR_INVALID_ARG, "%s: sizes must be >= 1", name);
+    if (act < ISAM_ACT_SILU || act > ISAM_ACT_SIGMOID)
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: unknown activation %d", name, act);
+    if (!x || !W) return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
+    if (D % 8 != 0) return set_error(ISAM_ERR_UNSUPPORTED, "%s: D (%d) must be a multiple of 8", name, D);
+    if (F > (1 << 29)) return set_error(ISAM_ERR_UNSUPPORTED, "%s: F (%d) is above 2^29", name, F);
+    if (!aligned(x, 16) || !aligned(W, 16))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: x and W must be 16-byte aligned", name);
+    return ISAM_OK;
+}
+
+int w4_validate(const char *name, int N, int K, int group) {
+    if (N < 1 || K < 1) return set_error(ISAM_ERR_INVALID_ARG, "%s: sizes must be >= 1", name);
+    if (group != 32 && group != 64 && group != 128)
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: group must be 32, 64 or 128", name);
+    if (K % 8 != 0) return set_error(ISAM_ERR_UNSUPPORTED, "%s: K (%d) must be a multiple of 8", name, K);
+    // The tiled words are counted in 64 bits, their blocks of 256 in 31.
+    if (static_cast<int64_t>((N + 15LL) / 16) * ((K + 127LL) / 128) > 0x7fffffffLL)
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: more than 2^31 weight tiles", name);
+    return ISAM_OK;
+}
+
+}  // namespace
+
+int isam_glr_forward(int T, int batch, int hidden, int g_type, const void *g, const float *h0,
+                     const int32_t *lengths, int h_type, void *h_out, float *h_last) {
+    int rc = glr_validate("isam_glr_forward", T, batch, hidden, g_type, h_type, g, h_out);
+    if (rc) return rc;
+    if (!aligned(h0, 4) || !aligned(lengths, 4) || !aligned(h_last, 4))
+        return set_error(ISAM_ERR_UNSUPPORTED, "isam_glr_forward: a pointer is not aligned to its element");
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    GlrDesc p{};
+    p.T = T, p.batch = batch, p.hidden = hidden, p.g_type = g_type, p.h_type = h_type;
+    p.g = g, p.h0 = h0, p.lengths = lengths, p.h_out = h_out, p.h_last = h_last;
+    return glr_forward_launch(p, *ds, current_stream());
+}
+
+int isam_glr_backward(int T, int batch, int hidden, int g_type, const void *g, const float *h0,
+                      const int32_t *lengths, int h_type, const void *h_out, const void *dh_out,
+                      const float *dh_last, void *dg, float *dh0) {
+    int rc = glr_validate("isam_glr_backward", T, batch, hidden, g_type, h_type, g, h_out);
+    if (rc) return rc;
+    if (!dg) return set_error(ISAM_ERR_INVALID_ARG, "isam_glr_backward: null pointer");
+    if (!aligned(h0, 4) || !aligned(lengths, 4) || !aligned(dh_last, 4) || !aligned(dh0, 4) ||
+        !aligned(dh_out, h_type == ISAM_F32 ? 4 : 2) || !aligned(dg, g_type == ISAM_F32 ? 4 : 2))
+        return set_error(ISAM_ERR_UNSUPPORTED, "isam_glr_backward: a pointer is not aligned to its element");
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    GlrDesc p{};
+    p.T = T, p.batch = batch, p.hidden = hidden, p.g_type = g_type, p.h_type = h_type;
+    p.g = g, p.h0 = h0, p.lengths = lengths, p.h_in = h_out, p.dh_out = dh_out, p.dh_last = dh_last;
+    p.dg = dg, p.dh0 = dh0;
+    return glr_backward_launch(p, *ds, current_stream());
+}
+
+int isam_glr_step(int batch, int hidden, int slots, int g_type, const void *g, const int32_t *slot_ids,
+                  const float *state, float *new_state, int h_type, void *h) {
+    int rc = glr_validate("isam_glr_step", 1, batch, hidden, g_type, h_type, g, h);
+    if (rc) return rc;
+    if (slots < 1) return set_error(ISAM_ERR_INVALID_ARG, "isam_glr_step: sizes must be >= 1");
+    if (!state || !new_state) return set_error(ISAM_ERR_INVALID_ARG, "isam_glr_step: null pointer");
+    if (!slot_ids && batch > slots)
+        return set_error(ISAM_ERR_INVALID_ARG, "isam_glr_step: batch (%d) above slots (%d) without slot_ids", batch,
+                         slots);
+    if (!aligned(slot_ids, 4) || !aligned(state, 4) || !aligned(new_state, 4))
+        return set_error(ISAM_ERR_UNSUPPORTED, "isam_glr_step: a pointer is not aligned to its element");
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    return glr_step_launch(batch, hidden, slots, g_type, g, slot_ids, state, new_state, h_type, h, current_stream());
+}
+
+int isam_glu_forward(int T, int D, int F, int act, const isam_bf16 *x, const isam_bf16 *W, isam_bf16 *h) {
+    int rc = glu_validate("isam_glu_forward", T, D, F, act, x, W);
+    if (rc) return rc;
+    if (!h) return set_error(ISAM_ERR_INVALID_ARG, "isam_glu_forward: null pointer");
+    if (!aligned(h, 2)) return set_error(ISAM_ERR_UNSUPPORTED, "isam_glu_forward: h must be 2-byte aligned");
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    GluDesc p{};
+    p.T = T, p.D = D, p.F = F, p.act = act, p.x = x, p.W = W, p.h = h;
+    return glu_forward_launch(p, *ds, current_stream());
+}
+
+int isam_glu_backward_workspace(int T, int D, int F, size_t *bytes) {
+    if (T < 1 || D < 1 || F < 1 || !bytes)
+        return set_error(ISAM_ERR_INVALID_ARG, "isam_glu_backward_workspace: sizes must be >= 1, bytes non-null");
+    *bytes = glu_backward_workspace(T, D, F);
+    return ISAM_OK;
+}
+
+int isam_glu_backward(int T, int D, int F, int act, const isam_bf16 *x, const isam_bf16 *W, const isam_bf16 *dh,
+                      void *workspace, isam_bf16 *dx, isam_bf16 *dW) {
+    int rc = glu_validate("isam_glu_backward", T, D, F, act, x, W);
+    if (rc) return rc;
+    if (!dh || !workspace) return set_error(ISAM_ERR_INVALID_ARG, "isam_glu_backward: null pointer");
+    if (F % 8 != 0) return set_error(ISAM_ERR_UNSUPPORTED, "isam_glu_backward: F (%d) must be a multiple of 8", F);
+    if (!aligned(dh, 16) || !aligned(workspace, 16) || !aligned(dx, 16) || !aligned(dW, 16))
+        return set_error(ISAM_ERR_UNSUPPORTED, "isam_glu_backward: pointers must be 16-byte aligned");
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    GluDesc p{};
+    p.T = T, p.D = D, p.F = F, p.act = act, p.x = x, p.W = W, p.dh = dh, p.workspace = workspace;
+    p.dx = dx, p.dW = dW;
+    return glu_backward_launch(p, *ds, current_stream());
+}
+
+int isam_w4_pack(int N, int K, int group, const uint8_t *codes, const isam_bf16 *scales, uint8_t *tiled,
+                 isam_bf16 *tiled_scales) {
+    int rc = w4_validate("isam_w4_pack", N, K, group);
+    if (rc) return rc;
+    if (!codes || !scales || !tiled || !tiled_scales)
+        return set_error(ISAM_ERR_INVALID_ARG, "isam_w4_pack: null pointer");
+    if (!aligned(tiled, 16) || !aligned(tiled_scales, 16) || !aligned(scales, 2))
+        return set_error(ISAM_ERR_UNSUPPORTED, "isam_w4_pack: misaligned pointer");
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    return w4_pack_launch(N, K, group, codes, scales, tiled, tiled_scales, current_stream());
+}
+
+int isam_gemv_w4(int M, int N, int K, int group, const isam_bf16 *x, const uint8_t *tiled,
+                 const isam_bf16 *tiled_scales, float *y) {
+    if (M < 1) return set_error(ISAM_ERR_INVALID_ARG, "isam_gemv_w4: sizes must be >= 1");
+    int rc = w4_validate("isam_gemv_w4", N, K, group);
+    if (rc) return rc;
+    if (!x || !tiled || !tiled_scales || !y) return set_error(ISAM_ERR_INVALID_ARG, "isam_gemv_w4: null pointer");
+    if (M > 32) return set_error(ISAM_ERR_UNSUPPORTED, "isam_gemv_w4: M (%d) is above 32", M);
+    if (!aligned(x, 16) || !aligned(tiled, 16) || !aligned(tiled_scales, 16) || !aligned(y, 4))
+        return set_error(ISAM_ERR_UNSUPPORTED, "isam_gemv_w4: misaligned pointer");
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    return gemv_w4_launch(M, N, K, group, x, tiled, tiled_scales, y, *ds, current_stream());
+}
+
 }  // extern "C"

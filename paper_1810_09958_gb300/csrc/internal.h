@@ -155,4 +155,46 @@ int depthwise_launch(int N, int H, int W, int C, const uint16_t *x, const uint16
 // out[4]: kernel (0 row ring, 1 per-pixel), image rows per tile, channel blocks, block width.
 int dwsep_plan(int W, int Cin, int Cout, int smem_optin, int *out);
 
+// Gated linear recurrence (forward uses h_out and h_last; backward h_in,
+// dh_out, dh_last, dg and dh0).  Null pointers as in include/isam.h.
+struct GlrDesc {
+    int T, batch, hidden;
+    int g_type, h_type;
+    const void *g;
+    const float *h0;
+    const int32_t *lengths;
+    void *h_out;
+    float *h_last;
+    const void *h_in;
+    const void *dh_out;
+    const float *dh_last;
+    void *dg;
+    float *dh0;
+};
+int glr_forward_launch(const GlrDesc &p, DeviceState &ds, cudaStream_t s);
+int glr_backward_launch(const GlrDesc &p, DeviceState &ds, cudaStream_t s);
+int glr_step_launch(int batch, int hidden, int slots, int g_type, const void *g, const int32_t *slot_ids,
+                    const float *state, float *new_state, int h_type, void *h, cudaStream_t s);
+
+// Gated feed-forward product (forward: h; backward: dh, workspace, dx, dW).
+struct GluDesc {
+    int T, D, F;
+    int act;
+    const uint16_t *x;
+    const uint16_t *W;
+    uint16_t *h;
+    const uint16_t *dh;
+    void *workspace;
+    uint16_t *dx;
+    uint16_t *dW;
+};
+int glu_forward_launch(const GluDesc &p, DeviceState &ds, cudaStream_t s);
+size_t glu_backward_workspace(int T, int D, int F);
+int glu_backward_launch(const GluDesc &p, DeviceState &ds, cudaStream_t s);
+
+int w4_pack_launch(int N, int K, int group, const uint8_t *codes, const uint16_t *scales, uint8_t *tiled,
+                   uint16_t *tiled_scales, cudaStream_t s);
+int gemv_w4_launch(int M, int N, int K, int group, const uint16_t *x, const uint8_t *tiled, const uint16_t *scales,
+                   float *y, DeviceState &ds, cudaStream_t s);
+
 }  // namespace isam

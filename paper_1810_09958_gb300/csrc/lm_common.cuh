@@ -1,0 +1,67 @@
+// lm_common.cuh -- element types, the gate and the activations shared by the
+// gated linear recurrence and the gated feed-forward kernels.
+#pragma once
+#include <cuda_bf16.h>
+
+#include "internal.h"
+
+namespace isam {
+
+using bf16 = __nv_bfloat16;
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(bf16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) {
+    return v;
+}
+template <>
+__device__ __forceinline__ bf16 from_f32<bf16>(float v) {
+    return __float2bfloat16_rn(v);
+}
+
+// sigmoid(x) and 1 - sigmoid(x), each to a few units in the last place of
+// its own size (the smaller of the two is not a difference from 1): with
+// e = exp(-|x|) they are 1 / (1 + e) and e / (1 + e), in the order of x's sign.
+struct Gate {
+    float keep;  // sigmoid(x)
+    float take;  // 1 - sigmoid(x)
+};
+__device__ __forceinline__ Gate gate(float x) {
+    const float e = __expf(-fabsf(x));
+    const float r = __fdividef(1.0f, 1.0f + e);
+    const float s = e * r;
+    return x >= 0.0f ? Gate{r, s} : Gate{s, r};
+}
+
+// act(a) and its derivative.
+template <int ACT>
+__device__ __forceinline__ void activation(float a, float &v, float &dv) {
+    if (ACT == ISAM_ACT_RELU) {
+        v = a > 0.0f ? a : (a != a ? a : 0.0f);
+        dv = a > 0.0f ? 1.0f : 0.0f;
+    } else if (ACT == ISAM_ACT_GELU) {
+        // a P(a) with P the normal distribution function, (1 + erf(a / sqrt 2)) / 2.
+        const float p = 0.5f + 0.5f * erff(a * 0.70710678118654752f);
+        v = a * p;
+        dv = p + a * (0.39894228040143268f * __expf(-0.5f * a * a));
+    } else {
+        const Gate s = gate(a);
+        if (ACT == ISAM_ACT_SIGMOID) {
+            v = s.keep;
+            dv = s.keep * s.take;
+        } else {
+            v = a * s.keep;
+            dv = s.keep * (1.0f + a * s.take);
+        }
+    }
+}
+
+inline int launch_status(const char *what) {
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? ISAM_OK : cuda_error(e, what);
+}
+
+}  // namespace isam

@@ -72,13 +72,24 @@ def load():
         lib.isam_gemm_plan_for.argtypes = [i, i, i, i, i, f, i, i, P, P]
         lib.isam_gru_plan_info.argtypes = [i, i, i, i, P]
         lib.isam_gru_plan_for.argtypes = [i, i, i, i, i, i, P]
+        lib.isam_glr_forward.argtypes = [i, i, i, i, P, P, P, i, P, P]
+        lib.isam_glr_backward.argtypes = [i, i, i, i, P, P, P, i, P, P, P, P, P]
+        lib.isam_glr_step.argtypes = [i, i, i, i, P, P, P, P, i, P]
+        lib.isam_glu_forward.argtypes = [i, i, i, i, P, P, P]
+        lib.isam_glu_backward_workspace.argtypes = [i, i, i, P]
+        lib.isam_glu_backward.argtypes = [i, i, i, i, P, P, P, P, P, P]
+        lib.isam_w4_pack.argtypes = [i, i, i, P, P, P, P]
+        lib.isam_gemv_w4.argtypes = [i, i, i, i, P, P, P, P]
         for name in ("isam_version", "isam_set_stream", "isam_sync", "isam_shutdown", "isam_gemm",
                      "isam_gemm_plan_info", "isam_gemm_plan_info2", "isam_gemm_grouped", "isam_gemm_fp8", "isam_gemm_grouped_fp8",
                      "isam_gemm_mxfp8", "isam_gemm_grouped_mxfp8",
                      "isam_gru_forward", "isam_gru_forward_reset_before",
                      "isam_gru_forward_stack",
                      "isam_dwsep_conv", "isam_dwsep_plan_info", "isam_dwsep_plan_for", "isam_depthwise_conv3x3",
-                     "isam_gru_plan_info", "isam_gru_plan_for", "isam_gemm_plan_for"):
+                     "isam_gru_plan_info", "isam_gru_plan_for", "isam_gemm_plan_for",
+                     "isam_glr_forward", "isam_glr_backward", "isam_glr_step",
+                     "isam_glu_forward", "isam_glu_backward_workspace", "isam_glu_backward",
+                     "isam_w4_pack", "isam_gemv_w4"):
             getattr(lib, name).restype = ctypes.c_int
         _lib = lib
         return lib
@@ -362,3 +373,164 @@ def gru_plan(layers, batch, hidden, reset_before=False, num_sms=None, smem_optin
     else:
         check(lib.isam_gru_plan_for(layers, batch, hidden, int(bool(reset_before)), num_sms, smem_optin, out))
     return dict(zip(_GRU_PLAN_KEYS, list(out)))
+
+
+def _elem_type(t, name):
+    """ISAM_F32 or ISAM_BF16 of a tensor."""
+    import torch
+    if t.dtype == torch.float32:
+        return 0
+    if t.dtype == torch.bfloat16:
+        return 1
+    raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+
+
+def _opt(t, dtype, numel, name):
+    if t is not None:
+        _dev(t, dtype, numel, name)
+
+
+def glr_forward(T, batch, hidden, g, h0, lengths, h_out, h_last=None) -> None:
+    """isam_glr_forward: h_t = z h_{t-1} + (1 - z) n over T steps, z = sigmoid of
+    the first and n the second half of g's rows (g [T,batch,2H] and h_out
+    [T,batch,H] fp32 or bf16; h0, h_last [batch,H] fp32 or None; lengths
+    [batch] int32 or None)."""
+    import torch
+    lib = load()
+    gt, ht = _elem_type(g, "g"), _elem_type(h_out, "h_out")
+    _dev(g, g.dtype, T * batch * 2 * hidden, "g")
+    _opt(h0, torch.float32, batch * hidden, "h0")
+    _opt(lengths, torch.int32, batch, "lengths")
+    _dev(h_out, h_out.dtype, T * batch * hidden, "h_out")
+    _opt(h_last, torch.float32, batch * hidden, "h_last")
+    _use_current_stream(lib)
+    check(lib.isam_glr_forward(T, batch, hidden, gt, _ptr(g), _ptr(h0), _ptr(lengths), ht, _ptr(h_out), _ptr(h_last)))
+
+
+def glr_backward(T, batch, hidden, g, h0, lengths, h_out, dh_out, dh_last, dg, dh0=None) -> None:
+    """isam_glr_backward: gradients dg (g's shape and type) and dh0 [batch,H]
+    fp32 (or None) of glr_forward from dh_out (h_out's shape and type, or None)
+    and dh_last [batch,H] fp32 (or None)."""
+    import torch
+    lib = load()
+    gt, ht = _elem_type(g, "g"), _elem_type(h_out, "h_out")
+    _dev(g, g.dtype, T * batch * 2 * hidden, "g")
+    _opt(h0, torch.float32, batch * hidden, "h0")
+    _opt(lengths, torch.int32, batch, "lengths")
+    _dev(h_out, h_out.dtype, T * batch * hidden, "h_out")
+    _opt(dh_out, h_out.dtype, T * batch * hidden, "dh_out")
+    _opt(dh_last, torch.float32, batch * hidden, "dh_last")
+    _dev(dg, g.dtype, T * batch * 2 * hidden, "dg")
+    _opt(dh0, torch.float32, batch * hidden, "dh0")
+    _use_current_stream(lib)
+    check(lib.isam_glr_backward(T, batch, hidden, gt, _ptr(g), _ptr(h0), _ptr(lengths), ht, _ptr(h_out), _ptr(dh_out),
+                                _ptr(dh_last), _ptr(dg), _ptr(dh0)))
+
+
+def glr_step(batch, hidden, slots, g, slot_ids, state, new_state, h) -> None:
+    """isam_glr_step: one token for `batch` sequences whose fp32 states are rows
+    slot_ids (int32, or None for row b) of state [slots,H]; new_state may be
+    state; h [batch,H] fp32 or bf16."""
+    import torch
+    lib = load()
+    gt, ht = _elem_type(g, "g"), _elem_type(h, "h")
+    _dev(g, g.dtype, batch * 2 * hidden, "g")
+    _opt(slot_ids, torch.int32, batch, "slot_ids")
+    _dev(state, torch.float32, slots * hidden, "state")
+    _dev(new_state, torch.float32, slots * hidden, "new_state")
+    _dev(h, h.dtype, batch * hidden, "h")
+    _use_current_stream(lib)
+    check(lib.isam_glr_step(batch, hidden, slots, gt, _ptr(g), _ptr(slot_ids), _ptr(state), _ptr(new_state), ht, _ptr(h)))
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
+
+
+def _act_code(act):
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}, got {act!r}")
+    return ACTIVATIONS[act]
+
+
+def glu_forward(T, D, F, act, x, W, h) -> None:
+    """isam_glu_forward: h = act(x Wg^T) * (x Wu^T) (x [T,D], W [2F,D] with the
+    gate rows first, h [T,F], all bf16; act "silu", "gelu", "relu" or "sigmoid")."""
+    import torch
+    lib = load()
+    code = _act_code(act)
+    _dev(x, torch.bfloat16, T * D, "x")
+    _dev(W, torch.bfloat16, 2 * F * D, "W")
+    _dev(h, torch.bfloat16, T * F, "h")
+    _use_current_stream(lib)
+    check(lib.isam_glu_forward(T, D, F, code, _ptr(x), _ptr(W), _ptr(h)))
+
+
+def glu_backward_workspace(T, D, F) -> int:
+    """isam_glu_backward_workspace: bytes of glu_backward's workspace."""
+    out = ctypes.c_size_t()
+    check(load().isam_glu_backward_workspace(T, D, F, ctypes.byref(out)))
+    return out.value
+
+
+def glu_backward(T, D, F, act, x, W, dh, dx, dW, workspace=None) -> None:
+    """isam_glu_backward: dx [T,D] and dW [2F,D] (bf16, either may be None) of
+    glu_forward from dh [T,F]; workspace a uint8 tensor of
+    glu_backward_workspace bytes, or None to take one from torch's allocator
+    on the current stream."""
+    import torch
+    lib = load()
+    code = _act_code(act)
+    _dev(x, torch.bfloat16, T * D, "x")
+    _dev(W, torch.bfloat16, 2 * F * D, "W")
+    _dev(dh, torch.bfloat16, T * F, "dh")
+    _opt(dx, torch.bfloat16, T * D, "dx")
+    _opt(dW, torch.bfloat16, 2 * F * D, "dW")
+    need = glu_backward_workspace(T, D, F)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    _dev(workspace, torch.uint8, workspace.numel(), "workspace")
+    if workspace.numel() < need:
+        raise ValueError(f"workspace has {workspace.numel()} bytes, {need} are needed")
+    _use_current_stream(lib)
+    check(lib.isam_glu_backward(T, D, F, code, _ptr(x), _ptr(W), _ptr(dh), _ptr(workspace), _ptr(dx), _ptr(dW)))
+
+
+def w4_tiled_bytes(N, K) -> int:
+    """Bytes of the tiled codes of an N x K matrix."""
+    return (N + 15) // 16 * ((K + 127) // 128) * 1024
+
+
+def w4_tiled_scales(N, K, group) -> int:
+    """Elements of the tiled scales of an N x K matrix."""
+    return (N + 15) // 16 * ((K + 127) // 128) * 16 * (128 // group)
+
+
+def w4_pack(N, K, group, codes, scales, tiled, tiled_scales) -> None:
+    """isam_w4_pack: codes [N,K/2] (uint8, even k in the low half) and scales
+    [N,ceil(K/group)] (bf16) into the tiled order gemv_w4 reads (uint8
+    w4_tiled_bytes, bf16 w4_tiled_scales)."""
+    import torch
+    lib = load()
+    if group not in (32, 64, 128):
+        raise ValueError(f"group must be 32, 64 or 128, got {group}")
+    _dev(codes, torch.uint8, N * (K // 2), "codes")
+    _dev(scales, torch.bfloat16, N * ((K + group - 1) // group), "scales")
+    _dev(tiled, torch.uint8, w4_tiled_bytes(N, K), "tiled")
+    _dev(tiled_scales, torch.bfloat16, w4_tiled_scales(N, K, group), "tiled_scales")
+    _use_current_stream(lib)
+    check(lib.isam_w4_pack(N, K, group, _ptr(codes), _ptr(scales), _ptr(tiled), _ptr(tiled_scales)))
+
+
+def gemv_w4(M, N, K, group, x, tiled, tiled_scales, y) -> None:
+    """isam_gemv_w4: y [M,N] fp32 = x [M,K] bf16 times 4-bit weights in
+    w4_pack's order, M <= 32."""
+    import torch
+    lib = load()
+    if group not in (32, 64, 128):
+        raise ValueError(f"group must be 32, 64 or 128, got {group}")
+    _dev(x, torch.bfloat16, M * K, "x")
+    _dev(tiled, torch.uint8, w4_tiled_bytes(N, K), "tiled")
+    _dev(tiled_scales, torch.bfloat16, w4_tiled_scales(N, K, group), "tiled_scales")
+    _dev(y, torch.float32, M * N, "y")
+    _use_current_stream(lib)
+    check(lib.isam_gemv_w4(M, N, K, group, _ptr(x), _ptr(tiled), _ptr(tiled_scales), _ptr(y)))
