@@ -463,7 +463,7 @@ enum { ISAM_F32 = 0, ISAM_BF16 = 1 };
  *
  * Gates, products and states are evaluated and carried in fp32; only h_out is
  * rounded.  Results do not depend on timing (no atomics).
- * Any T, batch, hidden >= 1 with T * batch * 2 * hidden below 2^40; pointers
+ * Any T up to 2^30, batch, hidden >= 1, at most 2^40 gate values; pointers
  * aligned to their element.  ISAM_ERR_INVALID_ARG for sizes < 1, null
  * pointers or unknown types; ISAM_ERR_UNSUPPORTED beyond the size limit or
  * for misaligned pointers.  Asynchronous on the stream set by

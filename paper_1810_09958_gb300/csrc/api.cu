@@ -580,8 +580,8 @@ int glr_validate(const char *name, int64_t T, int64_t batch, int64_t hidden, int
     if ((g_type != ISAM_F32 && g_type != ISAM_BF16) || (h_type != ISAM_F32 && h_type != ISAM_BF16))
         return set_error(ISAM_ERR_INVALID_ARG, "%s: types must be ISAM_F32 or ISAM_BF16", name);
     if (!g || !h) return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
-    if (batch * hidden > (int64_t{1} << 40) / (2 * T))
-        return set_error(ISAM_ERR_UNSUPPORTED, "%s: more than 2^40 gate values", name);
+    if (T > (1 << 30) || batch * hidden > (int64_t{1} << 40) / (2 * T))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: more than 2^30 steps or 2^40 gate values", name);
     if (!aligned(g, g_type == ISAM_F32 ? 4 : 2) || !aligned(h, h_type == ISAM_F32 ? 4 : 2))
         return set_error(ISAM_ERR_UNSUPPORTED, "%s: a pointer is not aligned to its element", name);
     return ISAM_OK;
