@@ -219,6 +219,22 @@ int make_tmap_3d_bf16(CUtensorMap *out, const void *base, const uint64_t dims_in
     return encode(out, key, 3, base, dims, strides, box);
 }
 
+int make_tmap_3d_plain(CUtensorMap *out, const void *base, bool f32, const uint64_t dims_in[3],
+                       const uint64_t strides_bytes[2], const uint32_t box_in[3]) {
+    const uint64_t key[12] = {f32 ? 0x3F32ull : 0x3B16ull, reinterpret_cast<uint64_t>(base),
+                              dims_in[0],  dims_in[1],
+                              dims_in[2],  strides_bytes[0],
+                              strides_bytes[1], box_in[0],
+                              box_in[1],   box_in[2],
+                              0,           0};
+    cuuint64_t dims[3] = {dims_in[0], dims_in[1], dims_in[2]};
+    cuuint64_t strides[2] = {strides_bytes[0], strides_bytes[1]};
+    cuuint32_t box[3] = {box_in[0], box_in[1], box_in[2]};
+    return encode(out, key, 3, base, dims, strides, box,
+                  f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                  CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
 }  // namespace isam
 
 using namespace isam;

@@ -14,17 +14,28 @@
 //
 // The warps of a CTA follow each other in time, the CTAs of a cluster too, and
 // a cluster walks its channels' time axis in rounds of (CTAs x warps x L)
-// steps, the next round's gates in flight while a round is folded.  Folds pass
-// between warps through shared memory, between CTAs through distributed shared
-// memory (one cluster barrier per round, buffers alternate); every warp
-// carries the state at the end of the round itself, from the same folds in
-// the same order, so nothing depends on timing.  The cluster size (1 to 8) is
-// picked so that one long sequence fills the GPU as a batch does.
+// steps, then takes the next channels (the grid is no larger than what is
+// resident).  Each warp has its own ring of tiles in shared memory, filled by
+// TMA (where rows are not 16-byte aligned: by each lane with asynchronous
+// copies of its own elements), so the loads of later rounds stay in flight
+// while a round is folded; states leave through shared memory and TMA as well.
+// With gates loaded straight into registers the forward kernel spent 34
+// instructions an element, half of them addresses, and stopped at 55% of the
+// copy bandwidth.  Folds pass between warps through shared memory, between
+// CTAs through distributed shared memory (asynchronous stores counted on an
+// mbarrier, buffers alternate; a cluster barrier per round, whose release waits
+// for the states' stores, took 529 us where this took 243 us on
+// 65536 x 1 x 2560); every warp carries the state at the end of the round
+// itself, from the same folds in the same order, so nothing depends on timing.
+// The cluster size (1 to 8) is picked so that one long sequence fills the GPU
+// as a batch does.
 //
 // The backward pass is the same scan from the last step to the first with
 // e_t = z_t (dh_t + e_{t+1}), d_t = dh_t + e_{t+1}.
 #include <algorithm>
+#include <mutex>
 
+#include "gemm_common.cuh"
 #include "internal.h"
 #include "lm_common.cuh"
 #include "ptx.cuh"
@@ -36,6 +47,7 @@ namespace {
 constexpr int kMaxWarps = 8;
 constexpr int kMaxCluster = 8;
 constexpr int kCtasPerSm = 2;  // launch bounds: at most 128 registers a thread
+constexpr int kStages = 2;     // tiles of each input in a warp's ring
 constexpr int kStepThreads = 128;
 
 // V neighbouring elements, moved as one word; data used once, so loads and
@@ -102,18 +114,68 @@ struct Fold {
 };
 __device__ __forceinline__ float positive(float a) { return fmaxf(a, 1.17549435e-38f); }
 
-// Folds of one round: of the CTA's warps, and of the cluster's CTAs.
+// Folds of one round: of the CTA's warps, and of the cluster's CTAs (written
+// by them, their bytes counted on `landed`).
 template <int V>
 struct FoldBuffers {
     Fold<V> warp[2][kMaxWarps][32];
     Fold<V> cta[2][kMaxCluster][32];
+    uint64_t landed[2];
+    int abort;
 };
+
+// Buffers of round r are written again in round r + 2.  A CTA sends its fold of
+// round r + 1 after all its warps are done with round r (their barrier in
+// exchange), and a fold of round r + 2 is sent by a warp that holds every
+// CTA's fold of round r + 1: nothing still reads, or waits for, round r.
+template <int V>
+__device__ __forceinline__ void exchange_init(FoldBuffers<V> &s, uint32_t cluster) {
+    if (threadIdx.x == 0) {
+        mbar_init(&s.landed[0], 1);
+        mbar_init(&s.landed[1], 1);
+        s.abort = 0;
+        fence_mbar_init();
+    }
+    if (cluster == 1)
+        __syncthreads();
+    else
+        cluster_sync_all();
+}
+
+// The end of a kernel: stores have left shared memory; after a wait that ran
+// out, copies into this CTA's shared memory get time to land; and no CTA leaves
+// while another may still send it folds.
+template <int V>
+__device__ __forceinline__ void exchange_end(FoldBuffers<V> &s, uint32_t cluster) {
+    if ((threadIdx.x & 31) == 0) bulk_wait_all<0>();
+    if (*static_cast<volatile int *>(&s.abort)) {
+        const unsigned long long t0 = globaltimer();
+        while (globaltimer() - t0 < 50000ull) {
+        }
+    }
+    __syncwarp();
+    if (cluster > 1) cluster_sync_all();
+}
+
+// Eight or sixteen bytes into a CTA of this cluster, counted on its barrier.
+// Asynchronous: unlike a release, it does not wait for this thread's stores of
+// states to reach L2.
+__device__ __forceinline__ void send(uint32_t to, const Fold<2> &f, uint32_t bar) {
+    st_async_f4(to, make_float4(f.a[0], f.a[1], f.b[0], f.b[1]), bar);
+}
+__device__ __forceinline__ void send(uint32_t to, const Fold<1> &f, uint32_t bar) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to),
+                 "f"(f.a[0]), "f"(f.b[0]), "r"(bar)
+                 : "memory");
+}
 
 // What a warp needs from the others' folds: `in` becomes the state before its
 // first step of this round, `carry` the state after the round.
 template <int V>
-__device__ __forceinline__ void exchange(FoldBuffers<V> &s, int parity, Fold<V> &own, int warp, int warps, int lane,
-                                         uint32_t rank, uint32_t cluster, float (&carry)[V], float (&in)[V]) {
+__device__ __forceinline__ void exchange(FoldBuffers<V> &s, int r, Fold<V> &own, int warp, int warps, int lane,
+                                         uint32_t rank, uint32_t cluster, const WaitCtx &wait, float (&carry)[V],
+                                         float (&in)[V]) {
+    const int parity = r & 1;
 #pragma unroll
     for (int i = 0; i < V; ++i) own.a[i] = positive(own.a[i]);
     s.warp[parity][warp][lane] = own;
@@ -147,18 +209,13 @@ __device__ __forceinline__ void exchange(FoldBuffers<V> &s, int parity, Fold<V> 
             all.a[i] = positive(own.a[i] * before.a[i]);
             all.b[i] = own.a[i] * before.b[i] + own.b[i];
         }
-        const uint32_t at = smem_u32(&s.cta[parity][rank][lane]);
-        for (uint32_t q = 0; q < cluster; ++q) {
-            const uint32_t to = mapa_shared(at, q);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4 * i), "f"(all.a[i]) : "memory");
-                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4 * (V + i)), "f"(all.b[i]) : "memory");
-            }
-        }
+        if (lane == 0)
+            mbar_arrive_expect_tx(&s.landed[parity], cluster * 32u * static_cast<uint32_t>(sizeof(Fold<V>)));
+        const uint32_t at = smem_u32(&s.cta[parity][rank][lane]), bar = smem_u32(&s.landed[parity]);
+        for (uint32_t q = 0; q < cluster; ++q) send(mapa_shared(at, q), all, mapa_shared(bar, q));
     }
     __syncwarp();
-    cluster_sync_all();
+    bounded_wait<true>(&s.landed[parity], (r >> 1) & 1, wait, 0x603u);
     for (uint32_t q = 0; q < cluster; ++q) {
         const Fold<V> f = s.cta[parity][q][lane];
 #pragma unroll
@@ -171,245 +228,454 @@ __device__ __forceinline__ void exchange(FoldBuffers<V> &s, int parity, Fold<V> 
 
 struct ScanParams {
     GlrDesc d;
-    int tiles;  // channel tiles of 32 V per sequence
+    int tiles;       // channel tiles of 32 V per sequence
+    int64_t groups;  // tiles * batch: the units a cluster takes one after another
     uint32_t cluster;
     uint32_t *err;
+    unsigned long long timeout_ns;
 };
 
-// Where this thread works.
-template <int V>
-struct Place {
-    int lane, warp, warps, b, c;
-    uint32_t rank;
-    bool on;        // the lane's channels exist (idle lanes read the last ones)
-    int len;        // steps of this sequence
-    int64_t chain;  // b * hidden + c
-    __device__ Place(const ScanParams &p) {
+// Asynchronous copy of one word of this lane into shared memory (completion by
+// lane_copies_wait); two bytes are below what the instruction moves and go
+// through a register.
+template <int BYTES>
+__device__ __forceinline__ void lane_copy(void *dst, const void *src) {
+    if constexpr (BYTES == 2)
+        *static_cast<unsigned short *>(dst) = *static_cast<const unsigned short *>(src);
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(dst)), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void lane_copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void lane_copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// A tile: L rows of a warp's 32 V channels.
+template <typename T, int V, int L>
+struct Tile {
+    T v[L][32 * V];
+    // One word of a lane, as floats.
+    __device__ __forceinline__ void get(int k, int lane, float (&x)[V]) const {
+        Pack<T, V> p;
+        p.w = *reinterpret_cast<const typename Pack<T, V>::W *>(&v[k][lane * V]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = to_f32(p.v[i]);
+    }
+    __device__ __forceinline__ void put(int k, int lane, const float (&x)[V]) {
+        Pack<T, V> p;
+#pragma unroll
+        for (int i = 0; i < V; ++i) p.v[i] = from_f32<T>(x[i]);
+        *reinterpret_cast<typename Pack<T, V>::W *>(&v[k][lane * V]) = p.w;
+    }
+};
+
+// Shared memory of a warp (tiles start 128-byte aligned: every size is a
+// multiple of 128).
+template <typename G, typename Hy, int V, int L>
+struct ForwardTiles {
+    struct In {
+        Tile<G, V, L> z, n;
+    } in[kStages];
+    Tile<Hy, V, L> out;
+};
+template <typename G, typename Hy, int V, int L>
+struct BackwardTiles {
+    struct In {
+        Tile<G, V, L> z, n;
+        Tile<Hy, V, L> before, dh;
+    } in[kStages];
+    Tile<G, V, L> dz, dn;
+};
+
+// A warp's place in its cluster, and one group of channels.
+struct Warp {
+    int lane, warp, warps;
+    uint32_t rank, cluster;
+    int chunk, span;  // this warp's L steps in a round of span warps, in time order
+    int64_t id, ids;  // this cluster, clusters of the grid
+    __device__ Warp(const ScanParams &p) {
         lane = threadIdx.x & 31;
         warp = threadIdx.x >> 5;
         warps = blockDim.x >> 5;
-        rank = blockIdx.x % p.cluster;
-        const uint32_t group = blockIdx.x / p.cluster;
-        b = group / p.tiles;
-        c = (static_cast<int>(group) - b * p.tiles) * 32 * V + lane * V;
-        on = c < p.d.hidden;
-        c = min(c, p.d.hidden - V);
+        cluster = p.cluster;
+        rank = blockIdx.x % cluster;
+        id = blockIdx.x / cluster;
+        ids = gridDim.x / cluster;
+        chunk = rank * warps + warp;
+        span = warps * cluster;
+    }
+};
+template <int V>
+struct Group {
+    int b, c;       // sequence, first channel of the tile
+    int len;        // steps of this sequence
+    int own;        // this lane's first channel, moved back into the row where the tile passes its end
+    bool on;        // the lane's channels exist
+    int64_t chain;  // b * hidden + own
+    __device__ __forceinline__ Group(const ScanParams &p, int64_t g, int lane) {
+        b = static_cast<int>(g / p.tiles);
+        c = static_cast<int>(g - static_cast<int64_t>(b) * p.tiles) * 32 * V;
+        on = c + lane * V < p.d.hidden;
+        own = min(c + lane * V, p.d.hidden - V);
         len = p.d.T;
         if (p.d.lengths) len = min(max(p.d.lengths[b], 0), p.d.T);
-        chain = static_cast<int64_t>(b) * p.d.hidden + c;
+        chain = static_cast<int64_t>(b) * p.d.hidden + own;
     }
 };
 
-template <typename G, typename Hy, int V, int L>
-__global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm) glr_forward_kernel(const ScanParams p) {
-    if (p.cluster > 1 && !launch_shape_ok(p.err, p.cluster, gridDim.x, 0x601u)) return;
-    __shared__ FoldBuffers<V> folds;
-    const Place<V> at(p);
-    const int hidden = p.d.hidden;
-    const int64_t step = static_cast<int64_t>(p.d.batch) * hidden;
-    const int span = at.warps * L, round = span * p.cluster;
-    const int rounds = (at.len + round - 1) / round;
-    const int first = at.rank * span + at.warp * L;
-    const G *g = static_cast<const G *>(p.d.g) + at.chain + static_cast<int64_t>(at.b) * hidden;  // rows of 2 hidden
-    Hy *out = static_cast<Hy *>(p.d.h_out) + at.chain;
-
-    float carry[V];
+// One value per channel of a lane from a [batch][hidden] array (or zero).
+template <int V>
+__device__ __forceinline__ void edge(const float *from, int64_t chain, float (&x)[V]) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) carry[i] = p.d.h0 ? p.d.h0[at.chain + i] : 0.0f;
-
-    Pack<G, V> gz[L], gn[L];
-    const auto fetch = [&](int t) {
-        const int n = min(at.len - t, L);
-        const G *q = g + 2 * step * t;
-        if (n == L) {
-#pragma unroll
-            for (int i = 0; i < L; ++i, q += 2 * step) {
-                load<G, V>(gz[i], q);
-                load<G, V>(gn[i], q + hidden);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < L; ++i, q += 2 * step)
-                if (i < n) {
-                    load<G, V>(gz[i], q);
-                    load<G, V>(gn[i], q + hidden);
-                }
-        }
-    };
-    if (rounds > 0) fetch(first);
-    for (int r = 0; r < rounds; ++r) {
-        const int t = r * round + first;
-        const int n = min(at.len - t, L);  // steps of this warp, below 1 past the end
-        float z[L][V], b[L][V];
-        Fold<V> own;
-#pragma unroll
-        for (int i = 0; i < V; ++i) own.a[i] = 1.0f, own.b[i] = 0.0f;
-        if (n == L) {
-#pragma unroll
-            for (int k = 0; k < L; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const Gate s = scan_gate(to_f32(gz[k].v[i]));
-                    z[k][i] = s.keep;
-                    b[k][i] = s.take * to_f32(gn[k].v[i]);
-                }
-        } else {
-#pragma unroll
-            for (int k = 0; k < L; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    z[k][i] = 1.0f, b[k][i] = 0.0f;
-                    if (k < n) {
-                        const Gate s = scan_gate(to_f32(gz[k].v[i]));
-                        z[k][i] = s.keep;
-                        b[k][i] = s.take * to_f32(gn[k].v[i]);
-                    }
-                }
-        }
-#pragma unroll
-        for (int k = 0; k < L; ++k)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                own.a[i] *= z[k][i];
-                own.b[i] = z[k][i] * own.b[i] + b[k][i];
-            }
-        if (r + 1 < rounds) fetch(t + round);
-        float h[V];
-        exchange<V>(folds, r & 1, own, at.warp, at.warps, at.lane, at.rank, p.cluster, carry, h);
-        if (at.on) {
-            Hy *q = out + step * t;
-            const int left = p.d.T - t;
-#pragma unroll
-            for (int k = 0; k < L; ++k, q += step) {
-                float v[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    h[i] = z[k][i] * h[i] + b[k][i];
-                    v[i] = k < n ? h[i] : 0.0f;
-                }
-                if (k < left) store<Hy, V>(q, v);
-            }
-        }
-    }
-    if (at.on) {
-        const float zero[V] = {};
-        for (int t = rounds * round + at.rank * at.warps + at.warp; t < p.d.T; t += at.warps * p.cluster)
-            store<Hy, V>(out + step * t, zero);
-        if (p.d.h_last && at.rank == 0 && at.warp == 0) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) p.d.h_last[at.chain + i] = carry[i];
-        }
-    }
-    if (p.cluster > 1) cluster_sync_all();  // no CTA leaves while another may still write its folds
+    for (int i = 0; i < V; ++i) x[i] = from ? from[chain + i] : 0.0f;
 }
 
-template <typename G, typename Hy, int V, int L>
-__global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm) glr_backward_kernel(const ScanParams p) {
-    if (p.cluster > 1 && !launch_shape_ok(p.err, p.cluster, gridDim.x, 0x602u)) return;
+template <typename G, typename Hy, int V, int L, bool TMA>
+__global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
+    glr_forward_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_h,
+                       const __grid_constant__ ScanParams p) {
+    if (p.cluster > 1 && !launch_shape_ok(p.err, p.cluster, gridDim.x, 0x601u)) return;
+    using Tiles = ForwardTiles<G, Hy, V, L>;
+    extern __shared__ __align__(128) uint8_t smem[];
     __shared__ FoldBuffers<V> folds;
-    const Place<V> at(p);
+    __shared__ uint64_t full_all[kMaxWarps][kStages];
+    const WaitCtx wait{p.timeout_ns, p.err, &folds.abort};
+    const Warp w(p);
+    Tiles &mine = reinterpret_cast<Tiles *>(smem)[w.warp];
+    uint64_t *full = full_all[w.warp];
+    if (TMA && w.lane == 0) {
+        for (int i = 0; i < kStages; ++i) mbar_init(&full[i], 1);
+        fence_mbar_init();
+    }
+    exchange_init(folds, p.cluster);
     const int hidden = p.d.hidden;
     const int64_t step = static_cast<int64_t>(p.d.batch) * hidden;
-    const int span = at.warps * L, round = span * p.cluster;
-    const int rounds = (at.len + round - 1) / round;
-    const int first = at.rank * span + at.warp * L;  // counted back from the last step
-    const int64_t goff = at.chain + static_cast<int64_t>(at.b) * hidden;
-    const G *g = static_cast<const G *>(p.d.g) + goff;
-    G *dg = static_cast<G *>(p.d.dg) + goff;
-    const Hy *hs = static_cast<const Hy *>(p.d.h_in) + at.chain;
-    const Hy *dh = static_cast<const Hy *>(p.d.dh_out) + at.chain;
-    const bool has_dh = p.d.dh_out != nullptr;
+    const int round = w.span * L, first = w.chunk * L;
 
-    float carry[V], h0[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        carry[i] = p.d.dh_last ? p.d.dh_last[at.chain + i] : 0.0f;
-        h0[i] = p.d.h0 ? p.d.h0[at.chain + i] : 0.0f;
-    }
-
-    Pack<G, V> gz[L], gn[L];
-    Pack<Hy, V> hb[L], gh[L];
-    const auto fetch = [&](int t) {  // steps t, t - 1, ... (the first n exist)
-        const int n = min(t + 1, L);
-        const G *q = g + 2 * step * t;
-        const Hy *qh = hs + step * (t - 1);
-        const Hy *qd = dh + step * t;
-        if (t >= L && has_dh) {
-#pragma unroll
-            for (int k = 0; k < L; ++k, q -= 2 * step, qh -= step, qd -= step) {
-                load<G, V>(gz[k], q);
-                load<G, V>(gn[k], q + hidden);
-                load<Hy, V>(hb[k], qh);
-                load<Hy, V>(gh[k], qd);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < L; ++k, q -= 2 * step, qh -= step, qd -= step)
-                if (k < n) {
-                    load<G, V>(gz[k], q);
-                    load<G, V>(gn[k], q + hidden);
-                    if (k < t) load<Hy, V>(hb[k], qh);
-                    if (has_dh) load<Hy, V>(gh[k], qd);
+    // Loads run kStages rounds ahead of their use, across groups.
+    int64_t load_group = w.id;
+    int load_round = 0, load_stage = 0;
+    const auto fetch = [&]() {
+        for (; load_group < p.groups; load_group += w.ids, load_round = 0) {
+            const Group<V> g(p, load_group, w.lane);
+            if (load_round * round >= g.len) continue;
+            const int t = load_round * round + first;
+            typename Tiles::In &to = mine.in[load_stage];
+            if (t < g.len) {
+                if (TMA) {
+                    if (w.lane == 0) {
+                        mbar_arrive_expect_tx(&full[load_stage], sizeof(to));
+                        tma_load_3d(&tm_g, &full[load_stage], &to.z, g.c, 2 * g.b, t);
+                        tma_load_3d(&tm_g, &full[load_stage], &to.n, g.c, 2 * g.b + 1, t);
+                    }
+                } else {
+                    const G *q = static_cast<const G *>(p.d.g) + g.chain + static_cast<int64_t>(g.b) * hidden +
+                                 2 * step * t;
+                    for (int k = 0; k < min(g.len - t, L); ++k, q += 2 * step) {
+                        lane_copy<sizeof(G) * V>(&to.z.v[k][w.lane * V], q);
+                        lane_copy<sizeof(G) * V>(&to.n.v[k][w.lane * V], q + hidden);
+                    }
                 }
-        }
-    };
-    if (rounds > 0) fetch(at.len - 1 - first);
-    for (int r = 0; r < rounds; ++r) {
-        const int t = at.len - 1 - (r * round + first);
-        const int n = min(t + 1, L);
-        // z, 1 - z, (h_{t-1} - n) z (1 - z) and dh of each step.
-        float z[L][V], take[L][V], q[L][V], d[L][V];
-        Fold<V> own;
-#pragma unroll
-        for (int i = 0; i < V; ++i) own.a[i] = 1.0f, own.b[i] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < L; ++k)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const bool live = k < n;
-                const Gate s = scan_gate(to_f32(gz[k].v[i]));
-                const float before = k == t ? h0[i] : to_f32(hb[k].v[i]);
-                z[k][i] = live ? s.keep : 1.0f;
-                take[k][i] = s.take;
-                q[k][i] = (before - to_f32(gn[k].v[i])) * (s.keep * s.take);
-                d[k][i] = live && has_dh ? to_f32(gh[k].v[i]) : 0.0f;
-                own.a[i] *= z[k][i];
-                own.b[i] = z[k][i] * (own.b[i] + d[k][i]);
             }
-        if (r + 1 < rounds) fetch(t - round);
-        float e[V];
-        exchange<V>(folds, r & 1, own, at.warp, at.warps, at.lane, at.rank, p.cluster, carry, e);
-        if (at.on) {
-            G *o = dg + 2 * step * t;
+            ++load_round;
+            break;
+        }
+        if (!TMA) lane_copies_commit();
+        load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
+    };
+    for (int i = 0; i < kStages; ++i) fetch();
+
+    float next[V];
+    if (w.id < p.groups) edge<V>(p.d.h0, Group<V>(p, w.id, w.lane).chain, next);
+    int it = 0, stage = 0;
+    uint32_t phases = 0;
+    for (int64_t gi = w.id; gi < p.groups; gi += w.ids) {
+        const Group<V> g(p, gi, w.lane);
+        const int rounds = (g.len + round - 1) / round;
+        Hy *out = static_cast<Hy *>(p.d.h_out) + g.chain;
+        float carry[V];
 #pragma unroll
-            for (int k = 0; k < L; ++k, o -= 2 * step) {
-                float dz[V], dn[V];
+        for (int i = 0; i < V; ++i) carry[i] = next[i];
+        if (gi + w.ids < p.groups) edge<V>(p.d.h0, Group<V>(p, gi + w.ids, w.lane).chain, next);
+        for (int r = 0; r < rounds; ++r, ++it) {
+            const int t = r * round + first;
+            const int n = min(g.len - t, L);  // steps of this warp, below 1 past the end
+            if (TMA) {
+                if (n > 0) {
+                    bounded_wait(&full[stage], (phases >> stage) & 1u, wait, 0x604u);
+                    phases ^= 1u << stage;
+                }
+            } else {
+                lane_copies_wait<kStages - 1>();
+            }
+            float z[L][V], b[L][V];
+            const typename Tiles::In &in = mine.in[stage];
+#pragma unroll
+            for (int k = 0; k < L; ++k) {
+                float gz[V], gn[V];
+                in.z.get(k, w.lane, gz);
+                in.n.get(k, w.lane, gn);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float whole = d[k][i] + e[i];
-                    dz[i] = whole * q[k][i];
-                    dn[i] = whole * take[k][i];
-                    e[i] = z[k][i] * whole;
+                    const Gate s = scan_gate(gz[i]);
+                    z[k][i] = s.keep;
+                    b[k][i] = s.take * gn[i];
                 }
-                if (k < n) {
-                    store<G, V>(o, dz);
-                    store<G, V>(o + hidden, dn);
+            }
+            if (n < L) {
+#pragma unroll
+                for (int k = 0; k < L; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        if (k >= n) z[k][i] = 1.0f, b[k][i] = 0.0f;
+            }
+            __syncwarp();  // every lane has read the tile
+            fetch();
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+            Fold<V> own;
+#pragma unroll
+            for (int i = 0; i < V; ++i) own.a[i] = 1.0f, own.b[i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < L; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    own.a[i] *= z[k][i];
+                    own.b[i] = z[k][i] * own.b[i] + b[k][i];
+                }
+            float h[V];
+            exchange<V>(folds, it, own, w.warp, w.warps, w.lane, w.rank, w.cluster, wait, carry, h);
+            if (TMA) {
+                if (w.lane == 0) bulk_wait_read<0>();  // the last round's states have left the tile
+                __syncwarp();
+            }
+            const auto emit = [&](bool whole) {
+                Hy *q = out + step * t;
+#pragma unroll
+                for (int k = 0; k < L; ++k, q += step) {
+                    float v[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        h[i] = z[k][i] * h[i] + b[k][i];
+                        v[i] = whole || k < n ? h[i] : 0.0f;
+                    }
+                    if (TMA)
+                        mine.out.put(k, w.lane, v);
+                    else if (g.on && (whole || t + k < p.d.T))
+                        store<Hy, V>(q, v);
+                }
+            };
+            if (n == L)
+                emit(true);
+            else
+                emit(false);
+            if (TMA) {
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (w.lane == 0 && t < p.d.T) {
+                    tma_store_3d(&tm_h, &mine.out, g.c, g.b, t);
+                    bulk_commit();
                 }
             }
         }
-    }
-    if (at.on) {
-        const float zero[V] = {};
-        for (int t = at.len + at.rank * at.warps + at.warp; t < p.d.T; t += at.warps * p.cluster) {
-            store<G, V>(dg + 2 * step * t, zero);
-            store<G, V>(dg + 2 * step * t + hidden, zero);
-        }
-        if (p.d.dh0 && at.rank == 0 && at.warp == 0) {
+        if (g.on) {
+            const float zero[V] = {};
+            for (int t = rounds * round + w.chunk; t < p.d.T; t += w.span) store<Hy, V>(out + step * t, zero);
+            if (p.d.h_last && w.chunk == 0) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) p.d.dh0[at.chain + i] = carry[i];
+                for (int i = 0; i < V; ++i) p.d.h_last[g.chain + i] = carry[i];
+            }
         }
     }
-    if (p.cluster > 1) cluster_sync_all();
+    exchange_end(folds, p.cluster);
+}
+
+template <typename G, typename Hy, int V, int L, bool TMA>
+__global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
+    glr_backward_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_h,
+                        const __grid_constant__ CUtensorMap tm_dh, const __grid_constant__ CUtensorMap tm_dg,
+                        const __grid_constant__ ScanParams p) {
+    if (p.cluster > 1 && !launch_shape_ok(p.err, p.cluster, gridDim.x, 0x602u)) return;
+    using Tiles = BackwardTiles<G, Hy, V, L>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ FoldBuffers<V> folds;
+    __shared__ uint64_t full_all[kMaxWarps][kStages];
+    const WaitCtx wait{p.timeout_ns, p.err, &folds.abort};
+    const Warp w(p);
+    Tiles &mine = reinterpret_cast<Tiles *>(smem)[w.warp];
+    uint64_t *full = full_all[w.warp];
+    if (TMA && w.lane == 0) {
+        for (int i = 0; i < kStages; ++i) mbar_init(&full[i], 1);
+        fence_mbar_init();
+    }
+    exchange_init(folds, p.cluster);
+    const int hidden = p.d.hidden;
+    const int64_t step = static_cast<int64_t>(p.d.batch) * hidden;
+    const bool has_dh = p.d.dh_out != nullptr;
+    // Rounds and their chunks start at multiples of L from step 0 and are taken
+    // from the last to the first: the folds' order is the reverse of time.
+    const int round = w.span * L, first = (w.span - 1 - w.chunk) * L;
+
+    int64_t load_group = w.id;
+    int load_round = 0, load_stage = 0;  // rounds counted from the last
+    const auto fetch = [&]() {
+        for (; load_group < p.groups; load_group += w.ids, load_round = 0) {
+            const Group<V> g(p, load_group, w.lane);
+            const int rounds = (g.len + round - 1) / round;
+            if (load_round >= rounds) continue;
+            const int t = (rounds - 1 - load_round) * round + first;
+            typename Tiles::In &to = mine.in[load_stage];
+            if (t < g.len) {
+                if (TMA) {
+                    if (w.lane == 0) {
+                        uint64_t *bar = &full[load_stage];
+                        mbar_arrive_expect_tx(bar, sizeof(to) - (has_dh ? 0 : sizeof(to.dh)));
+                        tma_load_3d(&tm_g, bar, &to.z, g.c, 2 * g.b, t);
+                        tma_load_3d(&tm_g, bar, &to.n, g.c, 2 * g.b + 1, t);
+                        tma_load_3d(&tm_h, bar, &to.before, g.c, g.b, t - 1);  // row -1 reads zeros
+                        if (has_dh) tma_load_3d(&tm_dh, bar, &to.dh, g.c, g.b, t);
+                    }
+                } else {
+                    const G *q = static_cast<const G *>(p.d.g) + g.chain + static_cast<int64_t>(g.b) * hidden +
+                                 2 * step * t;
+                    const Hy *qh = static_cast<const Hy *>(p.d.h_in) + g.chain + step * (t - 1);
+                    const Hy *qd = static_cast<const Hy *>(p.d.dh_out) + g.chain + step * t;
+                    for (int k = 0; k < min(g.len - t, L); ++k, q += 2 * step, qh += step, qd += step) {
+                        lane_copy<sizeof(G) * V>(&to.z.v[k][w.lane * V], q);
+                        lane_copy<sizeof(G) * V>(&to.n.v[k][w.lane * V], q + hidden);
+                        if (t + k > 0) lane_copy<sizeof(Hy) * V>(&to.before.v[k][w.lane * V], qh);
+                        if (has_dh) lane_copy<sizeof(Hy) * V>(&to.dh.v[k][w.lane * V], qd);
+                    }
+                }
+            }
+            ++load_round;
+            break;
+        }
+        if (!TMA) lane_copies_commit();
+        load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
+    };
+    for (int i = 0; i < kStages; ++i) fetch();
+
+    float next[V];
+    if (w.id < p.groups) edge<V>(p.d.dh_last, Group<V>(p, w.id, w.lane).chain, next);
+    int it = 0, stage = 0;
+    uint32_t phases = 0;
+    for (int64_t gi = w.id; gi < p.groups; gi += w.ids) {
+        const Group<V> g(p, gi, w.lane);
+        const int rounds = (g.len + round - 1) / round;
+        G *dg = static_cast<G *>(p.d.dg) + g.chain + static_cast<int64_t>(g.b) * hidden;
+        float carry[V], h0[V];
+        edge<V>(p.d.h0, g.chain, h0);
+#pragma unroll
+        for (int i = 0; i < V; ++i) carry[i] = next[i];
+        if (gi + w.ids < p.groups) edge<V>(p.d.dh_last, Group<V>(p, gi + w.ids, w.lane).chain, next);
+        for (int r = rounds - 1; r >= 0; --r, ++it) {
+            const int t = r * round + first;
+            const int n = min(g.len - t, L);
+            if (TMA) {
+                if (n > 0) {
+                    bounded_wait(&full[stage], (phases >> stage) & 1u, wait, 0x605u);
+                    phases ^= 1u << stage;
+                }
+            } else {
+                lane_copies_wait<kStages - 1>();
+            }
+            // z, 1 - z, (h_{t-1} - n) z (1 - z) and dh of each step.
+            float z[L][V], take[L][V], q[L][V], d[L][V];
+            const typename Tiles::In &in = mine.in[stage];
+#pragma unroll
+            for (int k = 0; k < L; ++k) {
+                float gz[V], gn[V], before[V];
+                in.z.get(k, w.lane, gz);
+                in.n.get(k, w.lane, gn);
+                in.before.get(k, w.lane, before);
+                in.dh.get(k, w.lane, d[k]);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const Gate s = scan_gate(gz[i]);
+                    if (k == 0 && t == 0) before[i] = h0[i];
+                    z[k][i] = s.keep;
+                    take[k][i] = s.take;
+                    q[k][i] = (before[i] - gn[i]) * (s.keep * s.take);
+                }
+            }
+            if (n < L || !has_dh) {
+#pragma unroll
+                for (int k = 0; k < L; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        if (k >= n) z[k][i] = 1.0f;
+                        if (k >= n || !has_dh) d[k][i] = 0.0f;
+                    }
+            }
+            __syncwarp();
+            fetch();
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+            Fold<V> own;
+#pragma unroll
+            for (int i = 0; i < V; ++i) own.a[i] = 1.0f, own.b[i] = 0.0f;
+#pragma unroll
+            for (int k = L - 1; k >= 0; --k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    own.a[i] *= z[k][i];
+                    own.b[i] = z[k][i] * (own.b[i] + d[k][i]);
+                }
+            float e[V];
+            exchange<V>(folds, it, own, w.warp, w.warps, w.lane, w.rank, w.cluster, wait, carry, e);
+            if (TMA) {
+                if (w.lane == 0) bulk_wait_read<0>();
+                __syncwarp();
+            }
+            const auto emit = [&](bool whole) {
+                G *o = dg + 2 * step * (t + L - 1);
+#pragma unroll
+                for (int k = L - 1; k >= 0; --k, o -= 2 * step) {
+                    float dz[V], dn[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float all = d[k][i] + e[i];
+                        const bool live = whole || k < n;
+                        dz[i] = live ? all * q[k][i] : 0.0f;
+                        dn[i] = live ? all * take[k][i] : 0.0f;
+                        e[i] = z[k][i] * all;
+                    }
+                    if (TMA) {
+                        mine.dz.put(k, w.lane, dz);
+                        mine.dn.put(k, w.lane, dn);
+                    } else if (g.on && (whole || t + k < p.d.T)) {
+                        store<G, V>(o, dz);
+                        store<G, V>(o + hidden, dn);
+                    }
+                }
+            };
+            if (n == L)
+                emit(true);
+            else
+                emit(false);
+            if (TMA) {
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (w.lane == 0 && t < p.d.T) {
+                    tma_store_3d(&tm_dg, &mine.dz, g.c, 2 * g.b, t);
+                    tma_store_3d(&tm_dg, &mine.dn, g.c, 2 * g.b + 1, t);
+                    bulk_commit();
+                }
+            }
+        }
+        if (g.on) {
+            const float zero[V] = {};
+            for (int t = rounds * round + w.chunk; t < p.d.T; t += w.span) {
+                store<G, V>(dg + 2 * step * t, zero);
+                store<G, V>(dg + 2 * step * t + hidden, zero);
+            }
+            if (p.d.dh0 && w.chunk == 0) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) p.d.dh0[g.chain + i] = carry[i];
+            }
+        }
+    }
+    exchange_end(folds, p.cluster);
 }
 
 // One token a sequence: one thread per V channels.
@@ -452,60 +718,149 @@ bool vector_ok(int hidden, int V, int type, const void *p) {
     return hidden % V == 0 && reinterpret_cast<uintptr_t>(p) % ((type == ISAM_F32 ? 4 : 2) * V) == 0;
 }
 
-int scan_launch(void (*fn)(const ScanParams), const GlrDesc &d, int V, int L, const DeviceState &ds, cudaStream_t s,
-                const char *what) {
-    ScanParams p{};
+// Rows of `hidden` elements on 16-byte boundaries: what TMA addresses.
+bool rows16(int hidden, int type, const void *p) {
+    const int size = type == ISAM_F32 ? 4 : 2;
+    return static_cast<int64_t>(hidden) * size % 16 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+}
+
+int rows_tmap(CUtensorMap *out, const void *p, int type, int hidden, int64_t rows, int T, int width, int L) {
+    const uint64_t size = type == ISAM_F32 ? 4 : 2;
+    const uint64_t dims[3] = {static_cast<uint64_t>(hidden), static_cast<uint64_t>(rows), static_cast<uint64_t>(T)};
+    const uint64_t strides[2] = {hidden * size, hidden * size * rows};
+    const uint32_t box[3] = {static_cast<uint32_t>(width), 1, static_cast<uint32_t>(L)};
+    return make_tmap_3d_plain(out, p, type == ISAM_F32, dims, strides, box);
+}
+
+// Clusters of `c` CTAs of this kernel resident at once, asked once per device,
+// kernel and shape.
+int resident_clusters(const void *fn, int c, int threads, int smem, const DeviceState &ds) {
+    struct Known {
+        int device;
+        const void *fn;
+        int c, threads, n;
+    };
+    static std::mutex mu;
+    static Known known[512];
+    static int count = 0;
+    std::lock_guard<std::mutex> lk(mu);
+    for (int i = 0; i < count; ++i)
+        if (known[i].device == ds.device && known[i].fn == fn && known[i].c == c && known[i].threads == threads)
+            return known[i].n;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    cfg.gridDim = dim3(static_cast<unsigned>(c * ds.num_sms));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = c;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, fn, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+    }
+    if (count < 512) known[count++] = Known{ds.device, fn, c, threads, n};
+    return n;
+}
+
+// Fills in the launch shape: `smem` bytes a warp.  The cluster size is the one
+// with the fewest rounds in all (rounds of a sequence times turns of a
+// cluster): several CTAs share a sequence's time where the channels alone would
+// leave SMs idle.
+int scan_shape(const void *fn, const GlrDesc &d, int V, int L, int smem, const DeviceState &ds, ScanParams &p,
+               cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr) {
     p.d = d;
     p.err = ds.err_word;
+    p.timeout_ns = wait_timeout_ns();
     p.tiles = (d.hidden + 32 * V - 1) / (32 * V);
-    const int64_t groups = static_cast<int64_t>(p.tiles) * d.batch;
+    p.groups = static_cast<int64_t>(p.tiles) * d.batch;
     const int warps = std::min(kMaxWarps, (d.T + L - 1) / L);
-    // The cluster size with the fewest rounds times waves of CTAs: enough CTAs
-    // for the GPU where the channels alone are too few, no more than one wave
-    // of them where time is split.
-    const int64_t slots = static_cast<int64_t>(ds.num_sms) * kCtasPerSm;
-    int64_t best = 0;
+    const int bytes = smem * warps;
+    const int rc = ensure_smem_optin(fn, smem * kMaxWarps, ds.device, "cudaFuncSetAttribute(gated linear recurrence)");
+    if (rc) return rc;
+    int64_t best = 0, grid = 0;
     for (int c = 1; c <= kMaxCluster; ++c) {
-        const int64_t rounds = (d.T + static_cast<int64_t>(c) * warps * L - 1) / (static_cast<int64_t>(c) * warps * L);
-        const int64_t cost = rounds * ((groups * c + slots - 1) / slots);
-        if (c == 1 || cost < best) {
+        const int64_t span = static_cast<int64_t>(c) * warps * L;
+        if (c > 1 && span - warps * L >= d.T) break;  // CTAs without steps
+        const int64_t resident = resident_clusters(fn, c, 32 * warps, bytes, ds);
+        if (resident < 1) continue;
+        const int64_t ids = std::min(resident, p.groups);
+        const int64_t cost = (d.T + span - 1) / span * ((p.groups + ids - 1) / ids);
+        if (grid == 0 || cost < best) {
             best = cost;
+            grid = ids * c;
             p.cluster = static_cast<uint32_t>(c);
         }
     }
-    if (groups * p.cluster > 0x7fffffffLL)
-        return set_error(ISAM_ERR_UNSUPPORTED, "batch * hidden is too large for one launch");
+    if (grid == 0) return set_error(ISAM_ERR_UNSUPPORTED, "the gated linear recurrence's kernel fits no SM");
+    cfg.gridDim = dim3(static_cast<unsigned>(grid));
+    cfg.blockDim = dim3(32 * warps);
+    cfg.dynamicSmemBytes = bytes;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = p.cluster;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.cluster > 1 ? 1 : 0;
+    return ISAM_OK;
+}
+
+template <typename G, typename Hy, int V, int L, bool TMA>
+int forward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
+    const auto fn = glr_forward_kernel<G, Hy, V, L, TMA>;
+    ScanParams p{};
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
-    cfg.gridDim = dim3(static_cast<unsigned>(groups * p.cluster));
-    cfg.blockDim = dim3(32 * warps);
-    cfg.stream = s;
-    if (p.cluster > 1) {
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = p.cluster;
-        attr[0].val.clusterDim.y = 1;
-        attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
+    int rc = scan_shape(reinterpret_cast<const void *>(fn), d, V, L, sizeof(ForwardTiles<G, Hy, V, L>), ds, p, cfg, attr);
+    if (rc) return rc;
+    CUtensorMap tg{}, th{};
+    if (TMA) {
+        if ((rc = rows_tmap(&tg, d.g, d.g_type, d.hidden, 2LL * d.batch, d.T, 32 * V, L))) return rc;
+        if ((rc = rows_tmap(&th, d.h_out, d.h_type, d.hidden, d.batch, d.T, 32 * V, L))) return rc;
     }
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, static_cast<const ScanParams>(p));
-    return e == cudaSuccess ? ISAM_OK : cuda_error(e, what);
+    cfg.stream = s;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, tg, th, p);
+    return e == cudaSuccess ? ISAM_OK : cuda_error(e, "launch glr_forward_kernel");
+}
+
+template <typename G, typename Hy, int V, int L, bool TMA>
+int backward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
+    const auto fn = glr_backward_kernel<G, Hy, V, L, TMA>;
+    ScanParams p{};
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    int rc = scan_shape(reinterpret_cast<const void *>(fn), d, V, L, sizeof(BackwardTiles<G, Hy, V, L>), ds, p, cfg, attr);
+    if (rc) return rc;
+    CUtensorMap tg{}, th{}, tdh{}, tdg{};
+    if (TMA) {
+        if ((rc = rows_tmap(&tg, d.g, d.g_type, d.hidden, 2LL * d.batch, d.T, 32 * V, L))) return rc;
+        if ((rc = rows_tmap(&th, d.h_in, d.h_type, d.hidden, d.batch, d.T, 32 * V, L))) return rc;
+        if (d.dh_out && (rc = rows_tmap(&tdh, d.dh_out, d.h_type, d.hidden, d.batch, d.T, 32 * V, L))) return rc;
+        if ((rc = rows_tmap(&tdg, d.dg, d.g_type, d.hidden, 2LL * d.batch, d.T, 32 * V, L))) return rc;
+    }
+    cfg.stream = s;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, tg, th, tdh, tdg, p);
+    return e == cudaSuccess ? ISAM_OK : cuda_error(e, "launch glr_backward_kernel");
 }
 
 }  // namespace
 
-// V and L keep a row of a warp at 128 bytes of gates and a thread's z, b and
-// prefetched gates within 128 registers.
+// V keeps a row of a warp at 128 bytes of gates, L its z and b (backward: four
+// values a step) within the registers of two CTAs an SM.
 int glr_forward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
     return by_types(d.g_type, d.h_type, [&](auto gt, auto ht) {
         using G = decltype(gt);
         using Hy = decltype(ht);
-        const char *what = "launch glr_forward_kernel";
-        if constexpr (sizeof(G) == 2) {
-            if (vector_ok(d.hidden, 2, d.g_type, d.g) && vector_ok(d.hidden, 2, d.h_type, d.h_out))
-                return scan_launch(glr_forward_kernel<G, Hy, 2, 16>, d, 2, 16, ds, s, what);
-        }
-        return scan_launch(glr_forward_kernel<G, Hy, 1, 16>, d, 1, 16, ds, s, what);
+        constexpr int V = sizeof(G) == 2 ? 2 : 1;
+        if (rows16(d.hidden, d.g_type, d.g) && rows16(d.hidden, d.h_type, d.h_out))
+            return forward_launch<G, Hy, V, 16, true>(d, ds, s);
+        if (V == 2 && vector_ok(d.hidden, V, d.g_type, d.g) && vector_ok(d.hidden, V, d.h_type, d.h_out))
+            return forward_launch<G, Hy, V, 16, false>(d, ds, s);
+        return forward_launch<G, Hy, 1, 16, false>(d, ds, s);
     });
 }
 
@@ -513,13 +868,14 @@ int glr_backward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
     return by_types(d.g_type, d.h_type, [&](auto gt, auto ht) {
         using G = decltype(gt);
         using Hy = decltype(ht);
-        const char *what = "launch glr_backward_kernel";
-        if constexpr (sizeof(G) == 2) {
-            if (vector_ok(d.hidden, 2, d.g_type, d.g) && vector_ok(d.hidden, 2, d.g_type, d.dg) &&
-                vector_ok(d.hidden, 2, d.h_type, d.h_in) && vector_ok(d.hidden, 2, d.h_type, d.dh_out))
-                return scan_launch(glr_backward_kernel<G, Hy, 2, 8>, d, 2, 8, ds, s, what);
-        }
-        return scan_launch(glr_backward_kernel<G, Hy, 1, 8>, d, 1, 8, ds, s, what);
+        constexpr int V = sizeof(G) == 2 ? 2 : 1;
+        if (rows16(d.hidden, d.g_type, d.g) && rows16(d.hidden, d.h_type, d.h_in) &&
+            rows16(d.hidden, d.h_type, d.dh_out) && rows16(d.hidden, d.g_type, d.dg))
+            return backward_launch<G, Hy, V, 8, true>(d, ds, s);
+        if (V == 2 && vector_ok(d.hidden, V, d.g_type, d.g) && vector_ok(d.hidden, V, d.g_type, d.dg) &&
+            vector_ok(d.hidden, V, d.h_type, d.h_in) && vector_ok(d.hidden, V, d.h_type, d.dh_out))
+            return backward_launch<G, Hy, V, 8, false>(d, ds, s);
+        return backward_launch<G, Hy, 1, 8, false>(d, ds, s);
     });
 }
 

@@ -60,6 +60,10 @@ int make_tmap_2d_u8(CUtensorMap *out, const void *base, uint64_t inner, uint64_t
 int make_tmap_3d_bf16(CUtensorMap *out, const void *base, const uint64_t dims[3],
                       const uint64_t strides_bytes[2], const uint32_t box[3]);
 
+// 3-D map of bf16 or fp32 elements without swizzle (boxes read row by row).
+int make_tmap_3d_plain(CUtensorMap *out, const void *base, bool f32, const uint64_t dims[3],
+                       const uint64_t strides_bytes[2], const uint32_t box[3]);
+
 // GEMM C = alpha op(A) op(B) + beta C (+ bias[n] per column when bias != null).
 struct GemmDesc {
     int M, N, K;
