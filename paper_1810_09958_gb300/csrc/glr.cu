@@ -44,14 +44,38 @@ namespace isam {
 
 namespace {
 
-constexpr int kMaxWarps = 8;
 constexpr int kMaxCluster = 8;
-constexpr int kCtasPerSm = 2;  // launch bounds: at most 128 registers a thread
-constexpr int kStages = 2;     // tiles of each input in a warp's ring
+constexpr int kStages = 2;  // tiles of each input in a warp's ring
+
+// Warps of a CTA, CTAs of an SM (launch bounds) and steps of a warp per round
+// (L).  A round costs a warp about 350 instructions beside its steps', so the
+// steps are as many as registers hold z and b (backward: four values) of.
+// Measured, us (65536 x 1 x 2560 bf16 forward, 4096 x 8 x 1024 bf16 backward):
+// 8 warps of 16 / 8 steps 207, 72; 4 warps of 32 / 16 steps 168, 62.  With
+// one fp32 channel a lane (128 x 32 x 1024 forward, 20001 x 2 x 1760 backward):
+// 8 warps of 16 / 8 steps 10.5, 189; 4 warps, 4 CTAs an SM 9.5, 224; 8 warps of
+// 32 / 16 steps 10.4, 201.
+template <int V, bool BACK>
+struct Shape;
+template <>
+struct Shape<2, false> {
+    static constexpr int kWarps = 4, kCtas = 2, kSteps = 32;
+};
+template <>
+struct Shape<2, true> {
+    static constexpr int kWarps = 4, kCtas = 2, kSteps = 16;
+};
+template <>
+struct Shape<1, false> {
+    static constexpr int kWarps = 4, kCtas = 4, kSteps = 16;
+};
+template <>
+struct Shape<1, true> {
+    static constexpr int kWarps = 8, kCtas = 2, kSteps = 8;
+};
 constexpr int kStepThreads = 128;
 
-// V neighbouring elements, moved as one word; data used once, so loads and
-// stores are marked streaming.
+// V neighbouring elements, moved as one word.
 template <int BYTES>
 struct Word;
 template <>
@@ -79,46 +103,147 @@ union Pack {
     __device__ Pack() {}
 };
 
-template <typename T, int V>
-__device__ __forceinline__ void load(Pack<T, V> &p, const T *at) {
-    p.w = __ldcs(reinterpret_cast<const typename Pack<T, V>::W *>(at));
+// The V channels of a lane in fp32.  Two of them share one instruction for
+// products and sums (f32x2), which halves the issue slots of the scan.
+template <int V>
+struct Lane;
+template <>
+struct Lane<1> {
+    float x;
+    __device__ __forceinline__ Lane() {}
+    __device__ __forceinline__ explicit Lane(float v) : x(v) {}
+    __device__ __forceinline__ Lane(const float (&v)[1]) : x(v[0]) {}
+    __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = x; }
+};
+template <>
+struct Lane<2> {
+    unsigned long long x;
+    __device__ __forceinline__ Lane() {}
+    __device__ __forceinline__ Lane(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(lo), "f"(hi)); }
+    __device__ __forceinline__ explicit Lane(float v) : Lane(v, v) {}
+    __device__ __forceinline__ Lane(const float (&v)[2]) : Lane(v[0], v[1]) {}
+    __device__ __forceinline__ void get(float (&v)[2]) const {
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(v[0]), "=f"(v[1]) : "l"(x));
+    }
+};
+__device__ __forceinline__ Lane<1> mul(Lane<1> a, Lane<1> b) { return Lane<1>(a.x * b.x); }
+__device__ __forceinline__ Lane<1> add(Lane<1> a, Lane<1> b) { return Lane<1>(a.x + b.x); }
+__device__ __forceinline__ Lane<1> fma(Lane<1> a, Lane<1> b, Lane<1> c) { return Lane<1>(fmaf(a.x, b.x, c.x)); }
+__device__ __forceinline__ Lane<2> mul(Lane<2> a, Lane<2> b) {
+    Lane<2> d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.x) : "l"(a.x), "l"(b.x));
+    return d;
+}
+__device__ __forceinline__ Lane<2> add(Lane<2> a, Lane<2> b) {
+    Lane<2> d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.x) : "l"(a.x), "l"(b.x));
+    return d;
+}
+__device__ __forceinline__ Lane<2> fma(Lane<2> a, Lane<2> b, Lane<2> c) {
+    Lane<2> d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.x) : "l"(a.x), "l"(b.x), "l"(c.x));
+    return d;
 }
 
+// Elements to fp32 and back, a lane's word at a time.
 template <typename T, int V>
-__device__ __forceinline__ void store(T *at, const float (&x)[V]) {
-    Pack<T, V> p;
+__device__ __forceinline__ Lane<V> widen(const Pack<T, V> &p) {
+    if constexpr (sizeof(T) == 2 && V == 2) {
+        return Lane<2>(__uint_as_float(p.w << 16), __uint_as_float(p.w & 0xffff0000u));
+    } else {
+        float v[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) p.v[i] = from_f32<T>(x[i]);
+        for (int i = 0; i < V; ++i) v[i] = to_f32(p.v[i]);
+        return Lane<V>(v);
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void narrow(Pack<T, V> &p, const Lane<V> &x);
+template <typename T, int V>
+__device__ __forceinline__ void store(T *at, const Lane<V> &x) {
+    Pack<T, V> p;
+    narrow<T, V>(p, x);
     __stcs(reinterpret_cast<typename Pack<T, V>::W *>(at), p.w);
+}
+template <typename T, int V>
+__device__ __forceinline__ void narrow(Pack<T, V> &p, const Lane<V> &x) {
+    float v[V];
+    x.get(v);
+    if constexpr (sizeof(T) == 2 && V == 2) {
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p.w) : "f"(v[1]), "f"(v[0]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) p.v[i] = from_f32<T>(v[i]);
+    }
+}
+// max(x, -87), a NaN staying one.
+template <typename T, int V>
+__device__ __forceinline__ Lane<V> widen_from_minus_87(Pack<T, V> p) {
+    if constexpr (sizeof(T) == 2 && V == 2) {
+        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(p.w) : "r"(0xC2AEC2AEu));
+        return widen<T, V>(p);
+    } else {
+        float v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            v[i] = to_f32(p.v[i]);
+            asm("max.NaN.f32 %0, %0, 0fC2AE0000;" : "+f"(v[i]));
+        }
+        return Lane<V>(v);
+    }
 }
 
 // sigmoid(x) and 1 - sigmoid(x) without a branch on the sign: with
 // e = exp(-x) they are 1 / (1 + e) and e / (1 + e), each accurate to its own
-// size; e stops at 2^126 so that e / (1 + e) stays 1 (a NaN passes).
-__device__ __forceinline__ Gate scan_gate(float x) {
-    float t = x * -1.4426950408889634f, e;
-    asm("min.NaN.f32 %0, %0, 0f42FC0000;" : "+f"(t));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-    return Gate{r, e * r};
-}
+// size.  x >= -87, where the first is 2e-38, keeps e finite.
+template <int V>
+struct Gates {
+    Lane<V> keep, take;
+    __device__ __forceinline__ explicit Gates(const Lane<V> &x) {
+        float t[V];
+        mul(x, Lane<V>(-1.4426950408889634f)).get(t);
+#pragma unroll
+        for (int i = 0; i < V; ++i) asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t[i]));
+        const Lane<V> e(t);
+        add(e, Lane<V>(1.0f)).get(t);
+#pragma unroll
+        for (int i = 0; i < V; ++i) asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(t[i]));
+        keep = Lane<V>(t);
+        take = mul(e, keep);
+    }
+};
 
 // One affine map per channel of a lane.  A product of many gates may underflow;
 // it is kept at 2^-126 (no gate is zero), so that an infinite state stays
 // infinite as it does step by step, instead of 0 * inf.  A finite state h is
 // changed by at most 2^-126 h.
 template <int V>
-struct Fold {
-    float a[V], b[V];
+struct __align__(8 * V) Fold {
+    Lane<V> a, b;
+    __device__ __forceinline__ Fold() {}
+    __device__ __forceinline__ Fold(float av, float bv) : a(av), b(bv) {}
+    // This map after `first`.
+    __device__ __forceinline__ Fold after(const Fold &first) const {
+        Fold f;
+        f.a = positive(mul(a, first.a));
+        f.b = fma(a, first.b, b);
+        return f;
+    }
+    __device__ __forceinline__ Lane<V> of(const Lane<V> &h) const { return fma(a, h, b); }
+    static __device__ __forceinline__ Lane<V> positive(const Lane<V> &a) {
+        float v[V];
+        a.get(v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = fmaxf(v[i], 1.17549435e-38f);
+        return Lane<V>(v);
+    }
 };
-__device__ __forceinline__ float positive(float a) { return fmaxf(a, 1.17549435e-38f); }
 
 // Folds of one round: of the CTA's warps, and of the cluster's CTAs (written
 // by them, their bytes counted on `landed`).
-template <int V>
+template <int V, int WARPS>
 struct FoldBuffers {
-    Fold<V> warp[2][kMaxWarps][32];
+    Fold<V> warp[2][WARPS][32];
     Fold<V> cta[2][kMaxCluster][32];
     uint64_t landed[2];
     int abort;
@@ -128,8 +253,8 @@ struct FoldBuffers {
 // round r + 1 after all its warps are done with round r (their barrier in
 // exchange), and a fold of round r + 2 is sent by a warp that holds every
 // CTA's fold of round r + 1: nothing still reads, or waits for, round r.
-template <int V>
-__device__ __forceinline__ void exchange_init(FoldBuffers<V> &s, uint32_t cluster) {
+template <int V, int WARPS>
+__device__ __forceinline__ void exchange_init(FoldBuffers<V, WARPS> &s, uint32_t cluster) {
     if (threadIdx.x == 0) {
         mbar_init(&s.landed[0], 1);
         mbar_init(&s.landed[1], 1);
@@ -145,8 +270,8 @@ __device__ __forceinline__ void exchange_init(FoldBuffers<V> &s, uint32_t cluste
 // The end of a kernel: stores have left shared memory; after a wait that ran
 // out, copies into this CTA's shared memory get time to land; and no CTA leaves
 // while another may still send it folds.
-template <int V>
-__device__ __forceinline__ void exchange_end(FoldBuffers<V> &s, uint32_t cluster) {
+template <int V, int WARPS>
+__device__ __forceinline__ void exchange_end(FoldBuffers<V, WARPS> &s, uint32_t cluster) {
     if ((threadIdx.x & 31) == 0) bulk_wait_all<0>();
     if (*static_cast<volatile int *>(&s.abort)) {
         const unsigned long long t0 = globaltimer();
@@ -161,54 +286,37 @@ __device__ __forceinline__ void exchange_end(FoldBuffers<V> &s, uint32_t cluster
 // Asynchronous: unlike a release, it does not wait for this thread's stores of
 // states to reach L2.
 __device__ __forceinline__ void send(uint32_t to, const Fold<2> &f, uint32_t bar) {
-    st_async_f4(to, make_float4(f.a[0], f.a[1], f.b[0], f.b[1]), bar);
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(to),
+                 "l"(f.a.x), "l"(f.b.x), "r"(bar)
+                 : "memory");
 }
 __device__ __forceinline__ void send(uint32_t to, const Fold<1> &f, uint32_t bar) {
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to),
-                 "f"(f.a[0]), "f"(f.b[0]), "r"(bar)
+                 "f"(f.a.x), "f"(f.b.x), "r"(bar)
                  : "memory");
 }
 
-// What a warp needs from the others' folds: `in` becomes the state before its
-// first step of this round, `carry` the state after the round.
-template <int V>
-__device__ __forceinline__ void exchange(FoldBuffers<V> &s, int r, Fold<V> &own, int warp, int warps, int lane,
-                                         uint32_t rank, uint32_t cluster, const WaitCtx &wait, float (&carry)[V],
-                                         float (&in)[V]) {
+// What a warp needs from the others' folds: returns the state before its first
+// step of this round; `carry` becomes the state after the round.
+template <int V, int WARPS>
+__device__ __forceinline__ Lane<V> exchange(FoldBuffers<V, WARPS> &s, int r, Fold<V> &own, int warp, int warps, int lane,
+                                            uint32_t rank, uint32_t cluster, const WaitCtx &wait, Lane<V> &carry) {
     const int parity = r & 1;
-#pragma unroll
-    for (int i = 0; i < V; ++i) own.a[i] = positive(own.a[i]);
+    own.a = Fold<V>::positive(own.a);
     s.warp[parity][warp][lane] = own;
     __syncthreads();
+    Lane<V> in;
     if (cluster == 1) {
         for (int w = 0; w < warps; ++w) {
-            const Fold<V> f = s.warp[parity][w][lane];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if (w == warp) in[i] = carry[i];
-                carry[i] = f.a[i] * carry[i] + f.b[i];
-            }
+            if (w == warp) in = carry;
+            carry = s.warp[parity][w][lane].of(carry);
         }
-        return;
+        return in;
     }
-    Fold<V> before;
-#pragma unroll
-    for (int i = 0; i < V; ++i) before.a[i] = 1.0f, before.b[i] = 0.0f;
-    for (int w = 0; w < warp; ++w) {
-        const Fold<V> f = s.warp[parity][w][lane];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            before.b[i] = f.a[i] * before.b[i] + f.b[i];
-            before.a[i] = positive(before.a[i] * f.a[i]);
-        }
-    }
+    Fold<V> before(1.0f, 0.0f);
+    for (int w = 0; w < warp; ++w) before = s.warp[parity][w][lane].after(before);
     if (warp == warps - 1) {
-        Fold<V> all;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            all.a[i] = positive(own.a[i] * before.a[i]);
-            all.b[i] = own.a[i] * before.b[i] + own.b[i];
-        }
+        const Fold<V> all = own.after(before);
         if (lane == 0)
             mbar_arrive_expect_tx(&s.landed[parity], cluster * 32u * static_cast<uint32_t>(sizeof(Fold<V>)));
         const uint32_t at = smem_u32(&s.cta[parity][rank][lane]), bar = smem_u32(&s.landed[parity]);
@@ -217,19 +325,16 @@ __device__ __forceinline__ void exchange(FoldBuffers<V> &s, int r, Fold<V> &own,
     __syncwarp();
     bounded_wait<true>(&s.landed[parity], (r >> 1) & 1, wait, 0x603u);
     for (uint32_t q = 0; q < cluster; ++q) {
-        const Fold<V> f = s.cta[parity][q][lane];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (q == rank) in[i] = before.a[i] * carry[i] + before.b[i];
-            carry[i] = f.a[i] * carry[i] + f.b[i];
-        }
+        if (q == rank) in = before.of(carry);
+        carry = s.cta[parity][q][lane].of(carry);
     }
+    return in;
 }
 
 struct ScanParams {
     GlrDesc d;
-    int tiles;       // channel tiles of 32 V per sequence
-    int64_t groups;  // tiles * batch: the units a cluster takes one after another
+    uint32_t tiles;   // channel tiles of 32 V per sequence
+    uint32_t groups;  // tiles * batch: the units a cluster takes one after another
     uint32_t cluster;
     uint32_t *err;
     unsigned long long timeout_ns;
@@ -255,17 +360,14 @@ __device__ __forceinline__ void lane_copies_wait() {
 template <typename T, int V, int L>
 struct Tile {
     T v[L][32 * V];
-    // One word of a lane, as floats.
-    __device__ __forceinline__ void get(int k, int lane, float (&x)[V]) const {
+    __device__ __forceinline__ Pack<T, V> get(int k, int lane) const {
         Pack<T, V> p;
         p.w = *reinterpret_cast<const typename Pack<T, V>::W *>(&v[k][lane * V]);
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = to_f32(p.v[i]);
+        return p;
     }
-    __device__ __forceinline__ void put(int k, int lane, const float (&x)[V]) {
+    __device__ __forceinline__ void put(int k, int lane, const Lane<V> &x) {
         Pack<T, V> p;
-#pragma unroll
-        for (int i = 0; i < V; ++i) p.v[i] = from_f32<T>(x[i]);
+        narrow<T, V>(p, x);
         *reinterpret_cast<typename Pack<T, V>::W *>(&v[k][lane * V]) = p.w;
     }
 };
@@ -293,7 +395,7 @@ struct Warp {
     int lane, warp, warps;
     uint32_t rank, cluster;
     int chunk, span;  // this warp's L steps in a round of span warps, in time order
-    int64_t id, ids;  // this cluster, clusters of the grid
+    uint32_t id, ids;  // this cluster, clusters of the grid
     __device__ Warp(const ScanParams &p) {
         lane = threadIdx.x & 31;
         warp = threadIdx.x >> 5;
@@ -313,33 +415,45 @@ struct Group {
     int own;        // this lane's first channel, moved back into the row where the tile passes its end
     bool on;        // the lane's channels exist
     int64_t chain;  // b * hidden + own
-    __device__ __forceinline__ Group(const ScanParams &p, int64_t g, int lane) {
+    int rounds;     // of this sequence
+    __device__ __forceinline__ Group(const ScanParams &p, uint32_t g, int lane, int round) {
+        g = min(g, p.groups - 1);  // behind the last one: not used
         b = static_cast<int>(g / p.tiles);
-        c = static_cast<int>(g - static_cast<int64_t>(b) * p.tiles) * 32 * V;
+        c = static_cast<int>(g - static_cast<uint32_t>(b) * p.tiles) * 32 * V;
         on = c + lane * V < p.d.hidden;
         own = min(c + lane * V, p.d.hidden - V);
         len = p.d.T;
         if (p.d.lengths) len = min(max(p.d.lengths[b], 0), p.d.T);
+        rounds = static_cast<int>((static_cast<uint32_t>(len) + round - 1) / static_cast<uint32_t>(round));
         chain = static_cast<int64_t>(b) * p.d.hidden + own;
     }
 };
 
 // One value per channel of a lane from a [batch][hidden] array (or zero).
 template <int V>
-__device__ __forceinline__ void edge(const float *from, int64_t chain, float (&x)[V]) {
+__device__ __forceinline__ Lane<V> edge(const float *from, int64_t chain) {
+    float x[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = from ? from[chain + i] : 0.0f;
+    return Lane<V>(x);
+}
+template <int V>
+__device__ __forceinline__ void put_edge(float *to, int64_t chain, const Lane<V> &x) {
+    float v[V];
+    x.get(v);
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[chain + i] = v[i];
 }
 
 template <typename G, typename Hy, int V, int L, bool TMA>
-__global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
+__global__ void __launch_bounds__(32 * Shape<V, false>::kWarps, Shape<V, false>::kCtas)
     glr_forward_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_h,
                        const __grid_constant__ ScanParams p) {
     if (p.cluster > 1 && !launch_shape_ok(p.err, p.cluster, gridDim.x, 0x601u)) return;
     using Tiles = ForwardTiles<G, Hy, V, L>;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ FoldBuffers<V> folds;
-    __shared__ uint64_t full_all[kMaxWarps][kStages];
+    __shared__ FoldBuffers<V, Shape<V, false>::kWarps> folds;
+    __shared__ uint64_t full_all[Shape<V, false>::kWarps][kStages];
     const WaitCtx wait{p.timeout_ns, p.err, &folds.abort};
     const Warp w(p);
     Tiles &mine = reinterpret_cast<Tiles *>(smem)[w.warp];
@@ -354,12 +468,17 @@ __global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
     const int round = w.span * L, first = w.chunk * L;
 
     // Loads run kStages rounds ahead of their use, across groups.
-    int64_t load_group = w.id;
+    uint32_t load_group = w.id;
+    Group<V> ahead(p, load_group, w.lane, round);
     int load_round = 0, load_stage = 0;
     const auto fetch = [&]() {
-        for (; load_group < p.groups; load_group += w.ids, load_round = 0) {
-            const Group<V> g(p, load_group, w.lane);
-            if (load_round * round >= g.len) continue;
+        while (load_group < p.groups && load_round >= ahead.rounds) {
+            load_group += w.ids;
+            load_round = 0;
+            ahead = Group<V>(p, load_group, w.lane, round);
+        }
+        if (load_group < p.groups) {
+            const Group<V> &g = ahead;
             const int t = load_round * round + first;
             typename Tiles::In &to = mine.in[load_stage];
             if (t < g.len) {
@@ -379,25 +498,20 @@ __global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
                 }
             }
             ++load_round;
-            break;
         }
         if (!TMA) lane_copies_commit();
         load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
     };
+    Lane<V> next = edge<V>(p.d.h0, ahead.chain);
     for (int i = 0; i < kStages; ++i) fetch();
-
-    float next[V];
-    if (w.id < p.groups) edge<V>(p.d.h0, Group<V>(p, w.id, w.lane).chain, next);
     int it = 0, stage = 0;
     uint32_t phases = 0;
-    for (int64_t gi = w.id; gi < p.groups; gi += w.ids) {
-        const Group<V> g(p, gi, w.lane);
-        const int rounds = (g.len + round - 1) / round;
+    for (uint32_t gi = w.id; gi < p.groups; gi += w.ids) {
+        const Group<V> g(p, gi, w.lane, round);
+        const int rounds = g.rounds;
         Hy *out = static_cast<Hy *>(p.d.h_out) + g.chain;
-        float carry[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) carry[i] = next[i];
-        if (gi + w.ids < p.groups) edge<V>(p.d.h0, Group<V>(p, gi + w.ids, w.lane).chain, next);
+        Lane<V> carry = next;
+        if (gi + w.ids < p.groups) next = edge<V>(p.d.h0, Group<V>(p, gi + w.ids, w.lane, round).chain);
         for (int r = 0; r < rounds; ++r, ++it) {
             const int t = r * round + first;
             const int n = min(g.len - t, L);  // steps of this warp, below 1 past the end
@@ -409,42 +523,29 @@ __global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
             } else {
                 lane_copies_wait<kStages - 1>();
             }
-            float z[L][V], b[L][V];
+            Lane<V> z[L], b[L];
             const typename Tiles::In &in = mine.in[stage];
 #pragma unroll
             for (int k = 0; k < L; ++k) {
-                float gz[V], gn[V];
-                in.z.get(k, w.lane, gz);
-                in.n.get(k, w.lane, gn);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const Gate s = scan_gate(gz[i]);
-                    z[k][i] = s.keep;
-                    b[k][i] = s.take * gn[i];
-                }
+                const Gates<V> s(widen_from_minus_87<G, V>(in.z.get(k, w.lane)));
+                z[k] = s.keep;
+                b[k] = mul(s.take, widen<G, V>(in.n.get(k, w.lane)));
             }
             if (n < L) {
 #pragma unroll
                 for (int k = 0; k < L; ++k)
-#pragma unroll
-                    for (int i = 0; i < V; ++i)
-                        if (k >= n) z[k][i] = 1.0f, b[k][i] = 0.0f;
+                    if (k >= n) z[k] = Lane<V>(1.0f), b[k] = Lane<V>(0.0f);
             }
             __syncwarp();  // every lane has read the tile
             fetch();
             stage = stage + 1 == kStages ? 0 : stage + 1;
-            Fold<V> own;
+            Fold<V> own(1.0f, 0.0f);
 #pragma unroll
-            for (int i = 0; i < V; ++i) own.a[i] = 1.0f, own.b[i] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < L; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    own.a[i] *= z[k][i];
-                    own.b[i] = z[k][i] * own.b[i] + b[k][i];
-                }
-            float h[V];
-            exchange<V>(folds, it, own, w.warp, w.warps, w.lane, w.rank, w.cluster, wait, carry, h);
+            for (int k = 0; k < L; ++k) {
+                own.a = mul(own.a, z[k]);
+                own.b = fma(z[k], own.b, b[k]);
+            }
+            Lane<V> h = exchange(folds, it, own, w.warp, w.warps, w.lane, w.rank, w.cluster, wait, carry);
             if (TMA) {
                 if (w.lane == 0) bulk_wait_read<0>();  // the last round's states have left the tile
                 __syncwarp();
@@ -453,12 +554,8 @@ __global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
                 Hy *q = out + step * t;
 #pragma unroll
                 for (int k = 0; k < L; ++k, q += step) {
-                    float v[V];
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        h[i] = z[k][i] * h[i] + b[k][i];
-                        v[i] = whole || k < n ? h[i] : 0.0f;
-                    }
+                    h = fma(z[k], h, b[k]);
+                    const Lane<V> v = whole || k < n ? h : Lane<V>(0.0f);
                     if (TMA)
                         mine.out.put(k, w.lane, v);
                     else if (g.on && (whole || t + k < p.d.T))
@@ -479,27 +576,24 @@ __global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
             }
         }
         if (g.on) {
-            const float zero[V] = {};
+            const Lane<V> zero(0.0f);
             for (int t = rounds * round + w.chunk; t < p.d.T; t += w.span) store<Hy, V>(out + step * t, zero);
-            if (p.d.h_last && w.chunk == 0) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) p.d.h_last[g.chain + i] = carry[i];
-            }
+            if (p.d.h_last && w.chunk == 0) put_edge<V>(p.d.h_last, g.chain, carry);
         }
     }
     exchange_end(folds, p.cluster);
 }
 
 template <typename G, typename Hy, int V, int L, bool TMA>
-__global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
+__global__ void __launch_bounds__(32 * Shape<V, true>::kWarps, Shape<V, true>::kCtas)
     glr_backward_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_h,
                         const __grid_constant__ CUtensorMap tm_dh, const __grid_constant__ CUtensorMap tm_dg,
                         const __grid_constant__ ScanParams p) {
     if (p.cluster > 1 && !launch_shape_ok(p.err, p.cluster, gridDim.x, 0x602u)) return;
     using Tiles = BackwardTiles<G, Hy, V, L>;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ FoldBuffers<V> folds;
-    __shared__ uint64_t full_all[kMaxWarps][kStages];
+    __shared__ FoldBuffers<V, Shape<V, true>::kWarps> folds;
+    __shared__ uint64_t full_all[Shape<V, true>::kWarps][kStages];
     const WaitCtx wait{p.timeout_ns, p.err, &folds.abort};
     const Warp w(p);
     Tiles &mine = reinterpret_cast<Tiles *>(smem)[w.warp];
@@ -516,14 +610,18 @@ __global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
     // from the last to the first: the folds' order is the reverse of time.
     const int round = w.span * L, first = (w.span - 1 - w.chunk) * L;
 
-    int64_t load_group = w.id;
+    uint32_t load_group = w.id;
+    Group<V> ahead(p, load_group, w.lane, round);
     int load_round = 0, load_stage = 0;  // rounds counted from the last
     const auto fetch = [&]() {
-        for (; load_group < p.groups; load_group += w.ids, load_round = 0) {
-            const Group<V> g(p, load_group, w.lane);
-            const int rounds = (g.len + round - 1) / round;
-            if (load_round >= rounds) continue;
-            const int t = (rounds - 1 - load_round) * round + first;
+        while (load_group < p.groups && load_round >= ahead.rounds) {
+            load_group += w.ids;
+            load_round = 0;
+            ahead = Group<V>(p, load_group, w.lane, round);
+        }
+        if (load_group < p.groups) {
+            const Group<V> &g = ahead;
+            const int t = (g.rounds - 1 - load_round) * round + first;
             typename Tiles::In &to = mine.in[load_stage];
             if (t < g.len) {
                 if (TMA) {
@@ -549,26 +647,21 @@ __global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
                 }
             }
             ++load_round;
-            break;
         }
         if (!TMA) lane_copies_commit();
         load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
     };
+    Lane<V> next = edge<V>(p.d.dh_last, ahead.chain);
     for (int i = 0; i < kStages; ++i) fetch();
-
-    float next[V];
-    if (w.id < p.groups) edge<V>(p.d.dh_last, Group<V>(p, w.id, w.lane).chain, next);
     int it = 0, stage = 0;
     uint32_t phases = 0;
-    for (int64_t gi = w.id; gi < p.groups; gi += w.ids) {
-        const Group<V> g(p, gi, w.lane);
-        const int rounds = (g.len + round - 1) / round;
+    for (uint32_t gi = w.id; gi < p.groups; gi += w.ids) {
+        const Group<V> g(p, gi, w.lane, round);
+        const int rounds = g.rounds;
         G *dg = static_cast<G *>(p.d.dg) + g.chain + static_cast<int64_t>(g.b) * hidden;
-        float carry[V], h0[V];
-        edge<V>(p.d.h0, g.chain, h0);
-#pragma unroll
-        for (int i = 0; i < V; ++i) carry[i] = next[i];
-        if (gi + w.ids < p.groups) edge<V>(p.d.dh_last, Group<V>(p, gi + w.ids, w.lane).chain, next);
+        const Lane<V> h0 = edge<V>(p.d.h0, g.chain);
+        Lane<V> carry = next;
+        if (gi + w.ids < p.groups) next = edge<V>(p.d.dh_last, Group<V>(p, gi + w.ids, w.lane, round).chain);
         for (int r = rounds - 1; r >= 0; --r, ++it) {
             const int t = r * round + first;
             const int n = min(g.len - t, L);
@@ -581,48 +674,35 @@ __global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
                 lane_copies_wait<kStages - 1>();
             }
             // z, 1 - z, (h_{t-1} - n) z (1 - z) and dh of each step.
-            float z[L][V], take[L][V], q[L][V], d[L][V];
+            Lane<V> z[L], take[L], q[L], d[L];
             const typename Tiles::In &in = mine.in[stage];
 #pragma unroll
             for (int k = 0; k < L; ++k) {
-                float gz[V], gn[V], before[V];
-                in.z.get(k, w.lane, gz);
-                in.n.get(k, w.lane, gn);
-                in.before.get(k, w.lane, before);
-                in.dh.get(k, w.lane, d[k]);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const Gate s = scan_gate(gz[i]);
-                    if (k == 0 && t == 0) before[i] = h0[i];
-                    z[k][i] = s.keep;
-                    take[k][i] = s.take;
-                    q[k][i] = (before[i] - gn[i]) * (s.keep * s.take);
-                }
+                const Gates<V> s(widen_from_minus_87<G, V>(in.z.get(k, w.lane)));
+                Lane<V> before = widen<Hy, V>(in.before.get(k, w.lane));
+                if (k == 0 && t == 0) before = h0;
+                z[k] = s.keep;
+                take[k] = s.take;
+                q[k] = mul(fma(widen<G, V>(in.n.get(k, w.lane)), Lane<V>(-1.0f), before), mul(s.keep, s.take));
+                d[k] = widen<Hy, V>(in.dh.get(k, w.lane));
             }
             if (n < L || !has_dh) {
 #pragma unroll
-                for (int k = 0; k < L; ++k)
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        if (k >= n) z[k][i] = 1.0f;
-                        if (k >= n || !has_dh) d[k][i] = 0.0f;
-                    }
+                for (int k = 0; k < L; ++k) {
+                    if (k >= n) z[k] = Lane<V>(1.0f);
+                    if (k >= n || !has_dh) d[k] = Lane<V>(0.0f);
+                }
             }
             __syncwarp();
             fetch();
             stage = stage + 1 == kStages ? 0 : stage + 1;
-            Fold<V> own;
+            Fold<V> own(1.0f, 0.0f);
 #pragma unroll
-            for (int i = 0; i < V; ++i) own.a[i] = 1.0f, own.b[i] = 0.0f;
-#pragma unroll
-            for (int k = L - 1; k >= 0; --k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    own.a[i] *= z[k][i];
-                    own.b[i] = z[k][i] * (own.b[i] + d[k][i]);
-                }
-            float e[V];
-            exchange<V>(folds, it, own, w.warp, w.warps, w.lane, w.rank, w.cluster, wait, carry, e);
+            for (int k = L - 1; k >= 0; --k) {
+                own.a = mul(own.a, z[k]);
+                own.b = mul(z[k], add(own.b, d[k]));
+            }
+            Lane<V> e = exchange(folds, it, own, w.warp, w.warps, w.lane, w.rank, w.cluster, wait, carry);
             if (TMA) {
                 if (w.lane == 0) bulk_wait_read<0>();
                 __syncwarp();
@@ -631,15 +711,11 @@ __global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
                 G *o = dg + 2 * step * (t + L - 1);
 #pragma unroll
                 for (int k = L - 1; k >= 0; --k, o -= 2 * step) {
-                    float dz[V], dn[V];
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float all = d[k][i] + e[i];
-                        const bool live = whole || k < n;
-                        dz[i] = live ? all * q[k][i] : 0.0f;
-                        dn[i] = live ? all * take[k][i] : 0.0f;
-                        e[i] = z[k][i] * all;
-                    }
+                    const Lane<V> all = add(d[k], e);
+                    const bool live = whole || k < n;
+                    const Lane<V> dz = live ? mul(all, q[k]) : Lane<V>(0.0f);
+                    const Lane<V> dn = live ? mul(all, take[k]) : Lane<V>(0.0f);
+                    e = mul(z[k], all);
                     if (TMA) {
                         mine.dz.put(k, w.lane, dz);
                         mine.dn.put(k, w.lane, dn);
@@ -664,15 +740,12 @@ __global__ void __launch_bounds__(32 * kMaxWarps, kCtasPerSm)
             }
         }
         if (g.on) {
-            const float zero[V] = {};
+            const Lane<V> zero(0.0f);
             for (int t = rounds * round + w.chunk; t < p.d.T; t += w.span) {
                 store<G, V>(dg + 2 * step * t, zero);
                 store<G, V>(dg + 2 * step * t + hidden, zero);
             }
-            if (p.d.dh0 && w.chunk == 0) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) p.d.dh0[g.chain + i] = carry[i];
-            }
+            if (p.d.dh0 && w.chunk == 0) put_edge<V>(p.d.dh0, g.chain, carry);
         }
     }
     exchange_end(folds, p.cluster);
@@ -694,17 +767,20 @@ __global__ void __launch_bounds__(kStepThreads)
         const int64_t at = static_cast<int64_t>(slot) * hidden + c;
         Pack<G, V> gz, gn;
         Pack<float, V> s;
-        load<G, V>(gz, g + b * 2 * hidden + c);
-        load<G, V>(gn, g + b * 2 * hidden + hidden + c);
+        gz.w = *reinterpret_cast<const typename Pack<G, V>::W *>(g + b * 2 * hidden + c);
+        gn.w = *reinterpret_cast<const typename Pack<G, V>::W *>(g + b * 2 * hidden + hidden + c);
         s.w = *reinterpret_cast<const typename Pack<float, V>::W *>(state + at);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const Gate z = scan_gate(to_f32(gz.v[k]));
+            const Gate z = gate(to_f32(gz.v[k]));
             s.v[k] = v[k] = z.keep * s.v[k] + z.take * to_f32(gn.v[k]);
         }
         *reinterpret_cast<typename Pack<float, V>::W *>(new_state + at) = s.w;
     }
-    store<Hy, V>(h + b * hidden + c, v);
+    Pack<Hy, V> o;
+#pragma unroll
+    for (int k = 0; k < V; ++k) o.v[k] = from_f32<Hy>(v[k]);
+    *reinterpret_cast<typename Pack<Hy, V>::W *>(h + b * hidden + c) = o.w;
 }
 
 template <typename F>
@@ -771,16 +847,20 @@ int resident_clusters(const void *fn, int c, int threads, int smem, const Device
 // with the fewest rounds in all (rounds of a sequence times turns of a
 // cluster): several CTAs share a sequence's time where the channels alone would
 // leave SMs idle.
-int scan_shape(const void *fn, const GlrDesc &d, int V, int L, int smem, const DeviceState &ds, ScanParams &p,
+template <typename S, int V>
+int scan_shape(const void *fn, const GlrDesc &d, int smem, const DeviceState &ds, ScanParams &p,
                cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr) {
+    constexpr int L = S::kSteps;
     p.d = d;
     p.err = ds.err_word;
     p.timeout_ns = wait_timeout_ns();
-    p.tiles = (d.hidden + 32 * V - 1) / (32 * V);
-    p.groups = static_cast<int64_t>(p.tiles) * d.batch;
-    const int warps = std::min(kMaxWarps, (d.T + L - 1) / L);
+    p.tiles = static_cast<uint32_t>((d.hidden + 32LL * V - 1) / (32 * V));
+    const int64_t groups = static_cast<int64_t>(p.tiles) * d.batch;
+    if (groups > (1LL << 31)) return set_error(ISAM_ERR_UNSUPPORTED, "batch * hidden is too large for one launch");
+    p.groups = static_cast<uint32_t>(groups);
+    const int warps = std::min(S::kWarps, (d.T + L - 1) / L);
     const int bytes = smem * warps;
-    const int rc = ensure_smem_optin(fn, smem * kMaxWarps, ds.device, "cudaFuncSetAttribute(gated linear recurrence)");
+    const int rc = ensure_smem_optin(fn, smem * S::kWarps, ds.device, "cudaFuncSetAttribute(gated linear recurrence)");
     if (rc) return rc;
     int64_t best = 0, grid = 0;
     for (int c = 1; c <= kMaxCluster; ++c) {
@@ -788,8 +868,8 @@ int scan_shape(const void *fn, const GlrDesc &d, int V, int L, int smem, const D
         if (c > 1 && span - warps * L >= d.T) break;  // CTAs without steps
         const int64_t resident = resident_clusters(fn, c, 32 * warps, bytes, ds);
         if (resident < 1) continue;
-        const int64_t ids = std::min(resident, p.groups);
-        const int64_t cost = (d.T + span - 1) / span * ((p.groups + ids - 1) / ids);
+        const int64_t ids = std::min(resident, groups);
+        const int64_t cost = (d.T + span - 1) / span * ((groups + ids - 1) / ids);
         if (grid == 0 || cost < best) {
             best = cost;
             grid = ids * c;
@@ -809,13 +889,15 @@ int scan_shape(const void *fn, const GlrDesc &d, int V, int L, int smem, const D
     return ISAM_OK;
 }
 
-template <typename G, typename Hy, int V, int L, bool TMA>
+template <typename G, typename Hy, int V, bool TMA>
 int forward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
+    using S = Shape<V, false>;
+    constexpr int L = S::kSteps;
     const auto fn = glr_forward_kernel<G, Hy, V, L, TMA>;
     ScanParams p{};
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
-    int rc = scan_shape(reinterpret_cast<const void *>(fn), d, V, L, sizeof(ForwardTiles<G, Hy, V, L>), ds, p, cfg, attr);
+    int rc = scan_shape<S, V>(reinterpret_cast<const void *>(fn), d, sizeof(ForwardTiles<G, Hy, V, L>), ds, p, cfg, attr);
     if (rc) return rc;
     CUtensorMap tg{}, th{};
     if (TMA) {
@@ -827,13 +909,15 @@ int forward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
     return e == cudaSuccess ? ISAM_OK : cuda_error(e, "launch glr_forward_kernel");
 }
 
-template <typename G, typename Hy, int V, int L, bool TMA>
+template <typename G, typename Hy, int V, bool TMA>
 int backward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
+    using S = Shape<V, true>;
+    constexpr int L = S::kSteps;
     const auto fn = glr_backward_kernel<G, Hy, V, L, TMA>;
     ScanParams p{};
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
-    int rc = scan_shape(reinterpret_cast<const void *>(fn), d, V, L, sizeof(BackwardTiles<G, Hy, V, L>), ds, p, cfg, attr);
+    int rc = scan_shape<S, V>(reinterpret_cast<const void *>(fn), d, sizeof(BackwardTiles<G, Hy, V, L>), ds, p, cfg, attr);
     if (rc) return rc;
     CUtensorMap tg{}, th{}, tdh{}, tdg{};
     if (TMA) {
@@ -857,10 +941,10 @@ int glr_forward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
         using Hy = decltype(ht);
         constexpr int V = sizeof(G) == 2 ? 2 : 1;
         if (rows16(d.hidden, d.g_type, d.g) && rows16(d.hidden, d.h_type, d.h_out))
-            return forward_launch<G, Hy, V, 16, true>(d, ds, s);
+            return forward_launch<G, Hy, V, true>(d, ds, s);
         if (V == 2 && vector_ok(d.hidden, V, d.g_type, d.g) && vector_ok(d.hidden, V, d.h_type, d.h_out))
-            return forward_launch<G, Hy, V, 16, false>(d, ds, s);
-        return forward_launch<G, Hy, 1, 16, false>(d, ds, s);
+            return forward_launch<G, Hy, V, false>(d, ds, s);
+        return forward_launch<G, Hy, 1, false>(d, ds, s);
     });
 }
 
@@ -871,11 +955,11 @@ int glr_backward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
         constexpr int V = sizeof(G) == 2 ? 2 : 1;
         if (rows16(d.hidden, d.g_type, d.g) && rows16(d.hidden, d.h_type, d.h_in) &&
             rows16(d.hidden, d.h_type, d.dh_out) && rows16(d.hidden, d.g_type, d.dg))
-            return backward_launch<G, Hy, V, 8, true>(d, ds, s);
+            return backward_launch<G, Hy, V, true>(d, ds, s);
         if (V == 2 && vector_ok(d.hidden, V, d.g_type, d.g) && vector_ok(d.hidden, V, d.g_type, d.dg) &&
             vector_ok(d.hidden, V, d.h_type, d.h_in) && vector_ok(d.hidden, V, d.h_type, d.dh_out))
-            return backward_launch<G, Hy, V, 8, false>(d, ds, s);
-        return backward_launch<G, Hy, 1, 8, false>(d, ds, s);
+            return backward_launch<G, Hy, V, false>(d, ds, s);
+        return backward_launch<G, Hy, 1, false>(d, ds, s);
     });
 }
 
