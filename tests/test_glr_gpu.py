@@ -147,6 +147,47 @@ def test_ordinary_and_long(T, B, H):
     check_both(T, B, H, "f32", "bf16", seed=12, lengths=[T - (T * b) // B for b in range(B)])
 
 
+@pytest.mark.parametrize("gt,ht", TYPES)
+@pytest.mark.parametrize("T,B,H,shift", [(70, 3, 67, 0), (70, 2, 67, 1), (41, 1, 129, 1), (33, 2, 66, 1), (65, 3, 1, 1),
+                                         (40, 1, 63, 3), (300, 1, 65, 1), (34, 2, 128, 1)])
+def test_rows_on_any_element(T, B, H, shift, gt, ht):
+    """Tensors that start `shift` elements into a buffer, rows of odd and even
+    widths: nothing before or behind an array is written, and its first and
+    last words are right."""
+    import torch
+    g, h0, n, dh, dl = make(T, B, H, gt, ht, seed=T + H)
+
+    def at(t):
+        buf = torch.full((t.numel() + shift + 8,), CANARY, dtype=t.dtype, device="cuda")
+        buf[shift:shift + t.numel()] = t.reshape(-1).cuda()
+        return buf, buf[shift:shift + t.numel()]
+
+    def clean(buf, n):
+        return bool((buf[:shift] == buf.new_tensor(CANARY)).all()) and bool((buf[shift + n:] == buf.new_tensor(CANARY)).all())
+
+    gd, dhd = at(g)[1], at(dh)[1]
+    hb, h = at(torch.zeros(T, B, H, dtype=tdtype(ht)))
+    db, dg = at(torch.zeros(T, B, 2 * H, dtype=tdtype(gt)))
+    last, dh0 = torch.empty(B, H, device="cuda"), torch.empty(B, H, device="cuda")
+    isam.glr_forward(T, B, H, gd, h0.cuda(), None, h, last)
+    isam.glr_backward(T, B, H, gd, h0.cuda(), None, h, dhd, dl.cuda(), dg, dh0)
+    isam.sync()
+    out, lr = lm_ref.recurrence(f64(g), f64(h0), n)
+    close(h.float().cpu().numpy().reshape(T, B, H), out, ht == "bf16")
+    close(last.cpu().numpy(), lr, False)
+    dref, eref = lm_ref.recurrence_backward(f64(g), f64(h0), n, h.double().cpu().numpy().reshape(T, B, H), f64(dh), f64(dl))
+    close(dg.float().cpu().numpy().reshape(T, B, 2 * H), dref, gt == "bf16")
+    close(dh0.cpu().numpy(), eref, False)
+    assert clean(hb, T * B * H) and clean(db, T * B * 2 * H)
+
+
+@pytest.mark.parametrize("gt,ht", TYPES)
+@pytest.mark.parametrize("T,B,H,lengths", [(16, 3, 65, None), (17, 3, 65, None), (19, 130, 1021, None),
+                                           (18, 256, 4096, None), (21, 4, 33000, [21, 0, 1, 9])])
+def test_few_steps_and_many_channels(T, B, H, lengths, gt, ht):
+    check_both(T, B, H, gt, ht, seed=T + B, lengths=lengths)
+
+
 def test_saturated_gates():
     """z = 1 to the last bit: the state stays h0 (what is taken of n, e^-40,
     is below a unit of it); z = 0: the state is the candidate."""
