@@ -1,111 +1,563 @@
 // glu.cu -- gated feed-forward product h = act(x Wg^T) * (x Wu^T), with
 // W = [Wg; Wu] one [2F][D] matrix, and its backward pass.
+//
+// One kernel on pairs of SMs (tcgen05 cta_group::2) computes 256 x BN tiles in
+// four roles.  PROJECT: A = x (256 tokens), B = BN/2 gate rows of W in the first
+// CTA's shared memory and the same features' up rows in the second's, so one
+// MMA gives both projections of a feature in one TMEM lane, BN/2 columns
+// apart, and the epilogue forms act(g) u without either reaching memory.
+// PROJECT_BACK: the same product, but the epilogue reads dh and writes
+// d = [dh u act'(g) | dh act(g)] (g and u fp32; d is rounded to bf16 once, as an
+// operand of the next products).  PRODUCT: dx = d W and dW = d^T x, bf16 out,
+// A K-major or MN-major, B MN-major.
+//
+// Bound: the tensor cores for many tokens, reading W for few.
+#include <algorithm>
+
+#include "gemm_common.cuh"
 #include "internal.h"
 #include "lm_common.cuh"
+#include "ptx.cuh"
 
 namespace isam {
 
 namespace {
 
-constexpr int kTile = 16;
+enum Role { PROJECT, PROJECT_BACK, PRODUCT };
 
-// Gate and up sums of one (token, feature) by one thread, 16 x 16 a block;
-// BACK: writes d[t][f] = dh u act'(g) and d[t][F + f] = dh act(g).
+constexpr int kPM = 256;   // tile rows of a pair
+constexpr int kHalf = 128; // rows of A in each CTA
+constexpr int kBK = 64;
+constexpr int kThreads = 192;
+constexpr int kAStage = kHalf * kBK * 2;
+constexpr int kStage = 4096;                  // 32 rows x 64 bf16 of a result, 128-byte swizzled
+constexpr int kEpiBytes = 4 * 2 * kStage;     // two a warp
+constexpr uint32_t kTmemCols = 512;           // two accumulators of up to 256 columns
+constexpr uint16_t kBoth = 0x3;
+
+enum : uint32_t {
+    SITE_U_EMPTY = 0x701,
+    SITE_U_FULL = 0x702,
+    SITE_U_TEMPTY = 0x703,
+    SITE_U_TFULL = 0x704,
+    SITE_U_DONE = 0x705,
+};
+
+// B's columns in each CTA (BN / 2), padded to what MN-major loads bring.
+constexpr int b_stage(int BN, bool B_MN) { return (B_MN ? (BN / 2 + 63) / 64 * 64 : BN / 2) * kBK * 2; }
+
+struct GluParams {
+    int T, F, N;       // tokens and features of a projection; N: columns of a product
+    int64_t M;         // rows of the result
+    int m_tiles, n_tiles, kb_total;
+    int stages, group_m;
+    int act;
+    int tma_out;       // the result's rows are on 16-byte boundaries
+    uint16_t *out;     // PROJECT: h
+    const uint16_t *dh;
+    unsigned long long timeout_ns;
+    uint32_t *err;
+};
+
+__device__ __forceinline__ void tile_coords(int tile, const GluParams &p, int &mt, int &nt) {
+    const int per_group = p.group_m * p.n_tiles;
+    const int g = tile / per_group;
+    const int first_m = g * p.group_m;
+    const int gm = min(p.group_m, p.m_tiles - first_m);
+    const int local = tile - g * per_group;
+    mt = first_m + local % gm;
+    nt = local / gm;
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t w;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+    return w;
+}
+
+// 32 gate and up sums of one token to packed bf16: h, or dg and du.
 template <int ACT, bool BACK>
-__global__ void __launch_bounds__(kTile *kTile)
-    glu_kernel(int T, int D, int F, const bf16 *x, const bf16 *W, const bf16 *dh, bf16 *out) {
-    __shared__ float sx[kTile][kTile + 1], sg[kTile][kTile + 1], su[kTile][kTile + 1];
-    const int tx = threadIdx.x % kTile, ty = threadIdx.x / kTile;
-    const int64_t f = static_cast<int64_t>(blockIdx.x) * kTile + tx, t = static_cast<int64_t>(blockIdx.y) * kTile + ty;
-    const int64_t wf = static_cast<int64_t>(blockIdx.x) * kTile + ty;
-    float g = 0.0f, u = 0.0f;
-    for (int k0 = 0; k0 < D; k0 += kTile) {
-        const int k = k0 + tx;
-        sx[ty][tx] = t < T && k < D ? to_f32(x[t * D + k]) : 0.0f;
-        sg[ty][tx] = wf < F && k < D ? to_f32(W[wf * D + k]) : 0.0f;
-        su[ty][tx] = wf < F && k < D ? to_f32(W[(wf + F) * D + k]) : 0.0f;
-        __syncthreads();
-        for (int i = 0; i < kTile; ++i) {
-            g += sx[ty][i] * sg[tx][i];
-            u += sx[ty][i] * su[tx][i];
+__device__ __forceinline__ void gate32(const uint32_t (&g)[32], const uint32_t (&u)[32], const uint32_t (&dh)[16],
+                                       uint32_t (&a)[16], uint32_t (&b)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float x[2], y[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float v, dv;
+            const float up = __uint_as_float(u[2 * i + k]);
+            activation<ACT>(__uint_as_float(g[2 * i + k]), v, dv);
+            if (BACK) {
+                const float d = __uint_as_float(k ? dh[i] & 0xffff0000u : dh[i] << 16);
+                x[k] = d * up * dv;
+                y[k] = d * v;
+            } else {
+                x[k] = v * up;
+            }
         }
-        __syncthreads();
+        a[i] = pack2(x[0], x[1]);
+        if (BACK) b[i] = pack2(y[0], y[1]);
     }
-    if (t >= T || f >= F) return;
-    float a, da;
-    activation<ACT>(g, a, da);
-    if (BACK) {
-        const float d = to_f32(dh[t * F + f]);
-        out[t * 2 * F + f] = from_f32<bf16>(d * u * da);
-        out[t * 2 * F + F + f] = from_f32<bf16>(d * a);
-    } else {
-        out[t * F + f] = from_f32<bf16>(a * u);
-    }
-}
-
-// C (M x N, bf16) = op(A) B, B K x N; A_T: A stored K x M.
-template <bool A_T>
-__global__ void __launch_bounds__(kTile *kTile)
-    glu_product_kernel(int64_t M, int64_t N, int64_t K, const bf16 *A, const bf16 *B, bf16 *C) {
-    __shared__ float sa[kTile][kTile + 1], sb[kTile][kTile + 1];
-    const int tx = threadIdx.x % kTile, ty = threadIdx.x / kTile;
-    const int64_t m0 = static_cast<int64_t>(blockIdx.y) * kTile, n = static_cast<int64_t>(blockIdx.x) * kTile + tx;
-    float sum = 0.0f;
-    for (int64_t k0 = 0; k0 < K; k0 += kTile) {
-        if (A_T)
-            sa[tx][ty] = m0 + tx < M && k0 + ty < K ? to_f32(A[(k0 + ty) * M + m0 + tx]) : 0.0f;
-        else
-            sa[ty][tx] = m0 + ty < M && k0 + tx < K ? to_f32(A[(m0 + ty) * K + k0 + tx]) : 0.0f;
-        sb[ty][tx] = n < N && k0 + ty < K ? to_f32(B[(k0 + ty) * N + n]) : 0.0f;
-        __syncthreads();
-        for (int i = 0; i < kTile; ++i) sum += sa[ty][i] * sb[i][tx];
-        __syncthreads();
-    }
-    if (m0 + ty < M && n < N) C[(m0 + ty) * N + n] = from_f32<bf16>(sum);
-}
-
-dim3 tiles(int64_t n, int64_t m) {
-    return dim3(static_cast<unsigned>((n + kTile - 1) / kTile), static_cast<unsigned>((m + kTile - 1) / kTile));
 }
 
 template <bool BACK>
-int glu_run(int T, int D, int F, int act, const uint16_t *x, const uint16_t *W, const uint16_t *dh, uint16_t *out,
+__device__ __forceinline__ void gate32(int act, const uint32_t (&g)[32], const uint32_t (&u)[32],
+                                       const uint32_t (&dh)[16], uint32_t (&a)[16], uint32_t (&b)[16]) {
+    if (act == ISAM_ACT_SILU)
+        gate32<ISAM_ACT_SILU, BACK>(g, u, dh, a, b);
+    else if (act == ISAM_ACT_GELU)
+        gate32<ISAM_ACT_GELU, BACK>(g, u, dh, a, b);
+    else if (act == ISAM_ACT_RELU)
+        gate32<ISAM_ACT_RELU, BACK>(g, u, dh, a, b);
+    else
+        gate32<ISAM_ACT_SIGMOID, BACK>(g, u, dh, a, b);
+}
+
+// 32 packed values (64 bytes) of this lane's row into half `half` of a
+// 32-row, 128-byte-swizzled staging tile.
+__device__ __forceinline__ void stage32(uint8_t *tile, int lane, int half, const uint32_t (&a)[16]) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const int pos = (half * 4 + c) ^ (lane & 7);
+        *reinterpret_cast<uint4 *>(tile + lane * 128 + pos * 16) =
+            make_uint4(a[4 * c], a[4 * c + 1], a[4 * c + 2], a[4 * c + 3]);
+    }
+}
+
+template <Role ROLE, int BN, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(kThreads, 1)
+    glu_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                    const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmC2,
+                    const __grid_constant__ GluParams p) {
+    if (!launch_shape_ok(p.err, 2u, gridDim.x, 0x7F0u)) return;
+    constexpr int kBHalf = BN / 2;
+    constexpr int kBStage = b_stage(BN, B_MN);
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                                ~static_cast<uintptr_t>(1023));
+    const int ST = p.stages;
+    uint8_t *sA = smem;
+    uint8_t *sB = smem + static_cast<size_t>(ST) * kAStage;
+    uint8_t *ebuf = sB + static_cast<size_t>(ST) * kBStage;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(ebuf + kEpiBytes);
+    uint64_t *full = bars;         // [ST] first CTA: both CTAs' copies of a stage landed
+    uint64_t *empty = full + ST;   // [ST] both: the pair's MMAs have read the stage
+    uint64_t *tfull = empty + ST;  // [2] both: accumulator complete
+    uint64_t *tempty = tfull + 2;  // [2] first CTA: 8 epilogue warps released it
+    uint64_t *done = tempty + 2;   // local epilogue warps finished with TMEM
+    uint64_t *mq = done + 1;       // first CTA: all its MMAs complete
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(mq + 1);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const bool leader = rank == 0;
+    const int pair = blockIdx.x >> 1;
+    const int num_pairs = gridDim.x >> 1;
+    const int num_tiles = p.m_tiles * p.n_tiles;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&tfull[i], 1);
+            mbar_init(&tempty[i], 8);
+        }
+        mbar_init(done, 4);
+        mbar_init(mq, 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+        tma_prefetch_desc(&tmA);
+        tma_prefetch_desc(&tmB);
+    }
+    __syncwarp();
+    if (warp == 1) {
+        tmem_alloc_pair(tmem_slot, kTmemCols);
+        tmem_relinquish_pair();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();  // both CTAs' barriers and TMEM exist before any cross-CTA traffic
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    const WaitCtx w{p.timeout_ns, p.err, abort_flag};
+
+    griddep_launch_dependents();
+    griddep_wait();
+
+    bool aborted = false;
+    if (warp == 0) {
+        // ------------------------------------------------ TMA producer (both CTAs)
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
+                int mt, nt;
+                tile_coords(tile, p, mt, nt);
+                const int arow = mt * kPM + static_cast<int>(rank) * kHalf;
+                // Projections: this CTA's rows of W are the tile's gate rows or its up rows.
+                const int bcol = ROLE == PRODUCT ? nt * BN + static_cast<int>(rank) * kBHalf
+                                                 : nt * kBHalf + (leader ? 0 : p.F);
+                for (int kb = 0; kb < p.kb_total; ++kb) {
+                    if (!bounded_wait<true>(&empty[stage], phase ^ 1u, w, SITE_U_EMPTY)) {
+                        ok = false;
+                        break;
+                    }
+                    if (leader) mbar_arrive_expect_tx(&full[stage], 2u * (kAStage + kBStage));
+                    const uint32_t fb = mapa_shared(smem_u32(&full[stage]), 0u);
+                    uint8_t *a = sA + static_cast<size_t>(stage) * kAStage;
+                    uint8_t *b = sB + static_cast<size_t>(stage) * kBStage;
+                    const int k0 = kb * kBK;
+                    if (A_MN) {
+                        tma_load_2d_pair(&tmA, fb, a, arow, k0);
+                        tma_load_2d_pair(&tmA, fb, a + 8192, arow + 64, k0);
+                    } else {
+                        tma_load_2d_pair(&tmA, fb, a, k0, arow);
+                    }
+                    if (B_MN) {
+#pragma unroll
+                        for (int c = 0; c < kBHalf; c += 64) tma_load_2d_pair(&tmB, fb, b + c * 128, bcol + c, k0);
+                    } else {
+                        tma_load_2d_pair(&tmB, fb, b, k0, bcol);
+                    }
+                    if (++stage == ST) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+            }
+            aborted = !ok;
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ------------------------------------------------ MMA issuer (first CTA)
+        if (lane == 0 && leader) {
+            const uint32_t idesc = idesc_bf16_f32(kPM, BN, A_MN, B_MN);
+            int stage = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            bool ok = true, issued = false;
+            for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
+                if (!bounded_wait<true>(&tempty[acc], acc_phase ^ 1u, w, SITE_U_TEMPTY)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t d = tmem_base + static_cast<uint32_t>(acc * 256);
+                for (int kb = 0; kb < p.kb_total; ++kb) {
+                    if (!bounded_wait<true>(&full[stage], phase, w, SITE_U_FULL)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t a0 = smem_u32(sA + static_cast<size_t>(stage) * kAStage);
+                    const uint32_t b0 = smem_u32(sB + static_cast<size_t>(stage) * kBStage);
+#pragma unroll
+                    for (int k = 0; k < kBK / 16; ++k) {
+                        const uint64_t ad =
+                            A_MN ? sdesc_sw128(a0 + k * 2048, 8192, 1024) : sdesc_sw128(a0 + k * 32, 16, 1024);
+                        const uint64_t bd =
+                            B_MN ? sdesc_sw128(b0 + k * 2048, 8192, 1024) : sdesc_sw128(b0 + k * 32, 16, 1024);
+                        umma_bf16_pair(d, ad, bd, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                    }
+                    issued = true;
+                    umma_commit_pair(&empty[stage], kBoth);
+                    if (++stage == ST) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+                if (!ok) break;
+                umma_commit_pair(&tfull[acc], kBoth);
+                if (++acc == 2) {
+                    acc = 0;
+                    acc_phase ^= 1u;
+                }
+            }
+            // Every MMA of this thread has completed before TMEM can be freed.
+            if (issued) {
+                umma_commit_pair(mq, 0x1);
+                drain_wait(mq, 0, p.timeout_ns);
+            }
+            aborted = !ok;
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------ epilogue (warps 2-5, both CTAs)
+        const int q = warp & 3;  // TMEM lane quadrant this warp may read
+        uint8_t *stg = ebuf + (warp - 2) * 2 * kStage;
+        int acc = 0, buf = 0;
+        uint32_t acc_phase = 0;
+        bool ok = true;
+        for (int tile = pair; tile < num_tiles; tile += num_pairs) {
+            int mt, nt;
+            tile_coords(tile, p, mt, nt);
+            const int row0 = mt * kPM + static_cast<int>(rank) * kHalf + q * 32;
+            const int64_t row = row0 + lane;
+            const uint32_t tb =
+                tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * 256);
+            if constexpr (ROLE == PRODUCT) {
+                if (!warp_wait<true>(&tfull[acc], acc_phase, w, SITE_U_TFULL)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const int col0 = nt * BN;
+#pragma unroll 1
+                for (int j = 0; j < BN / 64; ++j, buf ^= 1) {
+                    if (lane == 0) bulk_wait_read<1>();  // the store of two chunks ago has left the tile
+                    __syncwarp();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t r[32], a[16];
+                        tmem_ld32(tb + j * 64 + h * 32, r);
+                        tmem_ld_wait(r);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            a[i] = pack2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+                        stage32(stg + buf * kStage, lane, h, a);
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (row0 < p.M && col0 + j * 64 < p.N) tma_store_2d(&tmC, stg + buf * kStage, col0 + j * 64, row0);
+                        bulk_commit();
+                    }
+                }
+            } else {
+                constexpr bool BACK = ROLE == PROJECT_BACK;
+                const int f0 = nt * kBHalf;
+                uint32_t dh[16] = {}, next[16] = {};
+                const auto fetch = [&](int f) {  // 32 gradients of this lane's token (F is a multiple of 8)
+                    if (!BACK) return;
+                    const uint4 *at = reinterpret_cast<const uint4 *>(p.dh + row * p.F + f);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (row < p.T && f + 8 * c < p.F) v = __ldcs(at + c);
+                        next[4 * c] = v.x, next[4 * c + 1] = v.y, next[4 * c + 2] = v.z, next[4 * c + 3] = v.w;
+                    }
+                };
+                fetch(f0);
+                if (!warp_wait<true>(&tfull[acc], acc_phase, w, SITE_U_TFULL)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+#pragma unroll 1
+                for (int j = 0; j < kBHalf / 32; ++j) {
+                    const int f = f0 + j * 32;
+                    uint32_t g[32], u[32], a[16], b[16];
+                    tmem_ld32(tb + j * 32, g);
+                    tmem_ld32(tb + kBHalf + j * 32, u);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) dh[i] = next[i];
+                    if (j + 1 < kBHalf / 32) fetch(f + 32);
+                    tmem_ld_wait(g);
+                    tmem_ld_wait(u);
+                    gate32<BACK>(p.act, g, u, dh, a, b);
+                    if (p.tma_out) {
+                        // PROJECT: two 64-column tiles in turn; PROJECT_BACK: dg in one, du in the other.
+                        uint8_t *to = stg + (BACK ? 0 : buf * kStage);
+                        if ((j & 1) == 0) {
+                            if (lane == 0) {
+                                if (BACK)
+                                    bulk_wait_read<0>();
+                                else
+                                    bulk_wait_read<1>();
+                            }
+                            __syncwarp();
+                        }
+                        stage32(to, lane, j & 1, a);
+                        if (BACK) stage32(to + kStage, lane, j & 1, b);
+                        if (j & 1) {
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0) {
+                                const int c = f - 32;
+                                if (row0 < p.T && c < p.F) {
+                                    tma_store_2d(&tmC, to, c, row0);
+                                    if (BACK) tma_store_2d(&tmC2, to + kStage, c, row0);
+                                }
+                                bulk_commit();
+                            }
+                            buf ^= 1;
+                        }
+                    } else if (row < p.T) {
+                        uint16_t *at = p.out + row * p.F + f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            if (f + 2 * i < p.F) at[2 * i] = static_cast<uint16_t>(a[i]);
+                            if (f + 2 * i + 1 < p.F) at[2 * i + 1] = static_cast<uint16_t>(a[i] >> 16);
+                        }
+                    }
+                }
+            }
+            // Release this accumulator on the first CTA's barrier.
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote(&tempty[acc], 0u);
+            __syncwarp();
+            if (++acc == 2) {
+                acc = 0;
+                acc_phase ^= 1u;
+            }
+        }
+        if (lane == 0) bulk_wait_all<0>();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(done);
+        __syncwarp();
+        aborted = !ok;
+    }
+
+    // ---- teardown.  After an abort, copies this CTA issued may still be in
+    // flight towards its shared memory and complete on the first CTA's
+    // barriers: give them time to land (bounded, only on that path).
+    if (__syncthreads_or(aborted ? 1 : 0) && threadIdx.x == 0) {
+        const unsigned long long t0 = globaltimer();
+        while (globaltimer() - t0 < 50000ull) {
+        }
+    }
+    if (warp == 1) bounded_wait(done, 0, w, SITE_U_DONE);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    // Both CTAs' epilogues are done reading TMEM and the first CTA's MMAs have
+    // completed before the pair releases its TMEM together.
+    cluster_sync_all();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc_pair(tmem_base, kTmemCols);
+    }
+}
+
+size_t pair_smem(int stages, int bstage) {
+    return 1024 + static_cast<size_t>(stages) * (kAStage + bstage) + kEpiBytes + (2 * stages + 6) * 8 + 16;
+}
+
+template <Role ROLE, int BN, bool A_MN, bool B_MN>
+int pair_launch(GluParams p, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &c, const CUtensorMap &c2,
+                DeviceState &ds, cudaStream_t s) {
+    const auto fn = glu_pair_kernel<ROLE, BN, A_MN, B_MN>;
+    constexpr int bstage = b_stage(BN, B_MN);
+    const int pairs = gemm_cluster_capacity(ds, 2);
+    if (pairs < 1) return set_error(ISAM_ERR_UNSUPPORTED, "no pair of SMs is free for the gated feed-forward kernel");
+    int st = 8;
+    while (st > 2 && pair_smem(st, bstage) > static_cast<size_t>(ds.max_smem_optin)) --st;
+    p.stages = st;
+    p.group_m = 8;
+    p.timeout_ns = wait_timeout_ns();
+    p.err = ds.err_word;
+    const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.n_tiles;
+    if (tiles > 0x7fffffffLL) return set_error(ISAM_ERR_UNSUPPORTED, "too many tiles for one launch");
+    const int rc = ensure_smem_optin(reinterpret_cast<const void *>(fn), ds.max_smem_optin, ds.device,
+                                     "cudaFuncSetAttribute(gated feed-forward)");
+    if (rc) return rc;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    cfg.gridDim = dim3(static_cast<unsigned>(2 * std::min<int64_t>(tiles, pairs)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = pair_smem(st, bstage);
+    cfg.stream = s;
+    cfg.attrs = attr;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, a, b, c, c2, p);
+    return e == cudaSuccess ? ISAM_OK : cuda_error(e, "launch glu_pair_kernel");
+}
+
+int tiles_of(int64_t n, int tile) { return static_cast<int>((n + tile - 1) / tile); }
+
+// Rounds of tiles over the pairs, in columns: what a tile width costs.
+int64_t width_cost(int64_t m_tiles, int64_t n, int width, int pairs) {
+    return (m_tiles * tiles_of(n, width) + pairs - 1) / pairs * width;
+}
+
+template <Role ROLE, int BN>
+int project_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
+    GluParams p{};
+    p.T = d.T, p.F = d.F, p.M = d.T, p.N = d.F, p.act = d.act, p.out = d.h, p.dh = d.dh;
+    p.m_tiles = tiles_of(d.T, kPM);
+    p.n_tiles = tiles_of(d.F, BN / 2);
+    p.kb_total = tiles_of(d.D, kBK);
+    CUtensorMap a{}, b{}, c{}, c2{};
+    const uint64_t pitch = static_cast<uint64_t>(d.D) * 2, F = d.F;
+    int rc;
+    if ((rc = make_tmap_2d_bf16(&a, d.x, d.D, d.T, pitch, 64, kHalf))) return rc;
+    if ((rc = make_tmap_2d_bf16(&b, d.W, d.D, 2 * F, pitch, 64, BN / 2))) return rc;
+    if (ROLE == PROJECT_BACK) {
+        uint16_t *ws = static_cast<uint16_t *>(d.workspace);
+        p.tma_out = 1;
+        if ((rc = make_tmap_2d_bf16(&c, ws, F, d.T, 4 * F, 64, 32))) return rc;
+        if ((rc = make_tmap_2d_bf16(&c2, ws + F, F, d.T, 4 * F, 64, 32))) return rc;
+    } else if (F % 8 == 0 && reinterpret_cast<uintptr_t>(d.h) % 16 == 0) {
+        p.tma_out = 1;
+        if ((rc = make_tmap_2d_bf16(&c, d.h, F, d.T, 2 * F, 64, 32))) return rc;
+    }
+    return pair_launch<ROLE, BN, false, false>(p, a, b, c, c2, ds, s);
+}
+
+template <Role ROLE>
+int project(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
+    const int pairs = std::max(1, gemm_cluster_capacity(ds, 2));
+    const int64_t mt = tiles_of(d.T, kPM);
+    if (width_cost(mt, d.F, 64, pairs) < width_cost(mt, d.F, 128, pairs)) return project_launch<ROLE, 128>(d, ds, s);
+    return project_launch<ROLE, 256>(d, ds, s);
+}
+
+// C (M x N, bf16) = op(A) B with B K x N; A_MN: A stored K x M.
+template <bool A_MN, int BN>
+int product_launch(int64_t M, int N, int64_t K, const uint16_t *A, const uint16_t *B, uint16_t *C, DeviceState &ds,
+                   cudaStream_t s) {
+    GluParams p{};
+    p.M = M, p.N = N;
+    p.m_tiles = tiles_of(M, kPM);
+    p.n_tiles = tiles_of(N, BN);
+    p.kb_total = tiles_of(K, kBK);
+    CUtensorMap a{}, b{}, c{};
+    int rc;
+    rc = A_MN ? make_tmap_2d_bf16(&a, A, M, K, M * 2, 64, kBK) : make_tmap_2d_bf16(&a, A, K, M, K * 2, 64, kHalf);
+    if (rc) return rc;
+    if ((rc = make_tmap_2d_bf16(&b, B, N, K, static_cast<uint64_t>(N) * 2, 64, kBK))) return rc;
+    if ((rc = make_tmap_2d_bf16(&c, C, N, M, static_cast<uint64_t>(N) * 2, 64, 32))) return rc;
+    return pair_launch<PRODUCT, BN, A_MN, true>(p, a, b, c, c, ds, s);
+}
+
+template <bool A_MN>
+int product(int64_t M, int N, int64_t K, const uint16_t *A, const uint16_t *B, uint16_t *C, DeviceState &ds,
             cudaStream_t s) {
-    const auto fn = act == ISAM_ACT_SILU   ? glu_kernel<ISAM_ACT_SILU, BACK>
-                    : act == ISAM_ACT_GELU ? glu_kernel<ISAM_ACT_GELU, BACK>
-                    : act == ISAM_ACT_RELU ? glu_kernel<ISAM_ACT_RELU, BACK>
-                                           : glu_kernel<ISAM_ACT_SIGMOID, BACK>;
-    fn<<<tiles(F, T), kTile * kTile, 0, s>>>(T, D, F, reinterpret_cast<const bf16 *>(x),
-                                             reinterpret_cast<const bf16 *>(W), reinterpret_cast<const bf16 *>(dh),
-                                             reinterpret_cast<bf16 *>(out));
-    return launch_status("launch glu_kernel");
+    const int pairs = std::max(1, gemm_cluster_capacity(ds, 2));
+    const int64_t mt = tiles_of(M, kPM);
+    const int64_t c256 = width_cost(mt, N, 256, pairs), c192 = width_cost(mt, N, 192, pairs),
+                  c128 = width_cost(mt, N, 128, pairs);
+    if (c128 < std::min(c192, c256)) return product_launch<A_MN, 128>(M, N, K, A, B, C, ds, s);
+    if (c192 < c256) return product_launch<A_MN, 192>(M, N, K, A, B, C, ds, s);
+    return product_launch<A_MN, 256>(M, N, K, A, B, C, ds, s);
 }
 
 }  // namespace
 
-int glu_forward_launch(const GluDesc &p, DeviceState &ds, cudaStream_t s) {
-    return glu_run<false>(p.T, p.D, p.F, p.act, p.x, p.W, nullptr, p.h, s);
-}
+int glu_forward_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) { return project<PROJECT>(d, ds, s); }
 
 size_t glu_backward_workspace(int T, int D, int F) { return static_cast<size_t>(T) * F * 4; }
 
-int glu_backward_launch(const GluDesc &p, DeviceState &ds, cudaStream_t s) {
-    uint16_t *d = static_cast<uint16_t *>(p.workspace);
-    int rc = glu_run<true>(p.T, p.D, p.F, p.act, p.x, p.W, p.dh, d, s);
+int glu_backward_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
+    if (!d.dx && !d.dW) return ISAM_OK;
+    int rc = project<PROJECT_BACK>(d, ds, s);
     if (rc) return rc;
-    const int64_t F2 = 2 * static_cast<int64_t>(p.F);
-    if (p.dx) {
-        glu_product_kernel<false><<<tiles(p.D, p.T), kTile * kTile, 0, s>>>(
-            p.T, p.D, F2, reinterpret_cast<const bf16 *>(d), reinterpret_cast<const bf16 *>(p.W),
-            reinterpret_cast<bf16 *>(p.dx));
-        if ((rc = launch_status("launch glu_product_kernel"))) return rc;
-    }
-    if (p.dW) {
-        glu_product_kernel<true><<<tiles(p.D, F2), kTile * kTile, 0, s>>>(
-            F2, p.D, p.T, reinterpret_cast<const bf16 *>(d), reinterpret_cast<const bf16 *>(p.x),
-            reinterpret_cast<bf16 *>(p.dW));
-        if ((rc = launch_status("launch glu_product_kernel"))) return rc;
-    }
+    const uint16_t *ws = static_cast<const uint16_t *>(d.workspace);
+    const int64_t F2 = 2 * static_cast<int64_t>(d.F);
+    if (d.dx && (rc = product<false>(d.T, d.D, F2, ws, d.W, d.dx, ds, s))) return rc;
+    if (d.dW && (rc = product<true>(F2, d.D, d.T, ws, d.x, d.dW, ds, s))) return rc;
     return ISAM_OK;
 }
 
