@@ -4,6 +4,7 @@
 
 #include "internal.h"
 #include "lm_common.cuh"
+#include "ptx.cuh"
 
 namespace isam {
 
@@ -47,23 +48,54 @@ __global__ void __launch_bounds__(kThreads)
     tiled[i] = n < N && gr < groups ? scales[n * groups + gr] : static_cast<uint16_t>(0);
 }
 
-constexpr int kMaxWarps = 16;
-constexpr int kTileWords = 256;  // 32-bit words of a 16 x 128 tile
+constexpr int kTileBytes = 1024;  // codes of 16 rows x 128 k
+constexpr int kStages = 2;        // of a warp's ring
+constexpr int kMaxSmem = 224 * 1024;
 
-__device__ __forceinline__ void mma_16x8x16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-        "{%0, %1, %2, %3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// Bulk copy of global memory into shared memory, counted on a barrier.
+__device__ __forceinline__ void copy(uint32_t to, const void *from, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to),
+                 "l"(from), "r"(bytes), "r"(bar)
+                 : "memory");
 }
 
-// Codes 2 i and 2 i + 1 (in k) of a word as bf16 q - 8: the codes become the low
-// mantissa bits of 128 + q, and 136 is subtracted, all exact.
-__device__ __forceinline__ uint32_t dequant(uint32_t w, int i) {
-    uint32_t v;
-    asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(v) : "r"(w >> (4 * i)));
-    asm("fma.rn.bf16x2 %0, %0, %1, %2;" : "+r"(v) : "r"(0x3F803F80u), "r"(0xC308C308u));
+// c += a b (or c = a b) on 16 rows x 16 k x 8 tokens.
+template <bool FIRST>
+__device__ __forceinline__ void mma_16x8x16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if (FIRST) {
+        asm volatile(
+            "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+            "{%10, %10, %10, %10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+    } else {
+        asm volatile(
+            "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+            "{%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+}
+
+// The word's eight codes as four pairs of bf16 (q - 8) / 8, exactly, in the
+// order of k.  A code in the low four bits of a half is or-ed into the mantissa
+// of 16, where it counts eighths, and 17 is subtracted.  One in the next four
+// bits needs no shift: read as a bf16 it is q 2^-129 (eight and above reach the
+// lowest exponent, which has the spacing of the subnormals below it), and one
+// fused multiply-add makes that q / 8 - 1.
+__device__ __forceinline__ void dequant(uint32_t w, uint32_t (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; i += 2, w >>= 8) {
+        asm("lop3.b32 %0, %1, 0x000F000F, 0x41804180, 0xEA;" : "=r"(v[i]) : "r"(w));
+        asm("fma.rn.bf16x2 %0, %0, %1, %2;" : "+r"(v[i]) : "r"(0x3F803F80u), "r"(0xC188C188u));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[i + 1]) : "r"(w & 0x00F000F0u), "r"(0x7E807E80u), "r"(0xBF80BF80u));
+    }
+}
+
+// Shared-memory loads by 32-bit address.
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
     return v;
 }
 
@@ -72,14 +104,15 @@ template <int GROUP>
 struct RowScales {
     static constexpr int kPer = 128 / GROUP;
     uint32_t w[(kPer + 1) / 2];
-    __device__ __forceinline__ void load(const uint16_t *at) {
+    __device__ __forceinline__ void load(uint32_t at) {
         if constexpr (kPer == 4) {
-            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(at));
-            w[0] = v.x, w[1] = v.y;
+            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
         } else if constexpr (kPer == 2) {
-            w[0] = __ldg(reinterpret_cast<const uint32_t *>(at));
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at));
         } else {
-            w[0] = __ldg(at);
+            uint16_t h;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
+            w[0] = h;
         }
     }
     __device__ __forceinline__ float get(int j) const {
@@ -87,135 +120,290 @@ struct RowScales {
     }
 };
 
-// RB blocks of 16 rows by 8 NT tokens a CTA; its warps share K's tiles in turn
-// and their sums meet in shared memory, in the order of the warps.
+struct W4Params {
+    int M, N, K;
+    int kt;       // k tiles
+    int groups;   // of 16 RB rows
+    int team;     // warps that share the K of a group
+    int per_stage;  // k tiles of a stage
+    int x_stride;   // bytes of a token's row of x in shared memory
+    const uint16_t *x;
+    const uint8_t *tiled;
+    const uint16_t *scales;
+    float *y;
+    unsigned long long timeout_ns;
+    uint32_t *err;
+};
+
+template <int GROUP, int RB>
+constexpr int tile_bytes() {
+    return RB * (kTileBytes + 32 * (128 / GROUP));
+}
+template <int NT, int RB>
+constexpr int part_bytes() {  // a warp's sums, twice
+    return 2 * 8 * NT * 16 * RB * 4;
+}
+
+// One CTA an SM.  A team of its warps takes 16 RB rows by 8 NT tokens; its warps
+// share K's tiles in turn, `per_stage` neighbours each, and their sums meet in
+// shared memory, in the order of the warps.  Codes arrive by bulk copies into a
+// ring a warp, across groups of rows; x is in shared memory as a whole where it
+// fits (XS), rows 64 bytes off a multiple of 128 so that eight lanes' 16 bytes
+// touch every bank once.
 //
-// A tile is one k range of 128; lane 4 r + t holds rows r and 8 + r, in word j the
-// k of group t of 8 in 32-block j.  The order of k inside a product does not
-// matter, so the words' codes are operands of m16n8k16 as they lie, with the
-// token's same eight k, 16 bytes of x, beside them, and 16 of one 32-block's k in
-// each instruction: a scale applies to whole sums.
-template <int NT, int GROUP, int RB>
-__global__ void __launch_bounds__(32 * kMaxWarps)
-    gemv_w4_kernel(int M, int N, int K, int kt, const uint16_t *x, const uint4 *tiled, const uint16_t *scales,
-                   float *y) {
-    constexpr int kPer = 128 / GROUP;
-    extern __shared__ float part[];  // [warps][8 NT tokens][16 RB rows]
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+// Lane 4 r + t holds rows r and 8 + r of a tile, in word j the k of eight t of
+// 32-block j.  The order of k inside a product does not matter, so the words'
+// codes are operands of m16n8k16 as they lie, with the token's same eight k, 16
+// bytes of x, beside them, and 16 k of one 32-block in each instruction: a scale
+// applies to whole sums.
+//
+// Bound: reading the codes; beside it the instructions that make them bf16,
+// nine for eight codes.
+template <int NT, int GROUP, int RB, bool XS, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, 1) gemv_w4_kernel(const __grid_constant__ W4Params p) {
+    constexpr int kPer = 128 / GROUP, kRows = 16 * RB, kSize = kRows * 8 * NT;
+    // Word blocks of one scale summed before it applies (all of a tile's would cost
+    // registers where rows and tokens are many).
+    constexpr int kSpan = RB * NT > 2 ? 1 : GROUP / 32;
+    constexpr int kBlock = kTileBytes + 32 * kPer;  // codes and scales of one tile
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ uint64_t full_all[WARPS][kStages];
+    __shared__ int abort_flag;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int team = warp / p.team, member = warp - team * p.team, teams = WARPS / p.team;
+    const int per = p.per_stage, stage_bytes = per * RB * kBlock;
+    uint8_t *ring = smem + warp * kStages * stage_bytes;
+    float *part = reinterpret_cast<float *>(smem + WARPS * kStages * stage_bytes) + team * p.team * 2 * kSize;
+    uint8_t *xs = smem + WARPS * (kStages * stage_bytes + part_bytes<NT, RB>());
+    uint64_t *full = full_all[warp];
+    if (lane == 0)
+        for (int i = 0; i < kStages; ++i) mbar_init(&full[i], 1);
+    if (threadIdx.x == 0) abort_flag = 0;
+    fence_mbar_init();
+    __syncthreads();
+    const WaitCtx wait{p.timeout_ns, p.err, &abort_flag};
     const int r = lane >> 2, t = lane & 3;
-    const int nb = (N + 15) / 16, nb0 = blockIdx.x * RB;
-    float sum[RB][NT][4] = {};
-    uint4 code[RB][2];
-    RowScales<GROUP> sc[RB][2];
-    const auto load = [&](int k) {
-#pragma unroll
-        for (int b = 0; b < RB; ++b) {
-            const int64_t tile = static_cast<int64_t>(min(nb0 + b, nb - 1)) * kt + k;
-            const uint4 *at = tiled + tile * (kTileWords / 4) + lane;
-            code[b][0] = __ldcs(at);
-            code[b][1] = __ldcs(at + 32);
-            sc[b][0].load(scales + (tile * 16 + r) * kPer);
-            sc[b][1].load(scales + (tile * 16 + 8 + r) * kPer);
-        }
+    const int blocks = (p.N + 15) / 16;
+    const int first = team * gridDim.x + blockIdx.x, stride = teams * gridDim.x;  // groups of this team
+    const int k_first = member * per, k_stride = p.team * per;
+
+    // A stage: for each block of rows its tiles' codes, then their scales.
+    int load_group = first, load_k = k_first;
+    uint32_t load_to = smem_u32(ring), load_bar = smem_u32(full);
+    const uint32_t last_bar = load_bar + 8 * (kStages - 1);
+    const uint8_t *load_code;  // of the group's first block and load_k
+    const uint16_t *load_scale;
+    const auto enter = [&] {
+        const int64_t tile = static_cast<int64_t>(load_group) * RB * p.kt + load_k;
+        load_code = p.tiled + tile * kTileBytes;
+        load_scale = p.scales + tile * 16 * kPer;
     };
-    if (warp < kt) load(warp);
-    for (int k = warp; k < kt; k += warps) {
-        uint32_t w[RB][2][4];
-        RowScales<GROUP> s[RB][2];
+    enter();
+    const auto fetch = [&]() {  // lane 0
+        if (load_k >= p.kt) {
+            load_k = k_first;
+            load_group += stride;
+            enter();
+        }
+        if (load_group >= p.groups || load_k >= p.kt) return;
+        const uint32_t n = min(per, p.kt - load_k);
+        const int rows = RB == 1 ? 1 : min(RB, blocks - load_group * RB);
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(load_bar), "r"(rows * n * kBlock)
+                     : "memory");
 #pragma unroll
         for (int b = 0; b < RB; ++b)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                w[b][h][0] = code[b][h].x, w[b][h][1] = code[b][h].y;
-                w[b][h][2] = code[b][h].z, w[b][h][3] = code[b][h].w;
-                s[b][h] = sc[b][h];
+            if (b < rows) {
+                copy(load_to + b * per * kBlock, load_code + static_cast<int64_t>(b) * p.kt * kTileBytes, n * kTileBytes,
+                     load_bar);
+                copy(load_to + b * per * kBlock + per * kTileBytes, load_scale + static_cast<int64_t>(b) * p.kt * 16 * kPer,
+                     n * 32 * kPer, load_bar);
             }
-        if (k + warps < kt) load(k + warps);
-        float acc[RB][NT][4];
+        load_k += k_stride;
+        load_code += k_stride * kTileBytes;
+        load_scale += k_stride * 16 * kPer;
+        load_to += stage_bytes;
+        load_bar += 8;
+        if (load_bar > last_bar) {
+            load_bar -= 8 * kStages;
+            load_to -= kStages * stage_bytes;
+        }
+    };
+    if (lane == 0)
+        for (int i = 0; i < kStages; ++i) fetch();
+    if (XS) {
+        // x, and zeros behind K up to whole tiles.
+        const int chunks = 16 * p.kt;  // of 16 bytes
+        for (int i = threadIdx.x; i < p.M * chunks; i += 32 * WARPS) {
+            const int m = i / chunks, c = i - m * chunks;
+            uint8_t *to = xs + m * p.x_stride + 16 * c;
+            if (8 * c < p.K)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)),
+                             "l"(p.x + static_cast<int64_t>(m) * p.K + 8 * c)
+                             : "memory");
+            else
+                *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+    }
+
+    // A token's k of this lane (lanes behind the last token read it again).
+    const uint16_t *xg[NT];
+    uint32_t xa[NT];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint4 xv[NT];
+    for (int n = 0; n < NT; ++n) {
+        const int m = min(8 * n + r, p.M - 1);
+        xg[n] = p.x + static_cast<int64_t>(m) * p.K + 8 * t;
+        xa[n] = smem_u32(xs) + m * p.x_stride + 16 * t;
+    }
+    int stage = 0, half = 0;
+    uint32_t phase = 0;
+    const uint32_t ring_at = smem_u32(ring);
+    for (int g = first; g < p.groups; g += stride, half ^= 1) {
+        float sum[RB][NT][4] = {};
+        for (int k = k_first; k < p.kt; k += k_stride) {
+            bounded_wait(&full[stage], phase, wait, 0x801u);
+            uint32_t code_at = ring_at + stage * stage_bytes + 16 * lane;
+            uint32_t scale_at = ring_at + stage * stage_bytes + per * kTileBytes + 2 * kPer * r;
+            const uint32_t code_end = code_at + min(per, p.kt - k) * kTileBytes;
+            uint32_t x_at = 256 * k;  // bytes into a token's row
+#pragma unroll 1
+            for (; code_at != code_end; code_at += kTileBytes, scale_at += 32 * kPer, x_at += 256) {
+                uint4 code[RB][2];
+                RowScales<GROUP> scale[RB][2];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int m = 8 * n + r, at = 128 * k + 32 * j + 8 * t;
-                xv[n] = make_uint4(0, 0, 0, 0);
-                if (m < M && at < K) xv[n] = __ldg(reinterpret_cast<const uint4 *>(x + static_cast<int64_t>(m) * K + at));
-            }
+                for (int b = 0; b < RB; ++b)
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                if (j % (GROUP / 32) == 0) {
+                    for (int h = 0; h < 2; ++h) {
+                        code[b][h] = lds16(code_at + b * per * kBlock + 512 * h);
+                        scale[b][h].load(scale_at + b * per * kBlock + 16 * kPer * h);
+                    }
+                float acc[RB][NT][4];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[b][n][i] = 0.0f;
-                }
-                uint32_t a[4];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    a[0] = dequant(w[b][0][j], 2 * h);
-                    a[1] = dequant(w[b][1][j], 2 * h);
-                    a[2] = dequant(w[b][0][j], 2 * h + 1);
-                    a[3] = dequant(w[b][1][j], 2 * h + 1);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        mma_16x8x16(acc[b][n], a, h ? xv[n].z : xv[n].x, h ? xv[n].w : xv[n].y);
-                }
-                if ((j + 1) % (GROUP / 32) == 0) {
-                    const float lo = s[b][0].get(j / (GROUP / 32)), hi = s[b][1].get(j / (GROUP / 32));
+                for (int j = 0; j < 4; ++j) {
+                    uint4 xv[NT];
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        sum[b][n][0] += lo * acc[b][n][0];
-                        sum[b][n][1] += lo * acc[b][n][1];
-                        sum[b][n][2] += hi * acc[b][n][2];
-                        sum[b][n][3] += hi * acc[b][n][3];
+                        if (XS) {
+                            xv[n] = lds16(xa[n] + x_at + 64 * j);
+                        } else {
+                            xv[n] = make_uint4(0, 0, 0, 0);
+                            if (static_cast<int>(x_at / 2) + 32 * j + 8 * t < p.K)
+                                xv[n] = __ldg(reinterpret_cast<const uint4 *>(xg[n] + x_at / 2 + 32 * j));
+                        }
+                    }
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) {
+                        const uint32_t lo_w = j == 0 ? code[b][0].x : j == 1 ? code[b][0].y : j == 2 ? code[b][0].z : code[b][0].w;
+                        const uint32_t hi_w = j == 0 ? code[b][1].x : j == 1 ? code[b][1].y : j == 2 ? code[b][1].z : code[b][1].w;
+                        uint32_t v[2][4];
+                        dequant(lo_w, v[0]);
+                        dequant(hi_w, v[1]);
+                        const uint32_t a0[4] = {v[0][0], v[1][0], v[0][1], v[1][1]};
+                        const uint32_t a1[4] = {v[0][2], v[1][2], v[0][3], v[1][3]};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            if (j % kSpan == 0)
+                                mma_16x8x16<true>(acc[b][n], a0, xv[n].x, xv[n].y);
+                            else
+                                mma_16x8x16<false>(acc[b][n], a0, xv[n].x, xv[n].y);
+                            mma_16x8x16<false>(acc[b][n], a1, xv[n].z, xv[n].w);
+                        }
+                        if ((j + 1) % kSpan == 0) {
+                            const float lo = scale[b][0].get(j * 32 / GROUP), hi = scale[b][1].get(j * 32 / GROUP);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
+                                sum[b][n][0] = fmaf(lo, acc[b][n][0], sum[b][n][0]);
+                                sum[b][n][1] = fmaf(lo, acc[b][n][1], sum[b][n][1]);
+                                sum[b][n][2] = fmaf(hi, acc[b][n][2], sum[b][n][2]);
+                                sum[b][n][3] = fmaf(hi, acc[b][n][3], sum[b][n][3]);
+                            }
+                        }
                     }
                 }
             }
+            __syncwarp();  // every lane has read the stage
+            if (lane == 0) fetch();
+            if (++stage == kStages) {
+                stage = 0;
+                phase ^= 1u;
+            }
+        }
+        float *mine = part + half * p.team * kSize;
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    mine[member * kSize + (8 * n + 2 * t + (i & 1)) * kRows + 16 * b + r + 8 * (i >> 1)] = sum[b][n][i];
+        if (p.team == 1)
+            __syncwarp();
+        else
+            named_bar(1 + team, 32 * p.team);
+        for (int i = 32 * member + lane; i < kSize; i += 32 * p.team) {
+            const int m = i / kRows, n = g * kRows + i % kRows;
+            if (m >= p.M || n >= p.N) continue;
+            float v = 0.0f;
+            for (int q = 0; q < p.team; ++q) v += mine[q * kSize + i];
+            p.y[static_cast<int64_t>(m) * p.N + n] = 8.0f * v;  // (weights counted in eighths)
         }
     }
-    constexpr int kRows = 16 * RB, kSize = kRows * 8 * NT;
-#pragma unroll
-    for (int b = 0; b < RB; ++b)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                part[warp * kSize + (8 * n + 2 * t + (i & 1)) * kRows + 16 * b + r + 8 * (i >> 1)] = sum[b][n][i];
-    __syncthreads();
-    for (int i = threadIdx.x; i < kSize; i += blockDim.x) {
-        const int m = i / kRows, n = nb0 * 16 + i % kRows;
-        if (m >= M || n >= N) continue;
-        float v = 0.0f;
-        for (int q = 0; q < warps; ++q) v += part[q * kSize + i];
-        y[static_cast<int64_t>(m) * N + n] = v;
+    if (*static_cast<volatile int *>(&abort_flag)) {  // copies in flight get time to land
+        const unsigned long long t0 = globaltimer();
+        while (globaltimer() - t0 < 50000ull) {
+        }
     }
 }
 
-template <int NT, int GROUP, int RB>
-int gemv_launch(int M, int N, int K, const uint16_t *x, const uint8_t *tiled, const uint16_t *scales, float *y,
-                int warps, cudaStream_t s) {
-    const int nb = (N + 15) / 16, kt = (K + 127) / 128;
-    const size_t smem = static_cast<size_t>(warps) * 16 * RB * 8 * NT * sizeof(float);
-    gemv_w4_kernel<NT, GROUP, RB><<<(nb + RB - 1) / RB, 32 * warps, smem, s>>>(
-        M, N, K, kt, x, reinterpret_cast<const uint4 *>(tiled), scales, y);
+template <int NT, int GROUP, int RB, bool XS, int WARPS>
+int gemv_launch(W4Params p, DeviceState &ds, cudaStream_t s) {
+    static_assert(WARPS % 8 == 0, "teams of 8, 4, 2 and 1 warps share out a CTA's warps without rest");
+    const auto fn = gemv_w4_kernel<NT, GROUP, RB, XS, WARPS>;
+    const int rc = ensure_smem_optin(reinterpret_cast<const void *>(fn), kMaxSmem, ds.device,
+                                     "cudaFuncSetAttribute(4-bit product)");
+    if (rc) return rc;
+    p.groups = ((p.N + 15) / 16 + RB - 1) / RB;
+    const int grid = std::min(p.groups, ds.num_sms);
+    // The whole CTA on one group where there are no more groups than SMs, else
+    // teams of up to eight; no more warps than tiles.
+    p.team = p.groups <= ds.num_sms ? WARPS : 8;
+    while (p.team > p.kt) p.team = p.team > 8 ? 8 : p.team / 2;
+    const int x = XS ? p.x_stride * p.M : 0;
+    p.per_stage = XS ? 4 : 1;  // (x from global memory: the rest of the SM's memory caches it)
+    const auto bytes = [&] {
+        return WARPS * (kStages * p.per_stage * tile_bytes<GROUP, RB>() + part_bytes<NT, RB>()) + x;
+    };
+    while (p.per_stage > 1 && (bytes() > kMaxSmem || p.per_stage * p.team > p.kt)) p.per_stage /= 2;
+    fn<<<grid, 32 * WARPS, bytes(), s>>>(p);
     return launch_status("launch gemv_w4_kernel");
 }
 
+// x goes to shared memory where it leaves room for the ring.
+template <int NT, int GROUP, int RB, int WARPS>
+int gemv_x(W4Params p, DeviceState &ds, cudaStream_t s) {
+    p.x_stride = p.kt * 256 + 64;
+    const int64_t rest = WARPS * (kStages * tile_bytes<GROUP, RB>() + part_bytes<NT, RB>());
+    if (static_cast<int64_t>(p.x_stride) * p.M + rest <= kMaxSmem) return gemv_launch<NT, GROUP, RB, true, WARPS>(p, ds, s);
+    return gemv_launch<NT, GROUP, RB, false, WARPS>(p, ds, s);
+}
+
 template <int NT, int GROUP>
-int gemv_rows(int M, int N, int K, const uint16_t *x, const uint8_t *tiled, const uint16_t *scales, float *y,
-              const DeviceState &ds, cudaStream_t s) {
-    const int nb = (N + 15) / 16, kt = (K + 127) / 128;
-    const int warps = std::min(8, kt);
-    if (nb >= 8 * ds.num_sms) return gemv_launch<NT, GROUP, 2>(M, N, K, x, tiled, scales, y, warps, s);
-    return gemv_launch<NT, GROUP, 1>(M, N, K, x, tiled, scales, y, warps, s);
+int gemv_rows(const W4Params &p, DeviceState &ds, cudaStream_t s) {
+    if constexpr (NT == 1) {
+        return gemv_x<1, GROUP, 1, 16>(p, ds, s);
+    } else if constexpr (NT == 2) {
+        return gemv_x<2, GROUP, 1, 16>(p, ds, s);
+    } else {
+        return gemv_x<4, GROUP, 2, 8>(p, ds, s);
+    }
 }
 
 template <int NT>
-int gemv_group(int M, int N, int K, int group, const uint16_t *x, const uint8_t *tiled, const uint16_t *scales,
-               float *y, const DeviceState &ds, cudaStream_t s) {
-    if (group == 32) return gemv_rows<NT, 32>(M, N, K, x, tiled, scales, y, ds, s);
-    if (group == 64) return gemv_rows<NT, 64>(M, N, K, x, tiled, scales, y, ds, s);
-    return gemv_rows<NT, 128>(M, N, K, x, tiled, scales, y, ds, s);
+int gemv_group(const W4Params &p, int group, DeviceState &ds, cudaStream_t s) {
+    if (group == 32) return gemv_rows<NT, 32>(p, ds, s);
+    if (group == 64) return gemv_rows<NT, 64>(p, ds, s);
+    return gemv_rows<NT, 128>(p, ds, s);
 }
 
 }  // namespace
@@ -235,9 +423,10 @@ int w4_pack_launch(int N, int K, int group, const uint8_t *codes, const uint16_t
 
 int gemv_w4_launch(int M, int N, int K, int group, const uint16_t *x, const uint8_t *tiled, const uint16_t *scales,
                    float *y, DeviceState &ds, cudaStream_t s) {
-    if (M <= 8) return gemv_group<1>(M, N, K, group, x, tiled, scales, y, ds, s);
-    if (M <= 16) return gemv_group<2>(M, N, K, group, x, tiled, scales, y, ds, s);
-    return gemv_group<4>(M, N, K, group, x, tiled, scales, y, ds, s);
+    const W4Params p{M, N, K, (K + 127) / 128, 0, 0, 0, 0, x, tiled, scales, y, wait_timeout_ns(), ds.err_word};
+    if (M <= 8) return gemv_group<1>(p, group, ds, s);
+    if (M <= 16) return gemv_group<2>(p, group, ds, s);
+    return gemv_group<4>(p, group, ds, s);
 }
 
 }  // namespace isam
