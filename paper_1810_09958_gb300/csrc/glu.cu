@@ -9,14 +9,17 @@
 // PROJECT_BACK: the same product, but the epilogue reads dh and writes
 // d = [dh u act'(g) | dh act(g)] (g and u fp32; d is rounded to bf16 once, as an
 // operand of the next products).  PRODUCT: dx = d W and dW = d^T x, bf16 out,
-// A K-major or MN-major, B MN-major.
+// A K-major or MN-major, B MN-major; where the tiles are too few for the GPU the
+// sums over K are split, and a second kernel adds the fp32 parts in order.
 //
-// Bound: the tensor cores for many tokens, reading W for few.
+// Up to 32 tokens are a reading of W: glu_few_kernel streams 8 gate and 8 up rows
+// at a time through m16n8k16.
 #include <algorithm>
 
 #include "gemm_common.cuh"
 #include "internal.h"
 #include "lm_common.cuh"
+#include "mma_few.cuh"
 #include "ptx.cuh"
 
 namespace isam {
@@ -53,7 +56,9 @@ struct GluParams {
     int stages, group_m;
     int act;
     int tma_out;       // the result's rows are on 16-byte boundaries
-    uint16_t *out;     // PROJECT: h
+    int splits, kb_split;  // PRODUCT: parts of K, 64-wide blocks in each
+    float *parts;          // [splits][M][N] when there are several
+    uint16_t *out;     // h, or d
     const uint16_t *dh;
     unsigned long long timeout_ns;
     uint32_t *err;
@@ -155,7 +160,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool leader = rank == 0;
     const int pair = blockIdx.x >> 1;
     const int num_pairs = gridDim.x >> 1;
-    const int num_tiles = p.m_tiles * p.n_tiles;
+    const int num_tiles = p.m_tiles * p.n_tiles * p.splits;
+    const int tiles_split = p.m_tiles * p.n_tiles;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < ST; ++i) {
@@ -197,12 +203,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             bool ok = true;
             for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
                 int mt, nt;
-                tile_coords(tile, p, mt, nt);
+                const int split = tile / tiles_split;
+                tile_coords(tile - split * tiles_split, p, mt, nt);
+                const int kb0 = split * p.kb_split, kb1 = min(kb0 + p.kb_split, p.kb_total);
                 const int arow = mt * kPM + static_cast<int>(rank) * kHalf;
                 // Projections: this CTA's rows of W are the tile's gate rows or its up rows.
                 const int bcol = ROLE == PRODUCT ? nt * BN + static_cast<int>(rank) * kBHalf
                                                  : nt * kBHalf + (leader ? 0 : p.F);
-                for (int kb = 0; kb < p.kb_total; ++kb) {
+                for (int kb = kb0; kb < kb1; ++kb) {
                     if (!bounded_wait<true>(&empty[stage], phase ^ 1u, w, SITE_U_EMPTY)) {
                         ok = false;
                         break;
@@ -247,7 +255,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 tc_fence_after();
                 const uint32_t d = tmem_base + static_cast<uint32_t>(acc * 256);
-                for (int kb = 0; kb < p.kb_total; ++kb) {
+                const int split = tile / tiles_split;
+                const int kbs = min(p.kb_split, p.kb_total - split * p.kb_split);
+                for (int kb = 0; kb < kbs; ++kb) {
                     if (!bounded_wait<true>(&full[stage], phase, w, SITE_U_FULL)) {
                         ok = false;
                         break;
@@ -294,7 +304,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool ok = true;
         for (int tile = pair; tile < num_tiles; tile += num_pairs) {
             int mt, nt;
-            tile_coords(tile, p, mt, nt);
+            const int split = tile / tiles_split;
+            tile_coords(tile - split * tiles_split, p, mt, nt);
             const int row0 = mt * kPM + static_cast<int>(rank) * kHalf + q * 32;
             const int64_t row = row0 + lane;
             const uint32_t tb =
@@ -306,6 +317,22 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 tc_fence_after();
                 const int col0 = nt * BN;
+                if (p.splits > 1) {
+                    // This part's sums, from registers (N is a multiple of 8).
+                    float *at = p.parts + (static_cast<int64_t>(split) * p.M + row) * p.N + col0;
+#pragma unroll 1
+                    for (int j = 0; j < BN / 32; ++j) {
+                        if (row0 >= p.M || col0 + 32 * j >= p.N) break;
+                        uint32_t r[32];
+                        tmem_ld32(tb + j * 32, r);
+                        tmem_ld_wait(r);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            if (row < p.M && col0 + 32 * j + 4 * c < p.N)
+                                *reinterpret_cast<uint4 *>(at + 32 * j + 4 * c) =
+                                    make_uint4(r[4 * c], r[4 * c + 1], r[4 * c + 2], r[4 * c + 3]);
+                    }
+                } else
 #pragma unroll 1
                 for (int j = 0; j < BN / 64; ++j, buf ^= 1) {
                     if (lane == 0) bulk_wait_read<1>();  // the store of two chunks ago has left the tile
@@ -359,7 +386,21 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tmem_ld_wait(g);
                     tmem_ld_wait(u);
                     gate32<BACK>(p.act, g, u, dh, a, b);
-                    if (p.tma_out) {
+                    if (kBHalf % 64 != 0 && p.tma_out) {
+                        // A tile of 32 features: a row's 64 bytes go out by themselves.
+                        if (row < p.T) {
+                            uint16_t *at = p.out + row * (BACK ? 2 * static_cast<int64_t>(p.F) : p.F) + f;
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+                                if (f + 8 * c < p.F) {
+                                    *reinterpret_cast<uint4 *>(at + 8 * c) =
+                                        make_uint4(a[4 * c], a[4 * c + 1], a[4 * c + 2], a[4 * c + 3]);
+                                    if (BACK)
+                                        *reinterpret_cast<uint4 *>(at + p.F + 8 * c) =
+                                            make_uint4(b[4 * c], b[4 * c + 1], b[4 * c + 2], b[4 * c + 3]);
+                                }
+                        }
+                    } else if (p.tma_out) {
                         // PROJECT: two 64-column tiles in turn; PROJECT_BACK: dg in one, du in the other.
                         uint8_t *to = stg + (BACK ? 0 : buf * kStage);
                         if ((j & 1) == 0) {
@@ -452,7 +493,7 @@ int pair_launch(GluParams p, const CUtensorMap &a, const CUtensorMap &b, const C
     p.group_m = 8;
     p.timeout_ns = wait_timeout_ns();
     p.err = ds.err_word;
-    const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.n_tiles;
+    const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.n_tiles * p.splits;
     if (tiles > 0x7fffffffLL) return set_error(ISAM_ERR_UNSUPPORTED, "too many tiles for one launch");
     const int rc = ensure_smem_optin(reinterpret_cast<const void *>(fn), ds.max_smem_optin, ds.device,
                                      "cudaFuncSetAttribute(gated feed-forward)");
@@ -489,6 +530,7 @@ int project_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     p.m_tiles = tiles_of(d.T, kPM);
     p.n_tiles = tiles_of(d.F, BN / 2);
     p.kb_total = tiles_of(d.D, kBK);
+    p.splits = 1, p.kb_split = p.kb_total;
     CUtensorMap a{}, b{}, c{}, c2{};
     const uint64_t pitch = static_cast<uint64_t>(d.D) * 2, F = d.F;
     int rc;
@@ -497,6 +539,7 @@ int project_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     if (ROLE == PROJECT_BACK) {
         uint16_t *ws = static_cast<uint16_t *>(d.workspace);
         p.tma_out = 1;
+        p.out = ws;
         if ((rc = make_tmap_2d_bf16(&c, ws, F, d.T, 4 * F, 64, 32))) return rc;
         if ((rc = make_tmap_2d_bf16(&c2, ws + F, F, d.T, 4 * F, 64, 32))) return rc;
     } else if (F % 8 == 0 && reinterpret_cast<uintptr_t>(d.h) % 16 == 0) {
@@ -506,58 +549,318 @@ int project_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     return pair_launch<ROLE, BN, false, false>(p, a, b, c, c2, ds, s);
 }
 
+// 256 tokens x 128, 64 or 32 features a tile: the width with the fewest rounds of
+// tiles, where one of 32 counts as 48 (its loads are no less for the tokens).
 template <Role ROLE>
 int project(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     const int pairs = std::max(1, gemm_cluster_capacity(ds, 2));
     const int64_t mt = tiles_of(d.T, kPM);
-    if (width_cost(mt, d.F, 64, pairs) < width_cost(mt, d.F, 128, pairs)) return project_launch<ROLE, 128>(d, ds, s);
+    const int64_t c128 = width_cost(mt, d.F, 128, pairs), c64 = width_cost(mt, d.F, 64, pairs),
+                  c32 = width_cost(mt, d.F, 32, pairs) * 3 / 2;
+    if (c32 < std::min(c64, c128)) return project_launch<ROLE, 64>(d, ds, s);
+    if (c64 < c128) return project_launch<ROLE, 128>(d, ds, s);
     return project_launch<ROLE, 256>(d, ds, s);
+}
+
+// ---------------------------------------------------------------- few tokens
+constexpr int kFewTokens = 32;
+constexpr int kFewWarps = 16;
+constexpr int kTeam = 8;          // warps that share the depth of a group of features
+constexpr int kFewBlock = 2048;   // 64 deep: 8 gate and 8 up rows of 128 bytes
+constexpr int kFewSmem = 220 * 1024;
+
+struct FewParams {
+    int T, D, F;
+    int kb;        // 64-deep blocks of D
+    int groups;    // of 8 features
+    int stages, x_stride, act;
+    const uint16_t *x;
+    const uint16_t *dh;
+    uint16_t *out;  // h [T][F], or d [T][2F]
+    unsigned long long timeout_ns;
+    uint32_t *err;
+};
+
+template <int NT>
+constexpr int few_part() {  // a warp's sums, twice
+    return 2 * 16 * 8 * NT * 4;
+}
+
+__device__ __forceinline__ float act_of(int act, float a, float &da) {
+    float v;
+    if (act == ISAM_ACT_SILU)
+        activation<ISAM_ACT_SILU>(a, v, da);
+    else if (act == ISAM_ACT_GELU)
+        activation<ISAM_ACT_GELU>(a, v, da);
+    else if (act == ISAM_ACT_RELU)
+        activation<ISAM_ACT_RELU>(a, v, da);
+    else
+        activation<ISAM_ACT_SIGMOID>(a, v, da);
+    return v;
+}
+
+// Both projections of 8 features at a time by a team of eight warps, two teams a
+// CTA, one CTA an SM: rows 0-7 of an m16n8k16's A are gate rows, 8-15 the same
+// features' up rows.  W arrives by TMA (boxes of 8 rows x 64, 128-byte swizzled)
+// into a ring a warp, across groups; a warp's blocks are every eighth of D's, and
+// the team's sums meet in shared memory in the order of the warps.  x is in
+// shared memory as a whole, rows 64 bytes off a multiple of 128.  The order of k
+// inside a product does not matter: lane 4 r + t holds eight consecutive k of rows
+// r and 8 + r, and of token r, sixteen bytes each, which are two instructions'
+// operands.
+template <int NT, bool BACK>
+__global__ void __launch_bounds__(32 * kFewWarps, 1)
+    glu_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ FewParams p) {
+    constexpr int kSize = 16 * 8 * NT;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full_all[kFewWarps][8];
+    __shared__ int abort_flag;
+    uint8_t *smem =
+        reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int team = warp / kTeam, member = warp % kTeam;
+    uint8_t *ring = smem + warp * p.stages * kFewBlock;
+    float *part = reinterpret_cast<float *>(smem + kFewWarps * p.stages * kFewBlock) + team * kTeam * 2 * kSize;
+    uint8_t *xs = smem + kFewWarps * (p.stages * kFewBlock + few_part<NT>());
+    uint64_t *full = full_all[warp];
+    if (lane == 0)
+        for (int i = 0; i < p.stages; ++i) mbar_init(&full[i], 1);
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        tma_prefetch_desc(&tmW);
+    }
+    fence_mbar_init();
+    __syncthreads();
+    const WaitCtx wait{p.timeout_ns, p.err, &abort_flag};
+    const int r = lane >> 2, t = lane & 3;
+    constexpr int kTeams = kFewWarps / kTeam;
+    const int first = team * gridDim.x + blockIdx.x, stride = kTeams * gridDim.x;
+
+    int load_group = first, load_k = member, load_stage = 0;
+    const auto fetch = [&]() {  // lane 0
+        if (load_k >= p.kb) {
+            load_k = member;
+            load_group += stride;
+        }
+        if (load_group >= p.groups || load_k >= p.kb) return;
+        uint64_t *bar = &full[load_stage];
+        uint8_t *to = ring + load_stage * kFewBlock;
+        mbar_arrive_expect_tx(bar, kFewBlock);
+        tma_load_2d(&tmW, bar, to, load_k * 64, load_group * 8);
+        tma_load_2d(&tmW, bar, to + kFewBlock / 2, load_k * 64, p.F + load_group * 8);
+        load_k += kTeam;
+        load_stage = load_stage + 1 == p.stages ? 0 : load_stage + 1;
+    };
+    if (lane == 0)
+        for (int i = 0; i < p.stages; ++i) fetch();
+    {
+        // x, and zeros behind D up to whole blocks.
+        const int chunks = 8 * p.kb;  // of 16 bytes
+        for (int i = threadIdx.x; i < p.T * chunks; i += 32 * kFewWarps) {
+            const int m = i / chunks, c = i - m * chunks;
+            uint8_t *to = xs + m * p.x_stride + 16 * c;
+            if (8 * c < p.D)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)),
+                             "l"(p.x + static_cast<int64_t>(m) * p.D + 8 * c)
+                             : "memory");
+            else
+                *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+    }
+    uint32_t xa[NT];  // (lanes behind the last token read it again)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) xa[n] = smem_u32(xs) + min(8 * n + r, p.T - 1) * p.x_stride + 16 * t;
+    const uint32_t ring_at = smem_u32(ring) + 128 * r;
+    int stage = 0, half = 0;
+    uint32_t phase = 0;
+    for (int g = first; g < p.groups; g += stride, half ^= 1) {
+        float sum[NT][4] = {};
+        for (int k = member; k < p.kb; k += kTeam) {
+            bounded_wait(&full[stage], phase, wait, 0x711u);
+            const uint32_t at = ring_at + stage * kFewBlock;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t chunk = 16 * ((4 * j + t) ^ r);
+                const uint4 gate = lds16(at + chunk), up = lds16(at + kFewBlock / 2 + chunk);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint4 xv = lds16(xa[n] + 128 * k + 64 * j);
+                    const uint32_t a0[4] = {gate.x, up.x, gate.y, up.y}, a1[4] = {gate.z, up.z, gate.w, up.w};
+                    mma_16x8x16<false>(sum[n], a0, xv.x, xv.y);
+                    mma_16x8x16<false>(sum[n], a1, xv.z, xv.w);
+                }
+            }
+            __syncwarp();  // every lane has read the stage
+            if (lane == 0) fetch();
+            if (++stage == p.stages) {
+                stage = 0;
+                phase ^= 1u;
+            }
+        }
+        float *mine = part + half * kTeam * kSize;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                mine[member * kSize + (8 * n + 2 * t + (i & 1)) * 16 + r + 8 * (i >> 1)] = sum[n][i];
+        named_bar(1 + team, 32 * kTeam);
+        for (int i = 32 * member + lane; i < 8 * 8 * NT; i += 32 * kTeam) {
+            const int m = i >> 3, f = g * 8 + (i & 7);
+            if (m >= p.T || f >= p.F) continue;
+            float a = 0.0f, u = 0.0f, da;
+            for (int q = 0; q < kTeam; ++q) {
+                a += mine[q * kSize + 16 * m + (i & 7)];
+                u += mine[q * kSize + 16 * m + 8 + (i & 7)];
+            }
+            const float v = act_of(p.act, a, da);
+            bf16 *out = reinterpret_cast<bf16 *>(p.out);
+            if (BACK) {
+                const float d = __uint_as_float(static_cast<uint32_t>(p.dh[static_cast<int64_t>(m) * p.F + f]) << 16);
+                bf16 *row = out + static_cast<int64_t>(m) * 2 * p.F + f;
+                row[0] = from_f32<bf16>(d * u * da);
+                row[p.F] = from_f32<bf16>(d * v);
+            } else {
+                out[static_cast<int64_t>(m) * p.F + f] = from_f32<bf16>(v * u);
+            }
+        }
+    }
+    if (*static_cast<volatile int *>(&abort_flag)) {  // copies in flight get time to land
+        const unsigned long long t0 = globaltimer();
+        while (globaltimer() - t0 < 50000ull) {
+        }
+    }
+}
+
+// Stages of a warp's ring beside x, 0 where x does not fit.
+template <int NT>
+int few_stages(int T, int D) {
+    const int64_t x = static_cast<int64_t>(tiles_of(D, kBK) * 128 + 64) * T;
+    const int64_t left = kFewSmem - 1024 - x - kFewWarps * few_part<NT>();
+    const int64_t st = left / (kFewWarps * kFewBlock);
+    return st < 2 ? 0 : static_cast<int>(std::min<int64_t>(st, 4));
+}
+
+template <int NT, bool BACK>
+int few_launch(const GluDesc &d, int stages, DeviceState &ds, cudaStream_t s) {
+    const auto fn = glu_few_kernel<NT, BACK>;
+    FewParams p{};
+    p.T = d.T, p.D = d.D, p.F = d.F, p.act = d.act;
+    p.kb = tiles_of(d.D, kBK);
+    p.groups = tiles_of(d.F, 8);
+    p.stages = stages;
+    p.x_stride = p.kb * 128 + 64;
+    p.x = d.x, p.dh = d.dh, p.out = BACK ? static_cast<uint16_t *>(d.workspace) : d.h;
+    p.timeout_ns = wait_timeout_ns();
+    p.err = ds.err_word;
+    CUtensorMap w;
+    int rc = make_tmap_2d_bf16(&w, d.W, d.D, 2 * static_cast<uint64_t>(d.F), static_cast<uint64_t>(d.D) * 2, 64, 8);
+    if (rc) return rc;
+    if ((rc = ensure_smem_optin(reinterpret_cast<const void *>(fn), kFewSmem, ds.device,
+                                "cudaFuncSetAttribute(gated feed-forward, few tokens)")))
+        return rc;
+    const size_t smem = 1024 + kFewWarps * (stages * kFewBlock + few_part<NT>()) + static_cast<size_t>(p.x_stride) * d.T;
+    fn<<<std::min(p.groups, ds.num_sms), 32 * kFewWarps, smem, s>>>(w, p);
+    return launch_status("launch glu_few_kernel");
+}
+
+// The projections and their gate: h, or d into the workspace.
+template <Role ROLE>
+int gated(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
+    constexpr bool BACK = ROLE == PROJECT_BACK;
+    int st;
+    if (d.T <= 8 && (st = few_stages<1>(d.T, d.D))) return few_launch<1, BACK>(d, st, ds, s);
+    if (d.T > 8 && d.T <= 16 && (st = few_stages<2>(d.T, d.D))) return few_launch<2, BACK>(d, st, ds, s);
+    if (d.T > 16 && d.T <= kFewTokens && (st = few_stages<4>(d.T, d.D))) return few_launch<4, BACK>(d, st, ds, s);
+    return project<ROLE>(d, ds, s);
+}
+
+// ---------------------------------------------------------------- products
+constexpr int kPairs = 76;  // of a GB300, for the workspace's size
+constexpr int kMaxSplits = 16;
+
+// Parts of K for a product of few tiles: as many as leave every pair a tile, each
+// at least eight blocks deep.
+int product_splits(int64_t M, int N, int64_t K) {
+    const int64_t tiles = static_cast<int64_t>(tiles_of(M, kPM)) * tiles_of(N, 128);
+    const int64_t n = std::min<int64_t>({kPairs / tiles, kMaxSplits, tiles_of(K, kBK) / 8});
+    return static_cast<int>(std::max<int64_t>(n, 1));
+}
+
+constexpr int kSumThreads = 256;
+__global__ void __launch_bounds__(kSumThreads) glu_sum_kernel(int64_t quads, int splits, const float4 *parts, uint2 *out) {
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kSumThreads + threadIdx.x;
+    if (i >= quads) return;
+    float4 v = parts[i];
+    for (int q = 1; q < splits; ++q) {
+        const float4 w = parts[q * quads + i];
+        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    }
+    out[i] = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
 }
 
 // C (M x N, bf16) = op(A) B with B K x N; A_MN: A stored K x M.
 template <bool A_MN, int BN>
-int product_launch(int64_t M, int N, int64_t K, const uint16_t *A, const uint16_t *B, uint16_t *C, DeviceState &ds,
-                   cudaStream_t s) {
+int product_launch(int64_t M, int N, int64_t K, const uint16_t *A, const uint16_t *B, uint16_t *C, int splits,
+                   float *parts, DeviceState &ds, cudaStream_t s) {
     GluParams p{};
     p.M = M, p.N = N;
     p.m_tiles = tiles_of(M, kPM);
     p.n_tiles = tiles_of(N, BN);
     p.kb_total = tiles_of(K, kBK);
+    p.kb_split = tiles_of(p.kb_total, splits);
+    p.splits = tiles_of(p.kb_total, p.kb_split);  // no empty part
+    p.parts = parts;
     CUtensorMap a{}, b{}, c{};
     int rc;
     rc = A_MN ? make_tmap_2d_bf16(&a, A, M, K, M * 2, 64, kBK) : make_tmap_2d_bf16(&a, A, K, M, K * 2, 64, kHalf);
     if (rc) return rc;
     if ((rc = make_tmap_2d_bf16(&b, B, N, K, static_cast<uint64_t>(N) * 2, 64, kBK))) return rc;
     if ((rc = make_tmap_2d_bf16(&c, C, N, M, static_cast<uint64_t>(N) * 2, 64, 32))) return rc;
-    return pair_launch<PRODUCT, BN, A_MN, true>(p, a, b, c, c, ds, s);
+    if ((rc = pair_launch<PRODUCT, BN, A_MN, true>(p, a, b, c, c, ds, s))) return rc;
+    if (p.splits == 1) return ISAM_OK;
+    const int64_t quads = M * N / 4;
+    glu_sum_kernel<<<static_cast<unsigned>((quads + kSumThreads - 1) / kSumThreads), kSumThreads, 0, s>>>(
+        quads, p.splits, reinterpret_cast<const float4 *>(parts), reinterpret_cast<uint2 *>(C));
+    return launch_status("launch glu_sum_kernel");
 }
 
 template <bool A_MN>
-int product(int64_t M, int N, int64_t K, const uint16_t *A, const uint16_t *B, uint16_t *C, DeviceState &ds,
-            cudaStream_t s) {
+int product(int64_t M, int N, int64_t K, const uint16_t *A, const uint16_t *B, uint16_t *C, float *parts,
+            DeviceState &ds, cudaStream_t s) {
     const int pairs = std::max(1, gemm_cluster_capacity(ds, 2));
     const int64_t mt = tiles_of(M, kPM);
+    const int splits = parts ? product_splits(M, N, K) : 1;
+    if (splits > 1) return product_launch<A_MN, 128>(M, N, K, A, B, C, splits, parts, ds, s);
     const int64_t c256 = width_cost(mt, N, 256, pairs), c192 = width_cost(mt, N, 192, pairs),
                   c128 = width_cost(mt, N, 128, pairs);
-    if (c128 < std::min(c192, c256)) return product_launch<A_MN, 128>(M, N, K, A, B, C, ds, s);
-    if (c192 < c256) return product_launch<A_MN, 192>(M, N, K, A, B, C, ds, s);
-    return product_launch<A_MN, 256>(M, N, K, A, B, C, ds, s);
+    if (c128 < std::min(c192, c256)) return product_launch<A_MN, 128>(M, N, K, A, B, C, 1, nullptr, ds, s);
+    if (c192 < c256) return product_launch<A_MN, 192>(M, N, K, A, B, C, 1, nullptr, ds, s);
+    return product_launch<A_MN, 256>(M, N, K, A, B, C, 1, nullptr, ds, s);
 }
+
+// Bytes of d in the workspace, up to where the parts of dx follow.
+size_t d_bytes(int T, int F) { return (static_cast<size_t>(T) * F * 4 + 255) / 256 * 256; }
 
 }  // namespace
 
-int glu_forward_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) { return project<PROJECT>(d, ds, s); }
+int glu_forward_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) { return gated<PROJECT>(d, ds, s); }
 
-size_t glu_backward_workspace(int T, int D, int F) { return static_cast<size_t>(T) * F * 4; }
+size_t glu_backward_workspace(int T, int D, int F) {
+    const int splits = product_splits(T, D, 2 * static_cast<int64_t>(F));
+    return d_bytes(T, F) + (splits > 1 ? static_cast<size_t>(splits) * T * D * 4 : 0);
+}
 
 int glu_backward_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     if (!d.dx && !d.dW) return ISAM_OK;
-    int rc = project<PROJECT_BACK>(d, ds, s);
+    int rc = gated<PROJECT_BACK>(d, ds, s);
     if (rc) return rc;
     const uint16_t *ws = static_cast<const uint16_t *>(d.workspace);
+    float *parts = reinterpret_cast<float *>(static_cast<uint8_t *>(d.workspace) + d_bytes(d.T, d.F));
     const int64_t F2 = 2 * static_cast<int64_t>(d.F);
-    if (d.dx && (rc = product<false>(d.T, d.D, F2, ws, d.W, d.dx, ds, s))) return rc;
-    if (d.dW && (rc = product<true>(F2, d.D, d.T, ws, d.x, d.dW, ds, s))) return rc;
+    if (d.dx && (rc = product<false>(d.T, d.D, F2, ws, d.W, d.dx, parts, ds, s))) return rc;
+    if (d.dW && (rc = product<true>(F2, d.D, d.T, ws, d.x, d.dW, nullptr, ds, s))) return rc;
     return ISAM_OK;
 }
 

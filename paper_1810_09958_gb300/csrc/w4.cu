@@ -4,6 +4,7 @@
 
 #include "internal.h"
 #include "lm_common.cuh"
+#include "mma_few.cuh"
 #include "ptx.cuh"
 
 namespace isam {
@@ -59,24 +60,6 @@ __device__ __forceinline__ void copy(uint32_t to, const void *from, uint32_t byt
                  : "memory");
 }
 
-// c += a b (or c = a b) on 16 rows x 16 k x 8 tokens.
-template <bool FIRST>
-__device__ __forceinline__ void mma_16x8x16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    if (FIRST) {
-        asm volatile(
-            "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-            "{%10, %10, %10, %10};"
-            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
-    } else {
-        asm volatile(
-            "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-            "{%0, %1, %2, %3};"
-            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-}
-
 // The word's eight codes as four pairs of bf16 (q - 8) / 8, exactly, in the
 // order of k.  A code in the low four bits of a half is or-ed into the mantissa
 // of 16, where it counts eighths, and 17 is subtracted.  One in the next four
@@ -90,13 +73,6 @@ __device__ __forceinline__ void dequant(uint32_t w, uint32_t (&v)[4]) {
         asm("fma.rn.bf16x2 %0, %0, %1, %2;" : "+r"(v[i]) : "r"(0x3F803F80u), "r"(0xC188C188u));
         asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[i + 1]) : "r"(w & 0x00F000F0u), "r"(0x7E807E80u), "r"(0xBF80BF80u));
     }
-}
-
-// Shared-memory loads by 32-bit address.
-__device__ __forceinline__ uint4 lds16(uint32_t at) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-    return v;
 }
 
 // The scales of a row in one tile: 128 / GROUP bf16.
