@@ -122,10 +122,17 @@ def _dev(t, dtype, numel, name):
         raise ValueError(f"{name} is not on the current device")
 
 
+_raw_stream = None
+
+
 def _use_current_stream(lib):
+    global _raw_stream
     import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 3 us cheaper than building a Stream object
-    lib.isam_set_stream(raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream)
+    if _raw_stream is None:
+        # Where torch has it, 3 us cheaper than building a Stream object.
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _raw_stream = raw if raw else lambda _: torch.cuda.current_stream().cuda_stream
+    lib.isam_set_stream(_raw_stream(torch.cuda.current_device()))
 
 
 def sync() -> None:
@@ -376,19 +383,50 @@ def gru_plan(layers, batch, hidden, reset_before=False, num_sms=None, smem_optin
     return dict(zip(_GRU_PLAN_KEYS, list(out)))
 
 
-def _elem_type(t, name):
-    """ISAM_F32 or ISAM_BF16 of a tensor."""
-    import torch
-    if t.dtype == torch.float32:
-        return 0
-    if t.dtype == torch.bfloat16:
-        return 1
-    raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+# The calls below run for single tokens, where a few microseconds of checks count:
+# one look at the current device and stream a call, and the checks of a tensor
+# in one expression that falls back to _dev for its message.
+
+class _Call:
+    """The library, torch, and the current device and stream set for one call."""
+
+    __slots__ = ("lib", "torch", "device")
+
+    def __init__(self):
+        global _torch
+        if _torch is None:
+            import torch
+            _torch = torch
+        self.torch = _torch
+        self.lib = _lib if _lib is not None else load()
+        self.device = _torch.cuda.current_device() if _torch.cuda.is_initialized() else -1
+
+    def ptr(self, t, dtype, numel, name):
+        """The address of a tensor that is what it has to be."""
+        if not (t.is_cuda and t.dtype == dtype and t.numel() == numel and t.is_contiguous()
+                and t.get_device() == self.device):
+            _dev(t, dtype, numel, name)
+        return t.data_ptr()
+
+    def opt(self, t, dtype, numel, name):
+        return None if t is None else self.ptr(t, dtype, numel, name)
+
+    def kind(self, t, name):
+        """ISAM_F32 or ISAM_BF16 of a tensor."""
+        if t.dtype == self.torch.bfloat16:
+            return 1
+        if t.dtype == self.torch.float32:
+            return 0
+        raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+
+    def run(self, fn, *args):
+        _use_current_stream(self.lib)
+        rc = fn(*args)
+        if rc != ISAM_OK:
+            check(rc)
 
 
-def _opt(t, dtype, numel, name):
-    if t is not None:
-        _dev(t, dtype, numel, name)
+_torch = None
 
 
 def glr_forward(T, batch, hidden, g, h0, lengths, h_out, h_last=None) -> None:
@@ -396,52 +434,37 @@ def glr_forward(T, batch, hidden, g, h0, lengths, h_out, h_last=None) -> None:
     the first and n the second half of g's rows (g [T,batch,2H] and h_out
     [T,batch,H] fp32 or bf16; h0, h_last [batch,H] fp32 or None; lengths
     [batch] int32 or None)."""
-    import torch
-    lib = load()
-    gt, ht = _elem_type(g, "g"), _elem_type(h_out, "h_out")
-    _dev(g, g.dtype, T * batch * 2 * hidden, "g")
-    _opt(h0, torch.float32, batch * hidden, "h0")
-    _opt(lengths, torch.int32, batch, "lengths")
-    _dev(h_out, h_out.dtype, T * batch * hidden, "h_out")
-    _opt(h_last, torch.float32, batch * hidden, "h_last")
-    _use_current_stream(lib)
-    check(lib.isam_glr_forward(T, batch, hidden, gt, _ptr(g), _ptr(h0), _ptr(lengths), ht, _ptr(h_out), _ptr(h_last)))
+    c = _Call()
+    f32, n = c.torch.float32, T * batch * hidden
+    gt, ht = c.kind(g, "g"), c.kind(h_out, "h_out")
+    c.run(c.lib.isam_glr_forward, T, batch, hidden, gt, c.ptr(g, g.dtype, 2 * n, "g"),
+          c.opt(h0, f32, batch * hidden, "h0"), c.opt(lengths, c.torch.int32, batch, "lengths"), ht,
+          c.ptr(h_out, h_out.dtype, n, "h_out"), c.opt(h_last, f32, batch * hidden, "h_last"))
 
 
 def glr_backward(T, batch, hidden, g, h0, lengths, h_out, dh_out, dh_last, dg, dh0=None) -> None:
     """isam_glr_backward: gradients dg (g's shape and type) and dh0 [batch,H]
     fp32 (or None) of glr_forward from dh_out (h_out's shape and type, or None)
     and dh_last [batch,H] fp32 (or None)."""
-    import torch
-    lib = load()
-    gt, ht = _elem_type(g, "g"), _elem_type(h_out, "h_out")
-    _dev(g, g.dtype, T * batch * 2 * hidden, "g")
-    _opt(h0, torch.float32, batch * hidden, "h0")
-    _opt(lengths, torch.int32, batch, "lengths")
-    _dev(h_out, h_out.dtype, T * batch * hidden, "h_out")
-    _opt(dh_out, h_out.dtype, T * batch * hidden, "dh_out")
-    _opt(dh_last, torch.float32, batch * hidden, "dh_last")
-    _dev(dg, g.dtype, T * batch * 2 * hidden, "dg")
-    _opt(dh0, torch.float32, batch * hidden, "dh0")
-    _use_current_stream(lib)
-    check(lib.isam_glr_backward(T, batch, hidden, gt, _ptr(g), _ptr(h0), _ptr(lengths), ht, _ptr(h_out), _ptr(dh_out),
-                                _ptr(dh_last), _ptr(dg), _ptr(dh0)))
+    c = _Call()
+    f32, n, edge = c.torch.float32, T * batch * hidden, batch * hidden
+    gt, ht = c.kind(g, "g"), c.kind(h_out, "h_out")
+    c.run(c.lib.isam_glr_backward, T, batch, hidden, gt, c.ptr(g, g.dtype, 2 * n, "g"), c.opt(h0, f32, edge, "h0"),
+          c.opt(lengths, c.torch.int32, batch, "lengths"), ht, c.ptr(h_out, h_out.dtype, n, "h_out"),
+          c.opt(dh_out, h_out.dtype, n, "dh_out"), c.opt(dh_last, f32, edge, "dh_last"),
+          c.ptr(dg, g.dtype, 2 * n, "dg"), c.opt(dh0, f32, edge, "dh0"))
 
 
 def glr_step(batch, hidden, slots, g, slot_ids, state, new_state, h) -> None:
     """isam_glr_step: one token for `batch` sequences whose fp32 states are rows
     slot_ids (int32, or None for row b) of state [slots,H]; new_state may be
     state; h [batch,H] fp32 or bf16."""
-    import torch
-    lib = load()
-    gt, ht = _elem_type(g, "g"), _elem_type(h, "h")
-    _dev(g, g.dtype, batch * 2 * hidden, "g")
-    _opt(slot_ids, torch.int32, batch, "slot_ids")
-    _dev(state, torch.float32, slots * hidden, "state")
-    _dev(new_state, torch.float32, slots * hidden, "new_state")
-    _dev(h, h.dtype, batch * hidden, "h")
-    _use_current_stream(lib)
-    check(lib.isam_glr_step(batch, hidden, slots, gt, _ptr(g), _ptr(slot_ids), _ptr(state), _ptr(new_state), ht, _ptr(h)))
+    c = _Call()
+    f32, n = c.torch.float32, batch * hidden
+    gt, ht = c.kind(g, "g"), c.kind(h, "h")
+    c.run(c.lib.isam_glr_step, batch, hidden, slots, gt, c.ptr(g, g.dtype, 2 * n, "g"),
+          c.opt(slot_ids, c.torch.int32, batch, "slot_ids"), c.ptr(state, f32, slots * hidden, "state"),
+          c.ptr(new_state, f32, slots * hidden, "new_state"), ht, c.ptr(h, h.dtype, n, "h"))
 
 
 ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
@@ -456,14 +479,10 @@ def _act_code(act):
 def glu_forward(T, D, F, act, x, W, h) -> None:
     """isam_glu_forward: h = act(x Wg^T) * (x Wu^T) (x [T,D], W [2F,D] with the
     gate rows first, h [T,F], all bf16; act "silu", "gelu", "relu" or "sigmoid")."""
-    import torch
-    lib = load()
-    code = _act_code(act)
-    _dev(x, torch.bfloat16, T * D, "x")
-    _dev(W, torch.bfloat16, 2 * F * D, "W")
-    _dev(h, torch.bfloat16, T * F, "h")
-    _use_current_stream(lib)
-    check(lib.isam_glu_forward(T, D, F, code, _ptr(x), _ptr(W), _ptr(h)))
+    code, c = _act_code(act), _Call()
+    bf16 = c.torch.bfloat16
+    c.run(c.lib.isam_glu_forward, T, D, F, code, c.ptr(x, bf16, T * D, "x"), c.ptr(W, bf16, 2 * F * D, "W"),
+          c.ptr(h, bf16, T * F, "h"))
 
 
 def glu_backward_workspace(T, D, F) -> int:
@@ -478,22 +497,17 @@ def glu_backward(T, D, F, act, x, W, dh, dx, dW, workspace=None) -> None:
     glu_forward from dh [T,F]; workspace a uint8 tensor of
     glu_backward_workspace bytes, or None to take one from torch's allocator
     on the current stream."""
-    import torch
-    lib = load()
-    code = _act_code(act)
-    _dev(x, torch.bfloat16, T * D, "x")
-    _dev(W, torch.bfloat16, 2 * F * D, "W")
-    _dev(dh, torch.bfloat16, T * F, "dh")
-    _opt(dx, torch.bfloat16, T * D, "dx")
-    _opt(dW, torch.bfloat16, 2 * F * D, "dW")
+    code, c = _act_code(act), _Call()
+    bf16, u8 = c.torch.bfloat16, c.torch.uint8
+    args = (c.ptr(x, bf16, T * D, "x"), c.ptr(W, bf16, 2 * F * D, "W"), c.ptr(dh, bf16, T * F, "dh"))
+    out = (c.opt(dx, bf16, T * D, "dx"), c.opt(dW, bf16, 2 * F * D, "dW"))
     need = glu_backward_workspace(T, D, F)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-    _dev(workspace, torch.uint8, workspace.numel(), "workspace")
+        workspace = c.torch.empty(need, dtype=u8, device=x.device)
+    ws = c.ptr(workspace, u8, workspace.numel(), "workspace")
     if workspace.numel() < need:
         raise ValueError(f"workspace has {workspace.numel()} bytes, {need} are needed")
-    _use_current_stream(lib)
-    check(lib.isam_glu_backward(T, D, F, code, _ptr(x), _ptr(W), _ptr(dh), _ptr(workspace), _ptr(dx), _ptr(dW)))
+    c.run(c.lib.isam_glu_backward, T, D, F, code, *args, ws, *out)
 
 
 def w4_tiled_bytes(N, K) -> int:
@@ -510,28 +524,24 @@ def w4_pack(N, K, group, codes, scales, tiled, tiled_scales) -> None:
     """isam_w4_pack: codes [N,K/2] (uint8, even k in the low half) and scales
     [N,ceil(K/group)] (bf16) into the tiled order gemv_w4 reads (uint8
     w4_tiled_bytes, bf16 w4_tiled_scales)."""
-    import torch
-    lib = load()
     if group not in (32, 64, 128):
         raise ValueError(f"group must be 32, 64 or 128, got {group}")
-    _dev(codes, torch.uint8, N * (K // 2), "codes")
-    _dev(scales, torch.bfloat16, N * ((K + group - 1) // group), "scales")
-    _dev(tiled, torch.uint8, w4_tiled_bytes(N, K), "tiled")
-    _dev(tiled_scales, torch.bfloat16, w4_tiled_scales(N, K, group), "tiled_scales")
-    _use_current_stream(lib)
-    check(lib.isam_w4_pack(N, K, group, _ptr(codes), _ptr(scales), _ptr(tiled), _ptr(tiled_scales)))
+    c = _Call()
+    bf16, u8 = c.torch.bfloat16, c.torch.uint8
+    c.run(c.lib.isam_w4_pack, N, K, group, c.ptr(codes, u8, N * (K // 2), "codes"),
+          c.ptr(scales, bf16, N * ((K + group - 1) // group), "scales"),
+          c.ptr(tiled, u8, w4_tiled_bytes(N, K), "tiled"),
+          c.ptr(tiled_scales, bf16, w4_tiled_scales(N, K, group), "tiled_scales"))
 
 
 def gemv_w4(M, N, K, group, x, tiled, tiled_scales, y) -> None:
     """isam_gemv_w4: y [M,N] fp32 = x [M,K] bf16 times 4-bit weights in
     w4_pack's order, M <= 32."""
-    import torch
-    lib = load()
     if group not in (32, 64, 128):
         raise ValueError(f"group must be 32, 64 or 128, got {group}")
-    _dev(x, torch.bfloat16, M * K, "x")
-    _dev(tiled, torch.uint8, w4_tiled_bytes(N, K), "tiled")
-    _dev(tiled_scales, torch.bfloat16, w4_tiled_scales(N, K, group), "tiled_scales")
-    _dev(y, torch.float32, M * N, "y")
-    _use_current_stream(lib)
-    check(lib.isam_gemv_w4(M, N, K, group, _ptr(x), _ptr(tiled), _ptr(tiled_scales), _ptr(y)))
+    c = _Call()
+    bf16 = c.torch.bfloat16
+    c.run(c.lib.isam_gemv_w4, M, N, K, group, c.ptr(x, bf16, M * K, "x"),
+          c.ptr(tiled, c.torch.uint8, w4_tiled_bytes(N, K), "tiled"),
+          c.ptr(tiled_scales, bf16, w4_tiled_scales(N, K, group), "tiled_scales"),
+          c.ptr(y, c.torch.float32, M * N, "y"))
