@@ -9,8 +9,11 @@
 // PROJECT_BACK: the same product, but the epilogue reads dh and writes
 // d = [dh u act'(g) | dh act(g)] (g and u fp32; d is rounded to bf16 once, as an
 // operand of the next products).  PRODUCT: dx = d W and dW = d^T x, bf16 out,
-// A K-major or MN-major, B MN-major; where the tiles are too few for the GPU the
-// sums over K are split, and a second kernel adds the fp32 parts in order.
+// A K-major or MN-major, B MN-major; the tiles that a last round would leave most
+// pairs without are split over K, and a second kernel adds their fp32 parts in
+// order (4096 x 2560 x 15360, 160 tiles on 76 pairs).  PRODUCT_FEW: dx for up to 128
+// tokens with the roles changed, (W^T d^T), so that a stage is W and not empty
+// token rows.
 //
 // Up to 32 tokens are a reading of W: glu_few_kernel streams 8 gate and 8 up rows
 // at a time through m16n8k16.
@@ -26,7 +29,7 @@ namespace isam {
 
 namespace {
 
-enum Role { PROJECT, PROJECT_BACK, PRODUCT };
+enum Role { PROJECT, PROJECT_BACK, PRODUCT, PRODUCT_FEW };
 
 constexpr int kPM = 256;   // tile rows of a pair
 constexpr int kHalf = 128; // rows of A in each CTA
@@ -37,6 +40,7 @@ constexpr int kStage = 4096;                  // 32 rows x 64 bf16 of a result, 
 constexpr int kEpiBytes = 4 * 2 * kStage;     // two a warp
 constexpr uint32_t kTmemCols = 512;           // two accumulators of up to 256 columns
 constexpr uint16_t kBoth = 0x3;
+constexpr int kGroupM = 8;  // tiles of a rasterisation group
 
 enum : uint32_t {
     SITE_U_EMPTY = 0x701,
@@ -56,8 +60,11 @@ struct GluParams {
     int stages, group_m;
     int act;
     int tma_out;       // the result's rows are on 16-byte boundaries
-    int splits, kb_split;  // PRODUCT: parts of K, 64-wide blocks in each
-    float *parts;          // [splits][M][N] when there are several
+    // Products: tiles from main_tiles on are computed in `splits` parts of kb_split
+    // 64-wide blocks of K, to parts[part][tile - main_tiles][256][BN]; transposed
+    // ones all are, to parts[part][N][M].
+    int main_tiles, splits, kb_split;
+    float *parts;
     uint16_t *out;     // h, or d
     const uint16_t *dh;
     unsigned long long timeout_ns;
@@ -160,8 +167,26 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool leader = rank == 0;
     const int pair = blockIdx.x >> 1;
     const int num_pairs = gridDim.x >> 1;
-    const int num_tiles = p.m_tiles * p.n_tiles * p.splits;
-    const int tiles_split = p.m_tiles * p.n_tiles;
+    const int split_tiles = p.m_tiles * p.n_tiles - p.main_tiles;
+    const int num_tiles = p.main_tiles + split_tiles * p.splits;
+    // Tile i of the list: its place, its blocks of K, and its part (-1: the whole).
+    struct Item {
+        int mt, nt, kb0, kb1, part, local;
+    };
+    const auto item = [&](int i) {
+        Item t;
+        t.part = -1, t.local = 0, t.kb0 = 0, t.kb1 = p.kb_total;
+        int tile = i;
+        if ((ROLE == PRODUCT || ROLE == PRODUCT_FEW) && i >= p.main_tiles) {
+            t.part = (i - p.main_tiles) / split_tiles;
+            t.local = (i - p.main_tiles) - t.part * split_tiles;
+            t.kb0 = t.part * p.kb_split;
+            t.kb1 = min(t.kb0 + p.kb_split, p.kb_total);
+            tile = p.main_tiles + t.local;
+        }
+        tile_coords(tile, p, t.mt, t.nt);
+        return t;
+    };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < ST; ++i) {
@@ -202,15 +227,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t phase = 0;
             bool ok = true;
             for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
-                int mt, nt;
-                const int split = tile / tiles_split;
-                tile_coords(tile - split * tiles_split, p, mt, nt);
-                const int kb0 = split * p.kb_split, kb1 = min(kb0 + p.kb_split, p.kb_total);
-                const int arow = mt * kPM + static_cast<int>(rank) * kHalf;
+                const Item it = item(tile);
+                const int nt = it.nt;
+                const int arow = it.mt * kPM + static_cast<int>(rank) * kHalf;
                 // Projections: this CTA's rows of W are the tile's gate rows or its up rows.
-                const int bcol = ROLE == PRODUCT ? nt * BN + static_cast<int>(rank) * kBHalf
+                const int bcol = ROLE == PRODUCT || ROLE == PRODUCT_FEW ? nt * BN + static_cast<int>(rank) * kBHalf
                                                  : nt * kBHalf + (leader ? 0 : p.F);
-                for (int kb = kb0; kb < kb1; ++kb) {
+                for (int kb = it.kb0; kb < it.kb1; ++kb) {
                     if (!bounded_wait<true>(&empty[stage], phase ^ 1u, w, SITE_U_EMPTY)) {
                         ok = false;
                         break;
@@ -255,8 +278,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 tc_fence_after();
                 const uint32_t d = tmem_base + static_cast<uint32_t>(acc * 256);
-                const int split = tile / tiles_split;
-                const int kbs = min(p.kb_split, p.kb_total - split * p.kb_split);
+                const Item it = item(tile);
+                const int kbs = it.kb1 - it.kb0;
                 for (int kb = 0; kb < kbs; ++kb) {
                     if (!bounded_wait<true>(&full[stage], phase, w, SITE_U_FULL)) {
                         ok = false;
@@ -303,23 +326,42 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t acc_phase = 0;
         bool ok = true;
         for (int tile = pair; tile < num_tiles; tile += num_pairs) {
-            int mt, nt;
-            const int split = tile / tiles_split;
-            tile_coords(tile - split * tiles_split, p, mt, nt);
-            const int row0 = mt * kPM + static_cast<int>(rank) * kHalf + q * 32;
+            const Item it = item(tile);
+            const int nt = it.nt;
+            const int row0 = it.mt * kPM + static_cast<int>(rank) * kHalf + q * 32;
             const int64_t row = row0 + lane;
             const uint32_t tb =
                 tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * 256);
-            if constexpr (ROLE == PRODUCT) {
+            if constexpr (ROLE == PRODUCT_FEW) {
+                if (!warp_wait<true>(&tfull[acc], acc_phase, w, SITE_U_TFULL)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                // Lanes are columns of dx, TMEM columns its tokens: 128 bytes a token and warp.
+                float *at = p.parts + static_cast<int64_t>(it.part) * p.N * p.M + row;
+#pragma unroll 1
+                for (int j = 0; j < BN / 32; ++j) {
+                    const int t0 = nt * BN + 32 * j;
+                    if (row0 >= p.M || t0 >= p.N) break;
+                    uint32_t r[32];
+                    tmem_ld32(tb + j * 32, r);
+                    tmem_ld_wait(r);
+#pragma unroll
+                    for (int c = 0; c < 32; ++c)
+                        if (row < p.M && t0 + c < p.N) at[(t0 + c) * p.M] = __uint_as_float(r[c]);
+                }
+            } else if constexpr (ROLE == PRODUCT) {
                 if (!warp_wait<true>(&tfull[acc], acc_phase, w, SITE_U_TFULL)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
                 const int col0 = nt * BN;
-                if (p.splits > 1) {
+                if (it.part >= 0) {
                     // This part's sums, from registers (N is a multiple of 8).
-                    float *at = p.parts + (static_cast<int64_t>(split) * p.M + row) * p.N + col0;
+                    float *at = p.parts + (static_cast<int64_t>(it.part) * split_tiles + it.local) * kPM * BN +
+                                (row - it.mt * kPM) * BN;
 #pragma unroll 1
                     for (int j = 0; j < BN / 32; ++j) {
                         if (row0 >= p.M || col0 + 32 * j >= p.N) break;
@@ -490,11 +532,12 @@ int pair_launch(GluParams p, const CUtensorMap &a, const CUtensorMap &b, const C
     int st = 8;
     while (st > 2 && pair_smem(st, bstage) > static_cast<size_t>(ds.max_smem_optin)) --st;
     p.stages = st;
-    p.group_m = 8;
+    p.group_m = kGroupM;
     p.timeout_ns = wait_timeout_ns();
     p.err = ds.err_word;
-    const int64_t tiles = static_cast<int64_t>(p.m_tiles) * p.n_tiles * p.splits;
-    if (tiles > 0x7fffffffLL) return set_error(ISAM_ERR_UNSUPPORTED, "too many tiles for one launch");
+    const int64_t whole = static_cast<int64_t>(p.m_tiles) * p.n_tiles;
+    const int64_t tiles = p.main_tiles + (whole - p.main_tiles) * p.splits;
+    if (whole > 0x3fffffffLL || tiles > 0x7fffffffLL) return set_error(ISAM_ERR_UNSUPPORTED, "too many tiles for one launch");
     const int rc = ensure_smem_optin(reinterpret_cast<const void *>(fn), ds.max_smem_optin, ds.device,
                                      "cudaFuncSetAttribute(gated feed-forward)");
     if (rc) return rc;
@@ -518,11 +561,6 @@ int pair_launch(GluParams p, const CUtensorMap &a, const CUtensorMap &b, const C
 
 int tiles_of(int64_t n, int tile) { return static_cast<int>((n + tile - 1) / tile); }
 
-// Rounds of tiles over the pairs, in columns: what a tile width costs.
-int64_t width_cost(int64_t m_tiles, int64_t n, int width, int pairs) {
-    return (m_tiles * tiles_of(n, width) + pairs - 1) / pairs * width;
-}
-
 template <Role ROLE, int BN>
 int project_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     GluParams p{};
@@ -530,7 +568,7 @@ int project_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     p.m_tiles = tiles_of(d.T, kPM);
     p.n_tiles = tiles_of(d.F, BN / 2);
     p.kb_total = tiles_of(d.D, kBK);
-    p.splits = 1, p.kb_split = p.kb_total;
+    p.splits = 1, p.kb_split = p.kb_total, p.main_tiles = p.m_tiles * p.n_tiles;
     CUtensorMap a{}, b{}, c{}, c2{};
     const uint64_t pitch = static_cast<uint64_t>(d.D) * 2, F = d.F;
     int rc;
@@ -549,16 +587,17 @@ int project_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     return pair_launch<ROLE, BN, false, false>(p, a, b, c, c2, ds, s);
 }
 
-// 256 tokens x 128, 64 or 32 features a tile: the width with the fewest rounds of
-// tiles, where one of 32 counts as 48 (its loads are no less for the tokens).
+// 256 tokens x 128, 64 or 32 features a tile.  A round of tiles takes much the
+// same time at every width (0.31 us a 64-wide block of D), so narrower tiles are
+// taken only where all of them are one round.  Measured, us at 32 / 64 / 128
+// features: 100 x 4096 x 512 21.7 / 22.4 / 23.4, 200 x 1760 x 4096 21.0 / 13.8 /
+// 14.5, 2000 x 2560 x 7680 311 / 163 / 94.
 template <Role ROLE>
 int project(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     const int pairs = std::max(1, gemm_cluster_capacity(ds, 2));
     const int64_t mt = tiles_of(d.T, kPM);
-    const int64_t c128 = width_cost(mt, d.F, 128, pairs), c64 = width_cost(mt, d.F, 64, pairs),
-                  c32 = width_cost(mt, d.F, 32, pairs) * 3 / 2;
-    if (c32 < std::min(c64, c128)) return project_launch<ROLE, 64>(d, ds, s);
-    if (c64 < c128) return project_launch<ROLE, 128>(d, ds, s);
+    if (mt * tiles_of(d.F, 32) <= pairs) return project_launch<ROLE, 64>(d, ds, s);
+    if (mt * tiles_of(d.F, 64) <= pairs) return project_launch<ROLE, 128>(d, ds, s);
     return project_launch<ROLE, 256>(d, ds, s);
 }
 
@@ -777,18 +816,68 @@ int gated(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
 }
 
 // ---------------------------------------------------------------- products
-constexpr int kPairs = 76;  // of a GB300, for the workspace's size
+constexpr int kPairs = 76;  // of a GB300; the workspace's size does not ask the device
 constexpr int kMaxSplits = 16;
+constexpr int kFewColumns = 128;  // tokens of dx's transposed product
+constexpr int kOuterTokens = 16;  // tokens of dW as sums of outer products
+constexpr int kSumThreads = 256;
 
-// Parts of K for a product of few tiles: as many as leave every pair a tile, each
-// at least eight blocks deep.
-int product_splits(int64_t M, int N, int64_t K) {
-    const int64_t tiles = static_cast<int64_t>(tiles_of(M, kPM)) * tiles_of(N, 128);
-    const int64_t n = std::min<int64_t>({kPairs / tiles, kMaxSplits, tiles_of(K, kBK) / 8});
-    return static_cast<int>(std::max<int64_t>(n, 1));
+// How a product M x N over K is cut: tile width, whole tiles, parts of the others.
+struct Cut {
+    int width, main_tiles, tail_tiles, splits, kb_split;
+    size_t part_bytes() const {
+        return splits > 1 ? static_cast<size_t>(splits) * tail_tiles * kPM * width * sizeof(float) : 0;
+    }
+};
+
+// Rounds are counted in 64-wide blocks of K: a round of tiles takes the same time
+// at every width (a stage's loads do, measured 0.31 us at 64 to 256 columns), so
+// wide tiles are taken unless narrower ones need no more rounds; a last round
+// with less than half the pairs busy is split over K, which costs about 16
+// blocks' time for its parts.
+Cut cut_product(int64_t M, int N, int64_t K) {
+    const int kb = tiles_of(K, kBK);
+    Cut best{};
+    int64_t best_cost = 0;
+    for (const int width : {256, 192, 128}) {
+        const int64_t tiles = static_cast<int64_t>(tiles_of(M, kPM)) * tiles_of(N, width);
+        const int64_t rest = tiles % kPairs;
+        Cut c{width, static_cast<int>(std::min<int64_t>(tiles, 0x3fffffff)), 0, 1, kb};
+        int64_t cost = (tiles + kPairs - 1) / kPairs * kb;
+        const int splits = rest ? static_cast<int>(std::min<int64_t>({kPairs / rest, kMaxSplits, kb / 8})) : 1;
+        if (splits > 1) {
+            const int kb_split = tiles_of(kb, splits);
+            const int64_t split_cost = tiles / kPairs * kb + kb_split + 16;
+            if (split_cost < cost) {
+                cost = split_cost;
+                c = Cut{width, static_cast<int>(tiles - rest), static_cast<int>(rest), tiles_of(kb, kb_split), kb_split};
+            }
+        }
+        if (best.width == 0 || cost < best_cost) {
+            best = c;
+            best_cost = cost;
+        }
+    }
+    return best;
 }
 
-constexpr int kSumThreads = 256;
+// The split tiles' parts added in order, to bf16.  A block is one tile's row.
+__global__ void __launch_bounds__(kSumThreads) glu_sum_tiles_kernel(const GluParams p, int width, uint16_t *out) {
+    const int tiles = p.m_tiles * p.n_tiles - p.main_tiles;
+    const int local = blockIdx.x >> 8, r = blockIdx.x & 255;
+    int mt, nt;
+    tile_coords(p.main_tiles + local, p, mt, nt);
+    const int64_t row = static_cast<int64_t>(mt) * kPM + r;
+    const int c = threadIdx.x, col = nt * width + c;
+    if (row >= p.M || c >= width || col >= p.N) return;
+    const float *at = p.parts + (static_cast<int64_t>(local) * kPM + r) * width + c;
+    const int64_t step = static_cast<int64_t>(tiles) * kPM * width;
+    float v = 0.0f;
+    for (int q = 0; q < p.splits; ++q) v += at[q * step];
+    reinterpret_cast<bf16 *>(out)[row * p.N + col] = from_f32<bf16>(v);
+}
+
+// parts [splits][quads * 4] added in order, to bf16.
 __global__ void __launch_bounds__(kSumThreads) glu_sum_kernel(int64_t quads, int splits, const float4 *parts, uint2 *out) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kSumThreads + threadIdx.x;
     if (i >= quads) return;
@@ -802,15 +891,14 @@ __global__ void __launch_bounds__(kSumThreads) glu_sum_kernel(int64_t quads, int
 
 // C (M x N, bf16) = op(A) B with B K x N; A_MN: A stored K x M.
 template <bool A_MN, int BN>
-int product_launch(int64_t M, int N, int64_t K, const uint16_t *A, const uint16_t *B, uint16_t *C, int splits,
+int product_launch(int64_t M, int N, int64_t K, const uint16_t *A, const uint16_t *B, uint16_t *C, const Cut &cut,
                    float *parts, DeviceState &ds, cudaStream_t s) {
     GluParams p{};
     p.M = M, p.N = N;
     p.m_tiles = tiles_of(M, kPM);
     p.n_tiles = tiles_of(N, BN);
     p.kb_total = tiles_of(K, kBK);
-    p.kb_split = tiles_of(p.kb_total, splits);
-    p.splits = tiles_of(p.kb_total, p.kb_split);  // no empty part
+    p.main_tiles = cut.main_tiles, p.splits = cut.splits, p.kb_split = cut.kb_split;
     p.parts = parts;
     CUtensorMap a{}, b{}, c{};
     int rc;
@@ -820,27 +908,90 @@ int product_launch(int64_t M, int N, int64_t K, const uint16_t *A, const uint16_
     if ((rc = make_tmap_2d_bf16(&c, C, N, M, static_cast<uint64_t>(N) * 2, 64, 32))) return rc;
     if ((rc = pair_launch<PRODUCT, BN, A_MN, true>(p, a, b, c, c, ds, s))) return rc;
     if (p.splits == 1) return ISAM_OK;
-    const int64_t quads = M * N / 4;
-    glu_sum_kernel<<<static_cast<unsigned>((quads + kSumThreads - 1) / kSumThreads), kSumThreads, 0, s>>>(
-        quads, p.splits, reinterpret_cast<const float4 *>(parts), reinterpret_cast<uint2 *>(C));
-    return launch_status("launch glu_sum_kernel");
+    p.group_m = kGroupM;
+    glu_sum_tiles_kernel<<<static_cast<unsigned>(cut.tail_tiles) * kPM, kSumThreads, 0, s>>>(p, BN, C);
+    return launch_status("launch glu_sum_tiles_kernel");
 }
 
 template <bool A_MN>
 int product(int64_t M, int N, int64_t K, const uint16_t *A, const uint16_t *B, uint16_t *C, float *parts,
             DeviceState &ds, cudaStream_t s) {
-    const int pairs = std::max(1, gemm_cluster_capacity(ds, 2));
-    const int64_t mt = tiles_of(M, kPM);
-    const int splits = parts ? product_splits(M, N, K) : 1;
-    if (splits > 1) return product_launch<A_MN, 128>(M, N, K, A, B, C, splits, parts, ds, s);
-    const int64_t c256 = width_cost(mt, N, 256, pairs), c192 = width_cost(mt, N, 192, pairs),
-                  c128 = width_cost(mt, N, 128, pairs);
-    if (c128 < std::min(c192, c256)) return product_launch<A_MN, 128>(M, N, K, A, B, C, 1, nullptr, ds, s);
-    if (c192 < c256) return product_launch<A_MN, 192>(M, N, K, A, B, C, 1, nullptr, ds, s);
-    return product_launch<A_MN, 256>(M, N, K, A, B, C, 1, nullptr, ds, s);
+    const Cut cut = cut_product(M, N, K);
+    if (cut.width == 128) return product_launch<A_MN, 128>(M, N, K, A, B, C, cut, parts, ds, s);
+    if (cut.width == 192) return product_launch<A_MN, 192>(M, N, K, A, B, C, cut, parts, ds, s);
+    return product_launch<A_MN, 256>(M, N, K, A, B, C, cut, parts, ds, s);
 }
 
-// Bytes of d in the workspace, up to where the parts of dx follow.
+// dx^T = W^T d^T for few tokens: parts of K for every pair of SMs.
+int few_splits(int D, int64_t K) {
+    const int tiles = tiles_of(D, kPM);
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kPairs / tiles, kMaxSplits, tiles_of(K, kBK) / 8})));
+}
+
+template <int BN>
+int few_product_launch(const GluDesc &d, const uint16_t *dg, float *parts, DeviceState &ds, cudaStream_t s) {
+    const int64_t K = 2 * static_cast<int64_t>(d.F);
+    GluParams p{};
+    p.M = d.D, p.N = d.T;
+    p.m_tiles = tiles_of(d.D, kPM);
+    p.n_tiles = 1;
+    p.kb_total = tiles_of(K, kBK);
+    p.main_tiles = 0;
+    p.kb_split = tiles_of(p.kb_total, few_splits(d.D, K));
+    p.splits = tiles_of(p.kb_total, p.kb_split);
+    p.parts = parts;
+    CUtensorMap a{}, b{};
+    int rc;
+    if ((rc = make_tmap_2d_bf16(&a, d.W, d.D, K, static_cast<uint64_t>(d.D) * 2, 64, kBK))) return rc;
+    if ((rc = make_tmap_2d_bf16(&b, dg, K, d.T, K * 2, 64, BN / 2))) return rc;
+    if ((rc = pair_launch<PRODUCT_FEW, BN, true, false>(p, a, b, b, b, ds, s))) return rc;
+    const int64_t quads = static_cast<int64_t>(d.T) * d.D / 4;
+    glu_sum_kernel<<<static_cast<unsigned>((quads + kSumThreads - 1) / kSumThreads), kSumThreads, 0, s>>>(
+        quads, p.splits, reinterpret_cast<const float4 *>(parts), reinterpret_cast<uint2 *>(d.dx));
+    return launch_status("launch glu_sum_kernel");
+}
+
+// dW for few tokens: a sum of T outer products, bound by writing dW.  A thread has
+// eight columns of eight rows; a token's eight x and its eight d (the same for the
+// whole block) make 64 products, two a packed instruction.
+constexpr int kOuterThreads = 128, kOuterRows = 8;
+__global__ void __launch_bounds__(kOuterThreads)
+    glu_outer_kernel(int T, int D, int64_t F2, const uint16_t *d, const uint16_t *x, uint16_t *dW) {
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kOuterRows;
+    const int col = (blockIdx.y * kOuterThreads + threadIdx.x) * 8;
+    if (col >= D) return;
+    unsigned long long sum[kOuterRows][4] = {};
+    for (int t = 0; t < T; ++t) {
+        const uint4 xv = __ldg(reinterpret_cast<const uint4 *>(x + static_cast<int64_t>(t) * D + col));
+        const uint4 dv = __ldg(reinterpret_cast<const uint4 *>(d + t * F2 + row0));  // 2F is a multiple of 16
+        const uint32_t xw[4] = {xv.x, xv.y, xv.z, xv.w}, dw[4] = {dv.x, dv.y, dv.z, dv.w};
+        unsigned long long xp[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            asm("mov.b64 %0, {%1, %2};" : "=l"(xp[i]) : "r"(xw[i] << 16), "r"(xw[i] & 0xffff0000u));
+#pragma unroll
+        for (int r = 0; r < kOuterRows; ++r) {
+            const uint32_t v = r & 1 ? dw[r / 2] & 0xffff0000u : dw[r / 2] << 16;
+            unsigned long long dd;
+            asm("mov.b64 %0, {%1, %1};" : "=l"(dd) : "r"(v));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(sum[r][i]) : "l"(dd), "l"(xp[i]));
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kOuterRows; ++r) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float lo, hi;
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(sum[r][i]));
+            w[i] = pack2(lo, hi);
+        }
+        __stcs(reinterpret_cast<uint4 *>(dW + (row0 + r) * D + col), make_uint4(w[0], w[1], w[2], w[3]));
+    }
+}
+
+// Bytes of d in the workspace, up to where the products' parts follow.
 size_t d_bytes(int T, int F) { return (static_cast<size_t>(T) * F * 4 + 255) / 256 * 256; }
 
 }  // namespace
@@ -848,19 +999,35 @@ size_t d_bytes(int T, int F) { return (static_cast<size_t>(T) * F * 4 + 255) / 2
 int glu_forward_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) { return gated<PROJECT>(d, ds, s); }
 
 size_t glu_backward_workspace(int T, int D, int F) {
-    const int splits = product_splits(T, D, 2 * static_cast<int64_t>(F));
-    return d_bytes(T, F) + (splits > 1 ? static_cast<size_t>(splits) * T * D * 4 : 0);
+    const int64_t F2 = 2 * static_cast<int64_t>(F);
+    const size_t dx = T <= kFewColumns ? static_cast<size_t>(few_splits(D, F2)) * T * D * sizeof(float)
+                                       : cut_product(T, D, F2).part_bytes();
+    const size_t dW = T <= kOuterTokens ? 0 : cut_product(F2, D, T).part_bytes();
+    return d_bytes(T, F) + std::max(dx, dW);
 }
 
 int glu_backward_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     if (!d.dx && !d.dW) return ISAM_OK;
     int rc = gated<PROJECT_BACK>(d, ds, s);
     if (rc) return rc;
-    const uint16_t *ws = static_cast<const uint16_t *>(d.workspace);
+    const uint16_t *dg = static_cast<const uint16_t *>(d.workspace);
     float *parts = reinterpret_cast<float *>(static_cast<uint8_t *>(d.workspace) + d_bytes(d.T, d.F));
     const int64_t F2 = 2 * static_cast<int64_t>(d.F);
-    if (d.dx && (rc = product<false>(d.T, d.D, F2, ws, d.W, d.dx, parts, ds, s))) return rc;
-    if (d.dW && (rc = product<true>(F2, d.D, d.T, ws, d.x, d.dW, nullptr, ds, s))) return rc;
+    if (d.dx) {
+        rc = d.T <= 32            ? few_product_launch<32>(d, dg, parts, ds, s)
+             : d.T <= 64          ? few_product_launch<64>(d, dg, parts, ds, s)
+             : d.T <= kFewColumns ? few_product_launch<128>(d, dg, parts, ds, s)
+                                  : product<false>(d.T, d.D, F2, dg, d.W, d.dx, parts, ds, s);
+        if (rc) return rc;
+    }
+    if (d.dW && d.T <= kOuterTokens) {
+        const int cols = tiles_of(d.D, 8 * kOuterThreads);
+        if (cols > 65535) return set_error(ISAM_ERR_UNSUPPORTED, "isam_glu_backward: D (%d) is too large", d.D);
+        glu_outer_kernel<<<dim3(static_cast<unsigned>(F2 / kOuterRows), static_cast<unsigned>(cols)), kOuterThreads, 0,
+                           s>>>(d.T, d.D, F2, dg, d.x, d.dW);
+        return launch_status("launch glu_outer_kernel");
+    }
+    if (d.dW) return product<true>(F2, d.D, d.T, dg, d.x, d.dW, parts, ds, s);
     return ISAM_OK;
 }
 
