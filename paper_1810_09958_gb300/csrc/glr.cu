@@ -555,6 +555,7 @@ __global__ void __launch_bounds__(32 * Shape<V, false>::kWarps, Shape<V, false>:
         fence_mbar_init();
     }
     exchange_init(folds, p.cluster);
+    dependent_start();
     const int hidden = p.d.hidden;
     const int64_t step = static_cast<int64_t>(p.d.batch) * hidden;
     const int round = w.span * L, first = w.chunk * L;
@@ -698,6 +699,7 @@ __global__ void __launch_bounds__(32 * Shape<V, true>::kWarps, Shape<V, true>::k
         fence_mbar_init();
     }
     exchange_init(folds, p.cluster);
+    dependent_start();
     const int hidden = p.d.hidden;
     const int64_t step = static_cast<int64_t>(p.d.batch) * hidden;
     const bool has_dh = p.d.dh_out != nullptr;
@@ -862,6 +864,7 @@ __global__ void __launch_bounds__(kStepThreads)
     glr_walk_forward_kernel(const __grid_constant__ GlrDesc d, int64_t threads) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kStepThreads + threadIdx.x;
     if (i >= threads) return;
+    dependent_start();
     const int per = d.hidden / V;
     const int64_t b = i / per, chain = i * V;  // (a row of `per` threads is one of `hidden` channels)
     const int64_t step = static_cast<int64_t>(d.batch) * d.hidden;
@@ -907,6 +910,7 @@ __global__ void __launch_bounds__(kStepThreads)
     glr_walk_backward_kernel(const __grid_constant__ GlrDesc d, int64_t threads) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kStepThreads + threadIdx.x;
     if (i >= threads) return;
+    dependent_start();
     const int per = d.hidden / V;
     const int64_t b = i / per, chain = i * V;
     const int64_t step = static_cast<int64_t>(d.batch) * d.hidden;
@@ -971,6 +975,7 @@ __global__ void __launch_bounds__(kStepThreads)
                     float *new_state, Hy *h) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kStepThreads + threadIdx.x;
     if (i >= threads) return;
+    dependent_start();
     const int per = hidden / V;
     const int64_t b = i / per;
     const int c = static_cast<int>(i - b * per) * V;
@@ -1062,7 +1067,7 @@ int resident_clusters(const void *fn, int c, int threads, int smem, const Device
 // leave SMs idle.
 template <typename S, int V>
 int scan_shape(const void *fn, const GlrDesc &d, int smem, const DeviceState &ds, ScanParams &p,
-               cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr) {
+               cudaLaunchConfig_t &cfg) {
     constexpr int L = S::kSteps;
     p.d = d;
     p.err = ds.err_word;
@@ -1093,12 +1098,6 @@ int scan_shape(const void *fn, const GlrDesc &d, int smem, const DeviceState &ds
     cfg.gridDim = dim3(static_cast<unsigned>(grid));
     cfg.blockDim = dim3(32 * warps);
     cfg.dynamicSmemBytes = bytes;
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = p.cluster;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = p.cluster > 1 ? 1 : 0;
     return ISAM_OK;
 }
 
@@ -1109,17 +1108,15 @@ int forward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
     const auto fn = glr_forward_kernel<G, Hy, V, L, ROWS>;
     ScanParams p{};
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    int rc = scan_shape<S, V>(reinterpret_cast<const void *>(fn), d, sizeof(ForwardTiles<G, Hy, V, L, ROWS>), ds, p, cfg, attr);
+    int rc = scan_shape<S, V>(reinterpret_cast<const void *>(fn), d, sizeof(ForwardTiles<G, Hy, V, L, ROWS>), ds, p, cfg);
     if (rc) return rc;
     CUtensorMap tg{}, th{};
     if (ROWS == kTma) {
         if ((rc = rows_tmap(&tg, d.g, d.g_type, d.hidden, 2LL * d.batch, d.T, 32 * V, L))) return rc;
         if ((rc = rows_tmap(&th, d.h_out, d.h_type, d.hidden, d.batch, d.T, 32 * V, L))) return rc;
     }
-    cfg.stream = s;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, tg, th, p);
-    return e == cudaSuccess ? ISAM_OK : cuda_error(e, "launch glr_forward_kernel");
+    return launch_dependent(fn, cfg.gridDim, static_cast<int>(cfg.blockDim.x), cfg.dynamicSmemBytes, s, p.cluster,
+                            "launch glr_forward_kernel", tg, th, p);
 }
 
 template <typename G, typename Hy, int V, Rows ROWS>
@@ -1129,8 +1126,7 @@ int backward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
     const auto fn = glr_backward_kernel<G, Hy, V, L, ROWS>;
     ScanParams p{};
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    int rc = scan_shape<S, V>(reinterpret_cast<const void *>(fn), d, sizeof(BackwardTiles<G, Hy, V, L, ROWS>), ds, p, cfg, attr);
+    int rc = scan_shape<S, V>(reinterpret_cast<const void *>(fn), d, sizeof(BackwardTiles<G, Hy, V, L, ROWS>), ds, p, cfg);
     if (rc) return rc;
     CUtensorMap tg{}, th{}, tdh{}, tdg{};
     if (ROWS == kTma) {
@@ -1139,9 +1135,8 @@ int backward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
         if (d.dh_out && (rc = rows_tmap(&tdh, d.dh_out, d.h_type, d.hidden, d.batch, d.T, 32 * V, L))) return rc;
         if ((rc = rows_tmap(&tdg, d.dg, d.g_type, d.hidden, 2LL * d.batch, d.T, 32 * V, L))) return rc;
     }
-    cfg.stream = s;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, tg, th, tdh, tdg, p);
-    return e == cudaSuccess ? ISAM_OK : cuda_error(e, "launch glr_backward_kernel");
+    return launch_dependent(fn, cfg.gridDim, static_cast<int>(cfg.blockDim.x), cfg.dynamicSmemBytes, s, p.cluster,
+                            "launch glr_backward_kernel", tg, th, tdh, tdg, p);
 }
 
 // Whether walking beats the scan.  Measured forward, us, walk against scan, 1024
@@ -1157,8 +1152,7 @@ int walk_launch(void (*fn)(const GlrDesc, int64_t), const GlrDesc &d, int V, cud
     const int64_t threads = static_cast<int64_t>(d.batch) * (d.hidden / V);
     const int64_t blocks = (threads + kStepThreads - 1) / kStepThreads;
     if (blocks > 0x7fffffffLL) return set_error(ISAM_ERR_UNSUPPORTED, "batch * hidden is too large for one launch");
-    fn<<<static_cast<unsigned>(blocks), kStepThreads, 0, s>>>(d, threads);
-    return launch_status(what);
+    return launch_dependent(fn, dim3(static_cast<unsigned>(blocks)), kStepThreads, 0, s, 1, what, d, threads);
 }
 
 }  // namespace
@@ -1218,9 +1212,8 @@ int glr_step_launch(int batch, int hidden, int slots, int g_type, const void *g,
         const int64_t threads = static_cast<int64_t>(batch) * (four ? hidden / 4 : hidden);
         const unsigned blocks = static_cast<unsigned>((threads + kStepThreads - 1) / kStepThreads);
         const auto fn = four ? glr_step_kernel<G, Hy, 4> : glr_step_kernel<G, Hy, 1>;
-        fn<<<blocks, kStepThreads, 0, s>>>(threads, hidden, slots, static_cast<const G *>(g), slot_ids, state,
-                                           new_state, static_cast<Hy *>(h));
-        return launch_status("launch glr_step_kernel");
+        return launch_dependent(fn, dim3(blocks), kStepThreads, 0, s, 1, "launch glr_step_kernel", threads, hidden, slots,
+                                static_cast<const G *>(g), slot_ids, state, new_state, static_cast<Hy *>(h));
     });
 }
 

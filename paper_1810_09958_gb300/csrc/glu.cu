@@ -670,6 +670,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1)
     }
     fence_mbar_init();
     __syncthreads();
+    dependent_start();
     const WaitCtx wait{p.timeout_ns, p.err, &abort_flag};
     const int r = lane >> 2, t = lane & 3;
     constexpr int kTeams = kFewWarps / kTeam;
@@ -800,8 +801,8 @@ int few_launch(const GluDesc &d, int stages, DeviceState &ds, cudaStream_t s) {
                                 "cudaFuncSetAttribute(gated feed-forward, few tokens)")))
         return rc;
     const size_t smem = 1024 + kFewWarps * (stages * kFewBlock + few_part<NT>()) + static_cast<size_t>(p.x_stride) * d.T;
-    fn<<<std::min(p.groups, ds.num_sms), 32 * kFewWarps, smem, s>>>(w, p);
-    return launch_status("launch glu_few_kernel");
+    return launch_dependent(fn, dim3(std::min(p.groups, ds.num_sms)), 32 * kFewWarps, smem, s, 1,
+                            "launch glu_few_kernel", w, p);
 }
 
 // The projections and their gate: h, or d into the workspace.
@@ -861,31 +862,41 @@ Cut cut_product(int64_t M, int N, int64_t K) {
     return best;
 }
 
-// The split tiles' parts added in order, to bf16.  A block is one tile's row.
-__global__ void __launch_bounds__(kSumThreads) glu_sum_tiles_kernel(const GluParams p, int width, uint16_t *out) {
-    const int tiles = p.m_tiles * p.n_tiles - p.main_tiles;
-    const int local = blockIdx.x >> 8, r = blockIdx.x & 255;
+__device__ __forceinline__ float4 sum_parts(const float4 *at, int64_t step, int splits) {
+    float4 v = *at;
+#pragma unroll 4
+    for (int q = 1; q < splits; ++q) {
+        const float4 w = at[q * step];
+        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    }
+    return v;
+}
+
+// The split tiles' parts added in order, to bf16: four columns a thread.
+__global__ void __launch_bounds__(kSumThreads)
+    glu_sum_tiles_kernel(const __grid_constant__ GluParams p, int width, uint16_t *out) {
+    dependent_start();
+    const int tiles = p.m_tiles * p.n_tiles - p.main_tiles, per_row = width / 4;
+    const int i = blockIdx.x * kSumThreads + threadIdx.x;
+    const int local = i / (kPM * per_row), in = i - local * (kPM * per_row);
+    const int r = in / per_row, c = 4 * (in - r * per_row);
+    if (local >= tiles) return;
     int mt, nt;
     tile_coords(p.main_tiles + local, p, mt, nt);
     const int64_t row = static_cast<int64_t>(mt) * kPM + r;
-    const int c = threadIdx.x, col = nt * width + c;
-    if (row >= p.M || c >= width || col >= p.N) return;
-    const float *at = p.parts + (static_cast<int64_t>(local) * kPM + r) * width + c;
-    const int64_t step = static_cast<int64_t>(tiles) * kPM * width;
-    float v = 0.0f;
-    for (int q = 0; q < p.splits; ++q) v += at[q * step];
-    reinterpret_cast<bf16 *>(out)[row * p.N + col] = from_f32<bf16>(v);
+    const int col = nt * width + c;
+    if (row >= p.M || col >= p.N) return;  // (N is a multiple of 8)
+    const float4 v = sum_parts(reinterpret_cast<const float4 *>(p.parts) + i, static_cast<int64_t>(tiles) * kPM * per_row,
+                               p.splits);
+    *reinterpret_cast<uint2 *>(out + row * p.N + col) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
 }
 
 // parts [splits][quads * 4] added in order, to bf16.
 __global__ void __launch_bounds__(kSumThreads) glu_sum_kernel(int64_t quads, int splits, const float4 *parts, uint2 *out) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kSumThreads + threadIdx.x;
     if (i >= quads) return;
-    float4 v = parts[i];
-    for (int q = 1; q < splits; ++q) {
-        const float4 w = parts[q * quads + i];
-        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
-    }
+    dependent_start();
+    const float4 v = sum_parts(parts + i, quads, splits);
     out[i] = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
 }
 
@@ -909,8 +920,9 @@ int product_launch(int64_t M, int N, int64_t K, const uint16_t *A, const uint16_
     if ((rc = pair_launch<PRODUCT, BN, A_MN, true>(p, a, b, c, c, ds, s))) return rc;
     if (p.splits == 1) return ISAM_OK;
     p.group_m = kGroupM;
-    glu_sum_tiles_kernel<<<static_cast<unsigned>(cut.tail_tiles) * kPM, kSumThreads, 0, s>>>(p, BN, C);
-    return launch_status("launch glu_sum_tiles_kernel");
+    const int quads = cut.tail_tiles * kPM * BN / 4;  // below 76 tiles
+    return launch_dependent(glu_sum_tiles_kernel, dim3(tiles_of(quads, kSumThreads)), kSumThreads, 0, s, 1,
+                            "launch glu_sum_tiles_kernel", p, BN, C);
 }
 
 template <bool A_MN>
@@ -946,9 +958,9 @@ int few_product_launch(const GluDesc &d, const uint16_t *dg, float *parts, Devic
     if ((rc = make_tmap_2d_bf16(&b, dg, K, d.T, K * 2, 64, BN / 2))) return rc;
     if ((rc = pair_launch<PRODUCT_FEW, BN, true, false>(p, a, b, b, b, ds, s))) return rc;
     const int64_t quads = static_cast<int64_t>(d.T) * d.D / 4;
-    glu_sum_kernel<<<static_cast<unsigned>((quads + kSumThreads - 1) / kSumThreads), kSumThreads, 0, s>>>(
-        quads, p.splits, reinterpret_cast<const float4 *>(parts), reinterpret_cast<uint2 *>(d.dx));
-    return launch_status("launch glu_sum_kernel");
+    return launch_dependent(glu_sum_kernel, dim3(tiles_of(quads, kSumThreads)), kSumThreads, 0, s, 1,
+                            "launch glu_sum_kernel", quads, p.splits, reinterpret_cast<const float4 *>(parts),
+                            reinterpret_cast<uint2 *>(d.dx));
 }
 
 // dW for few tokens: a sum of T outer products, bound by writing dW.  A thread has
@@ -960,7 +972,9 @@ __global__ void __launch_bounds__(kOuterThreads)
     const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kOuterRows;
     const int col = (blockIdx.y * kOuterThreads + threadIdx.x) * 8;
     if (col >= D) return;
+    dependent_start();
     unsigned long long sum[kOuterRows][4] = {};
+#pragma unroll 4
     for (int t = 0; t < T; ++t) {
         const uint4 xv = __ldg(reinterpret_cast<const uint4 *>(x + static_cast<int64_t>(t) * D + col));
         const uint4 dv = __ldg(reinterpret_cast<const uint4 *>(d + t * F2 + row0));  // 2F is a multiple of 16
@@ -1023,9 +1037,8 @@ int glu_backward_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     if (d.dW && d.T <= kOuterTokens) {
         const int cols = tiles_of(d.D, 8 * kOuterThreads);
         if (cols > 65535) return set_error(ISAM_ERR_UNSUPPORTED, "isam_glu_backward: D (%d) is too large", d.D);
-        glu_outer_kernel<<<dim3(static_cast<unsigned>(F2 / kOuterRows), static_cast<unsigned>(cols)), kOuterThreads, 0,
-                           s>>>(d.T, d.D, F2, dg, d.x, d.dW);
-        return launch_status("launch glu_outer_kernel");
+        return launch_dependent(glu_outer_kernel, dim3(static_cast<unsigned>(F2 / kOuterRows), static_cast<unsigned>(cols)),
+                                kOuterThreads, 0, s, 1, "launch glu_outer_kernel", d.T, d.D, F2, dg, d.x, d.dW);
     }
     if (d.dW) return product<true>(F2, d.D, d.T, dg, d.x, d.dW, parts, ds, s);
     return ISAM_OK;

@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 
 #include "internal.h"
+#include "ptx.cuh"
 
 namespace isam {
 
@@ -57,6 +58,40 @@ __device__ __forceinline__ void activation(float a, float &v, float &dv) {
             dv = s.keep * (1.0f + a * s.take);
         }
     }
+}
+
+// Launches a kernel that begins with dependent_start(): its CTAs may be set up
+// while the stream's previous kernel drains (programmatic dependent launch).
+// `cluster` CTAs a cluster where above 1.
+template <typename... Params, typename... Args>
+int launch_dependent(void (*fn)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t s, unsigned cluster,
+                     const char *what, Args &&...args) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 1;
+    if (cluster > 1) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = cluster;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, static_cast<Params>(args)...);
+    return e == cudaSuccess ? ISAM_OK : cuda_error(e, what);
+}
+
+// Before a kernel's first access to global memory: the next kernel may be set
+// up from here, and everything the previous ones wrote is visible after.
+__device__ __forceinline__ void dependent_start() {
+    griddep_launch_dependents();
+    griddep_wait();
 }
 
 inline int launch_status(const char *what) {

@@ -157,6 +157,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) gemv_w4_kernel(const __grid_con
     if (threadIdx.x == 0) abort_flag = 0;
     fence_mbar_init();
     __syncthreads();
+    dependent_start();
     const WaitCtx wait{p.timeout_ns, p.err, &abort_flag};
     const int r = lane >> 2, t = lane & 3;
     const int blocks = (p.N + 15) / 16;
@@ -351,8 +352,7 @@ int gemv_launch(W4Params p, DeviceState &ds, cudaStream_t s) {
         return WARPS * (kStages * p.per_stage * tile_bytes<GROUP, RB>() + part_bytes<NT, RB>()) + x;
     };
     while (p.per_stage > 1 && (bytes() > kMaxSmem || p.per_stage * p.team > p.kt)) p.per_stage /= 2;
-    fn<<<grid, 32 * WARPS, bytes(), s>>>(p);
-    return launch_status("launch gemv_w4_kernel");
+    return launch_dependent(fn, dim3(grid), 32 * WARPS, bytes(), s, 1, "launch gemv_w4_kernel", p);
 }
 
 // x goes to shared memory where it leaves room for the ring.
