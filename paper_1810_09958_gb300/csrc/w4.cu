@@ -98,10 +98,10 @@ struct RowScales {
 
 struct W4Params {
     int M, N, K;
-    int kt;       // k tiles
-    int groups;   // of 16 RB rows
-    int team;     // warps that share the K of a group
-    int per_stage;  // k tiles of a stage
+    int kt;         // k tiles
+    int groups;     // of 16 RB rows
+    int team;       // warps that share the K of a group
+    int per;        // k tiles of a warp in a stage
     int x_stride;   // bytes of a token's row of x in shared memory
     const uint16_t *x;
     const uint8_t *tiled;
@@ -120,12 +120,14 @@ constexpr int part_bytes() {  // a warp's sums, twice
     return 2 * 8 * NT * 16 * RB * 4;
 }
 
-// One CTA an SM.  A team of its warps takes 16 RB rows by 8 NT tokens; its warps
-// share K's tiles in turn, `per_stage` neighbours each, and their sums meet in
-// shared memory, in the order of the warps.  Codes arrive by bulk copies into a
-// ring a warp, across groups of rows; x is in shared memory as a whole where it
-// fits (XS), rows 64 bytes off a multiple of 128 so that eight lanes' 16 bytes
-// touch every bank once.
+// One CTA an SM.  A team of its warps takes 16 RB rows by 8 NT tokens at a time;
+// its warps share K's tiles, `per` neighbours each in a stage, and their sums meet
+// in shared memory, in the order of the warps.  A thread of a warp of its own
+// brings a team's stage, the codes of team * per neighbouring tiles and their
+// scales, by two bulk copies a block of rows, across groups of rows.  (Copies by
+// each warp for itself took 130 instructions a stage beside a tile's 107.)  x is
+// in shared memory as a whole where it fits (XS), rows 64 bytes off a multiple of
+// 128 so that eight lanes' 16 bytes touch every bank once.
 //
 // Lane 4 r + t holds rows r and 8 + r of a tile, in word j the k of eight t of
 // 32-block j.  The order of k inside a product does not matter, so the words'
@@ -136,194 +138,188 @@ constexpr int part_bytes() {  // a warp's sums, twice
 // Bound: reading the codes; beside it the instructions that make them bf16,
 // nine for eight codes.
 template <int NT, int GROUP, int RB, bool XS, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS, 1) gemv_w4_kernel(const __grid_constant__ W4Params p) {
+__global__ void __launch_bounds__(32 * (WARPS + 1), 1) gemv_w4_kernel(const __grid_constant__ W4Params p) {
     constexpr int kPer = 128 / GROUP, kRows = 16 * RB, kSize = kRows * 8 * NT;
     // Word blocks of one scale summed before it applies (all of a tile's would cost
     // registers where rows and tokens are many).
     constexpr int kSpan = RB * NT > 2 ? 1 : GROUP / 32;
     constexpr int kBlock = kTileBytes + 32 * kPer;  // codes and scales of one tile
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ uint64_t full_all[WARPS][kStages];
+    __shared__ uint64_t full[WARPS][kStages], empty[WARPS][kStages];  // of each team
     __shared__ int abort_flag;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int team = warp / p.team, member = warp - team * p.team, teams = WARPS / p.team;
-    const int per = p.per_stage, stage_bytes = per * RB * kBlock;
-    uint8_t *ring = smem + warp * kStages * stage_bytes;
-    float *part = reinterpret_cast<float *>(smem + WARPS * kStages * stage_bytes) + team * p.team * 2 * kSize;
-    uint8_t *xs = smem + WARPS * (kStages * stage_bytes + part_bytes<NT, RB>());
-    uint64_t *full = full_all[warp];
-    if (lane == 0)
-        for (int i = 0; i < kStages; ++i) mbar_init(&full[i], 1);
+    const int teams = WARPS / p.team, tiles = p.team * p.per;  // of a stage
+    const int stage_bytes = tiles * RB * kBlock;
+    uint8_t *xs = smem + WARPS * part_bytes<NT, RB>() + teams * kStages * stage_bytes;
+    if (threadIdx.x < teams)
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&full[threadIdx.x][i], 1);
+            mbar_init(&empty[threadIdx.x][i], p.team);
+        }
     if (threadIdx.x == 0) abort_flag = 0;
     fence_mbar_init();
     __syncthreads();
     dependent_start();
     const WaitCtx wait{p.timeout_ns, p.err, &abort_flag};
-    const int r = lane >> 2, t = lane & 3;
     const int blocks = (p.N + 15) / 16;
-    const int first = team * gridDim.x + blockIdx.x, stride = teams * gridDim.x;  // groups of this team
-    const int k_first = member * per, k_stride = p.team * per;
+    const int stride = teams * gridDim.x;  // groups: team t's are t * gridDim.x + blockIdx.x and every stride-th
 
-    // A stage: for each block of rows its tiles' codes, then their scales.
-    int load_group = first, load_k = k_first;
-    uint32_t load_to = smem_u32(ring), load_bar = smem_u32(full);
-    const uint32_t last_bar = load_bar + 8 * (kStages - 1);
-    const uint8_t *load_code;  // of the group's first block and load_k
-    const uint16_t *load_scale;
-    const auto enter = [&] {
-        const int64_t tile = static_cast<int64_t>(load_group) * RB * p.kt + load_k;
-        load_code = p.tiled + tile * kTileBytes;
-        load_scale = p.scales + tile * 16 * kPer;
-    };
-    enter();
-    const auto fetch = [&]() {  // lane 0
-        if (load_k >= p.kt) {
-            load_k = k_first;
-            load_group += stride;
-            enter();
-        }
-        if (load_group >= p.groups || load_k >= p.kt) return;
-        const uint32_t n = min(per, p.kt - load_k);
-        const int rows = RB == 1 ? 1 : min(RB, blocks - load_group * RB);
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(load_bar), "r"(rows * n * kBlock)
-                     : "memory");
-#pragma unroll
-        for (int b = 0; b < RB; ++b)
-            if (b < rows) {
-                copy(load_to + b * per * kBlock, load_code + static_cast<int64_t>(b) * p.kt * kTileBytes, n * kTileBytes,
-                     load_bar);
-                copy(load_to + b * per * kBlock + per * kTileBytes, load_scale + static_cast<int64_t>(b) * p.kt * 16 * kPer,
-                     n * 32 * kPer, load_bar);
-            }
-        load_k += k_stride;
-        load_code += k_stride * kTileBytes;
-        load_scale += k_stride * 16 * kPer;
-        load_to += stage_bytes;
-        load_bar += 8;
-        if (load_bar > last_bar) {
-            load_bar -= 8 * kStages;
-            load_to -= kStages * stage_bytes;
-        }
-    };
-    if (lane == 0)
-        for (int i = 0; i < kStages; ++i) fetch();
-    if (XS) {
-        // x, and zeros behind K up to whole tiles.
-        const int chunks = 16 * p.kt;  // of 16 bytes
-        for (int i = threadIdx.x; i < p.M * chunks; i += 32 * WARPS) {
-            const int m = i / chunks, c = i - m * chunks;
-            uint8_t *to = xs + m * p.x_stride + 16 * c;
-            if (8 * c < p.K)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)),
-                             "l"(p.x + static_cast<int64_t>(m) * p.K + 8 * c)
-                             : "memory");
-            else
-                *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        __syncthreads();
-    }
-
-    // A token's k of this lane (lanes behind the last token read it again).
-    const uint16_t *xg[NT];
-    uint32_t xa[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int m = min(8 * n + r, p.M - 1);
-        xg[n] = p.x + static_cast<int64_t>(m) * p.K + 8 * t;
-        xa[n] = smem_u32(xs) + m * p.x_stride + 16 * t;
-    }
-    int stage = 0, half = 0;
-    uint32_t phase = 0;
-    const uint32_t ring_at = smem_u32(ring);
-    for (int g = first; g < p.groups; g += stride, half ^= 1) {
-        float sum[RB][NT][4] = {};
-        for (int k = k_first; k < p.kt; k += k_stride) {
-            bounded_wait(&full[stage], phase, wait, 0x801u);
-            uint32_t code_at = ring_at + stage * stage_bytes + 16 * lane;
-            uint32_t scale_at = ring_at + stage * stage_bytes + per * kTileBytes + 2 * kPer * r;
-            const uint32_t code_end = code_at + min(per, p.kt - k) * kTileBytes;
-            uint32_t x_at = 256 * k;  // bytes into a token's row
-#pragma unroll 1
-            for (; code_at != code_end; code_at += kTileBytes, scale_at += 32 * kPer, x_at += 256) {
-                uint4 code[RB][2];
-                RowScales<GROUP> scale[RB][2];
-#pragma unroll
-                for (int b = 0; b < RB; ++b)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        code[b][h] = lds16(code_at + b * per * kBlock + 512 * h);
-                        scale[b][h].load(scale_at + b * per * kBlock + 16 * kPer * h);
-                    }
-                float acc[RB][NT][4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint4 xv[NT];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        if (XS) {
-                            xv[n] = lds16(xa[n] + x_at + 64 * j);
-                        } else {
-                            xv[n] = make_uint4(0, 0, 0, 0);
-                            if (static_cast<int>(x_at / 2) + 32 * j + 8 * t < p.K)
-                                xv[n] = __ldg(reinterpret_cast<const uint4 *>(xg[n] + x_at / 2 + 32 * j));
+    if (warp == WARPS) {
+        // A stage: for each block of rows its tiles' codes, then their scales.
+        if (lane == 0) {
+            const uint32_t ring = smem_u32(smem + WARPS * part_bytes<NT, RB>());
+            int stage = 0;
+            uint32_t phase = 1;
+            bool ok = true;
+            for (int g0 = blockIdx.x; ok && g0 < p.groups; g0 += stride)
+                for (int k = 0; ok && k < p.kt; k += tiles) {
+                    const uint32_t n = min(tiles, p.kt - k);
+                    for (int team = 0; team < teams; ++team) {
+                        const int g = g0 + team * gridDim.x;
+                        if (g >= p.groups) break;
+                        if (!bounded_wait(&empty[team][stage], phase, wait, 0x802u)) {
+                            ok = false;
+                            break;
+                        }
+                        const uint32_t bar = smem_u32(&full[team][stage]);
+                        uint32_t to = ring + (team * kStages + stage) * stage_bytes;
+                        const int rows = RB == 1 ? 1 : min(RB, blocks - g * RB);
+                        mbar_arrive_expect_tx(&full[team][stage], rows * n * kBlock);
+                        for (int b = 0; b < rows; ++b) {
+                            const int64_t tile = static_cast<int64_t>(g * RB + b) * p.kt + k;
+                            copy(to, p.tiled + tile * kTileBytes, n * kTileBytes, bar);
+                            copy(to + tiles * kTileBytes, p.scales + tile * 16 * kPer, n * 32 * kPer, bar);
+                            to += tiles * kBlock;
                         }
                     }
+                    if (++stage == kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+        }
+        __syncwarp();
+    } else {
+        const int team = warp / p.team, member = warp - team * p.team;
+        const uint32_t ring = smem_u32(smem + WARPS * part_bytes<NT, RB>()) + team * kStages * stage_bytes;
+        float *part = reinterpret_cast<float *>(smem) + team * p.team * 2 * kSize;
+        const int r = lane >> 2, t = lane & 3;
+        if (XS) {
+            // x, and zeros behind K up to whole tiles.
+            const int chunks = 16 * p.kt;  // of 16 bytes
+            for (int i = threadIdx.x; i < p.M * chunks; i += 32 * WARPS) {
+                const int m = i / chunks, c = i - m * chunks;
+                uint8_t *to = xs + m * p.x_stride + 16 * c;
+                if (8 * c < p.K)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)),
+                                 "l"(p.x + static_cast<int64_t>(m) * p.K + 8 * c)
+                                 : "memory");
+                else
+                    *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            named_bar(15, 32 * WARPS);
+        }
+        // A token's k of this lane (lanes behind the last token read it again).
+        const uint16_t *xg[NT];
+        uint32_t xa[NT];
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) {
-                        const uint32_t lo_w = j == 0 ? code[b][0].x : j == 1 ? code[b][0].y : j == 2 ? code[b][0].z : code[b][0].w;
-                        const uint32_t hi_w = j == 0 ? code[b][1].x : j == 1 ? code[b][1].y : j == 2 ? code[b][1].z : code[b][1].w;
-                        uint32_t v[2][4];
-                        dequant(lo_w, v[0]);
-                        dequant(hi_w, v[1]);
-                        const uint32_t a0[4] = {v[0][0], v[1][0], v[0][1], v[1][1]};
-                        const uint32_t a1[4] = {v[0][2], v[1][2], v[0][3], v[1][3]};
+        for (int n = 0; n < NT; ++n) {
+            const int m = min(8 * n + r, p.M - 1);
+            xg[n] = p.x + static_cast<int64_t>(m) * p.K + 8 * t;
+            xa[n] = smem_u32(xs) + m * p.x_stride + 16 * t;
+        }
+        int stage = 0, half = 0;
+        uint32_t phase = 0;
+        for (int g = team * gridDim.x + blockIdx.x; g < p.groups; g += stride, half ^= 1) {
+            float sum[RB][NT][4] = {};
+            for (int k0 = 0; k0 < p.kt; k0 += tiles) {
+                const int k = member * p.per, n_tiles = min(p.per, p.kt - k0 - k);  // of the stage; below 1: none
+                bounded_wait(&full[team][stage], phase, wait, 0x801u);
+                uint32_t code_at = ring + stage * stage_bytes + k * kTileBytes + 16 * lane;
+                uint32_t scale_at = ring + stage * stage_bytes + tiles * kTileBytes + k * 32 * kPer + 2 * kPer * r;
+                const uint32_t code_end = code_at + max(n_tiles, 0) * kTileBytes;
+                uint32_t x_at = 256 * (k0 + k);  // bytes into a token's row
+#pragma unroll 1
+                for (; code_at != code_end; code_at += kTileBytes, scale_at += 32 * kPer, x_at += 256) {
+                    uint4 code[RB][2];
+                    RowScales<GROUP> scale[RB][2];
+#pragma unroll
+                    for (int b = 0; b < RB; ++b)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            code[b][h] = lds16(code_at + b * tiles * kBlock + 512 * h);
+                            scale[b][h].load(scale_at + b * tiles * kBlock + 16 * kPer * h);
+                        }
+                    float acc[RB][NT][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint4 xv[NT];
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            if (j % kSpan == 0)
-                                mma_16x8x16<true>(acc[b][n], a0, xv[n].x, xv[n].y);
-                            else
-                                mma_16x8x16<false>(acc[b][n], a0, xv[n].x, xv[n].y);
-                            mma_16x8x16<false>(acc[b][n], a1, xv[n].z, xv[n].w);
+                            if (XS) {
+                                xv[n] = lds16(xa[n] + x_at + 64 * j);
+                            } else {
+                                xv[n] = make_uint4(0, 0, 0, 0);
+                                if (static_cast<int>(x_at / 2) + 32 * j + 8 * t < p.K)
+                                    xv[n] = __ldg(reinterpret_cast<const uint4 *>(xg[n] + x_at / 2 + 32 * j));
+                            }
                         }
-                        if ((j + 1) % kSpan == 0) {
-                            const float lo = scale[b][0].get(j * 32 / GROUP), hi = scale[b][1].get(j * 32 / GROUP);
+#pragma unroll
+                        for (int b = 0; b < RB; ++b) {
+                            const auto word = [&](const uint4 &c) { return j == 0 ? c.x : j == 1 ? c.y : j == 2 ? c.z : c.w; };
+                            uint32_t v[2][4];
+                            dequant(word(code[b][0]), v[0]);
+                            dequant(word(code[b][1]), v[1]);
+                            const uint32_t a0[4] = {v[0][0], v[1][0], v[0][1], v[1][1]};
+                            const uint32_t a1[4] = {v[0][2], v[1][2], v[0][3], v[1][3]};
 #pragma unroll
                             for (int n = 0; n < NT; ++n) {
-                                sum[b][n][0] = fmaf(lo, acc[b][n][0], sum[b][n][0]);
-                                sum[b][n][1] = fmaf(lo, acc[b][n][1], sum[b][n][1]);
-                                sum[b][n][2] = fmaf(hi, acc[b][n][2], sum[b][n][2]);
-                                sum[b][n][3] = fmaf(hi, acc[b][n][3], sum[b][n][3]);
+                                if (j % kSpan == 0)
+                                    mma_16x8x16<true>(acc[b][n], a0, xv[n].x, xv[n].y);
+                                else
+                                    mma_16x8x16<false>(acc[b][n], a0, xv[n].x, xv[n].y);
+                                mma_16x8x16<false>(acc[b][n], a1, xv[n].z, xv[n].w);
+                            }
+                            if ((j + 1) % kSpan == 0) {
+                                const float lo = scale[b][0].get(j * 32 / GROUP), hi = scale[b][1].get(j * 32 / GROUP);
+#pragma unroll
+                                for (int n = 0; n < NT; ++n) {
+                                    sum[b][n][0] = fmaf(lo, acc[b][n][0], sum[b][n][0]);
+                                    sum[b][n][1] = fmaf(lo, acc[b][n][1], sum[b][n][1]);
+                                    sum[b][n][2] = fmaf(hi, acc[b][n][2], sum[b][n][2]);
+                                    sum[b][n][3] = fmaf(hi, acc[b][n][3], sum[b][n][3]);
+                                }
                             }
                         }
                     }
                 }
+                __syncwarp();  // every lane has read the stage
+                if (lane == 0) mbar_arrive(&empty[team][stage]);
+                if (++stage == kStages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
             }
-            __syncwarp();  // every lane has read the stage
-            if (lane == 0) fetch();
-            if (++stage == kStages) {
-                stage = 0;
-                phase ^= 1u;
+            float *mine = part + half * p.team * kSize;
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        mine[member * kSize + (8 * n + 2 * t + (i & 1)) * kRows + 16 * b + r + 8 * (i >> 1)] = sum[b][n][i];
+            if (p.team == 1)
+                __syncwarp();
+            else
+                named_bar(1 + team, 32 * p.team);
+            for (int i = 32 * member + lane; i < kSize; i += 32 * p.team) {
+                const int m = i / kRows, n = g * kRows + i % kRows;
+                if (m >= p.M || n >= p.N) continue;
+                float v = 0.0f;
+                for (int q = 0; q < p.team; ++q) v += mine[q * kSize + i];
+                p.y[static_cast<int64_t>(m) * p.N + n] = 8.0f * v;  // (weights counted in eighths)
             }
-        }
-        float *mine = part + half * p.team * kSize;
-#pragma unroll
-        for (int b = 0; b < RB; ++b)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    mine[member * kSize + (8 * n + 2 * t + (i & 1)) * kRows + 16 * b + r + 8 * (i >> 1)] = sum[b][n][i];
-        if (p.team == 1)
-            __syncwarp();
-        else
-            named_bar(1 + team, 32 * p.team);
-        for (int i = 32 * member + lane; i < kSize; i += 32 * p.team) {
-            const int m = i / kRows, n = g * kRows + i % kRows;
-            if (m >= p.M || n >= p.N) continue;
-            float v = 0.0f;
-            for (int q = 0; q < p.team; ++q) v += mine[q * kSize + i];
-            p.y[static_cast<int64_t>(m) * p.N + n] = 8.0f * v;  // (weights counted in eighths)
         }
     }
     if (*static_cast<volatile int *>(&abort_flag)) {  // copies in flight get time to land
@@ -346,13 +342,15 @@ int gemv_launch(W4Params p, DeviceState &ds, cudaStream_t s) {
     // teams of up to eight; no more warps than tiles.
     p.team = p.groups <= ds.num_sms ? WARPS : 8;
     while (p.team > p.kt) p.team = p.team > 8 ? 8 : p.team / 2;
+    // As few stages of a group as give a warp at most four tiles in each (x from
+    // global memory: one, as the rest of the SM's memory caches it) and fit.
     const int x = XS ? p.x_stride * p.M : 0;
-    p.per_stage = XS ? 4 : 1;  // (x from global memory: the rest of the SM's memory caches it)
-    const auto bytes = [&] {
-        return WARPS * (kStages * p.per_stage * tile_bytes<GROUP, RB>() + part_bytes<NT, RB>()) + x;
-    };
-    while (p.per_stage > 1 && (bytes() > kMaxSmem || p.per_stage * p.team > p.kt)) p.per_stage /= 2;
-    return launch_dependent(fn, dim3(grid), 32 * WARPS, bytes(), s, 1, "launch gemv_w4_kernel", p);
+    const int rest = kMaxSmem - x - WARPS * part_bytes<NT, RB>();
+    const int most = std::max(1, std::min(XS ? 4 : 1, rest / (WARPS * kStages * tile_bytes<GROUP, RB>())));
+    const int stages = (p.kt + p.team * most - 1) / (p.team * most);
+    p.per = (p.kt + p.team * stages - 1) / (p.team * stages);
+    const size_t smem = WARPS * (part_bytes<NT, RB>() + kStages * p.per * tile_bytes<GROUP, RB>()) + x;
+    return launch_dependent(fn, dim3(grid), 32 * (WARPS + 1), smem, s, 1, "launch gemv_w4_kernel", p);
 }
 
 // x goes to shared memory where it leaves room for the ring.
