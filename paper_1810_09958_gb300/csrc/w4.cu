@@ -353,23 +353,28 @@ int gemv_launch(W4Params p, DeviceState &ds, cudaStream_t s) {
     return launch_dependent(fn, dim3(grid), 32 * (WARPS + 1), smem, s, 1, "launch gemv_w4_kernel", p);
 }
 
-// x goes to shared memory where it leaves room for the ring.
-template <int NT, int GROUP, int RB, int WARPS>
+// x goes to shared memory where it leaves room for the ring: RB and WARPS of the
+// kernel that has it there, and of the one that reads it through the L1 cache
+// (two blocks of rows share what is read).  Measured, us, with (RB, warps):
+// 16 x 14336 x 4096 (fits) (1, 16) 14.3, (2, 8) 15.8; 16 x 8192 x 8192 (does not)
+// 25.9, 20.6; 32 x 14336 x 2048 (fits) (1, 8) 14.6, (2, 8) 16.7, (1, 16) 20.3;
+// 32 x 8192 x 8192 (does not) 43.0, 37.9, 52.2.
+template <int NT, int GROUP, int RB, int WARPS, int RB_L1, int WARPS_L1>
 int gemv_x(W4Params p, DeviceState &ds, cudaStream_t s) {
     p.x_stride = p.kt * 256 + 64;
     const int64_t rest = WARPS * (kStages * tile_bytes<GROUP, RB>() + part_bytes<NT, RB>());
     if (static_cast<int64_t>(p.x_stride) * p.M + rest <= kMaxSmem) return gemv_launch<NT, GROUP, RB, true, WARPS>(p, ds, s);
-    return gemv_launch<NT, GROUP, RB, false, WARPS>(p, ds, s);
+    return gemv_launch<NT, GROUP, RB_L1, false, WARPS_L1>(p, ds, s);
 }
 
 template <int NT, int GROUP>
 int gemv_rows(const W4Params &p, DeviceState &ds, cudaStream_t s) {
     if constexpr (NT == 1) {
-        return gemv_x<1, GROUP, 1, 16>(p, ds, s);
+        return gemv_x<1, GROUP, 1, 16, 1, 16>(p, ds, s);
     } else if constexpr (NT == 2) {
-        return gemv_x<2, GROUP, 1, 16>(p, ds, s);
+        return gemv_x<2, GROUP, 1, 16, 2, 8>(p, ds, s);
     } else {
-        return gemv_x<4, GROUP, 2, 8>(p, ds, s);
+        return gemv_x<4, GROUP, 1, 8, 2, 8>(p, ds, s);
     }
 }
 

@@ -100,6 +100,14 @@ def test_sizes(M, N, K, group):
     check(M, N, K, group, seed=N + K)
 
 
+@pytest.mark.parametrize("M,N,K,group", [(8, 40, 16384, 32), (9, 50, 8200, 64), (16, 33, 9000, 32), (17, 65, 4104, 128),
+                                         (32, 100, 5000, 32), (1, 2500, 264, 64), (3, 4900, 40, 32), (20, 2600, 136, 128)])
+def test_x_that_fits_and_x_that_does_not(M, N, K, group):
+    """x beside the ring in shared memory, and x too large for it; teams of one,
+    two, four and eight warps."""
+    check(M, N, K, group, seed=M + N + K)
+
+
 @pytest.mark.parametrize("M,N,K,group", [(1, 160, 1024, 32), (8, 1001, 520, 64), (32, 64, 2048, 128), (3, 7, 40, 32)])
 def test_integer_data_is_exact(M, N, K, group):
     check(M, N, K, group, seed=77, exact=True)
