@@ -55,22 +55,34 @@ constexpr int kStages = 2;  // tiles of each input in a warp's ring
 // one fp32 channel a lane (128 x 32 x 1024 forward, 20001 x 2 x 1760 backward):
 // 8 warps of 16 / 8 steps 10.5, 189; 4 warps, 4 CTAs an SM 9.5, 224; 8 warps of
 // 32 / 16 steps 10.4, 201.
-template <int V, bool BACK>
+// Rows that TMA does not bring cost the warps more instructions a step, and more
+// warps hide them: 4 warps of 32 / 16 steps and 8 of 16 / 8, 7791 x 3 x 2042
+// backward 202, 121; 3104 x 1 x 1757 forward 29, 24; 4096 x 8 x 1022 backward
+// 108, 112.
+template <int V, bool BACK, bool TMA>
 struct Shape;
 template <>
-struct Shape<2, false> {
+struct Shape<2, false, true> {
     static constexpr int kWarps = 4, kCtas = 2, kSteps = 32;
 };
 template <>
-struct Shape<2, true> {
+struct Shape<2, true, true> {
     static constexpr int kWarps = 4, kCtas = 2, kSteps = 16;
 };
 template <>
-struct Shape<1, false> {
-    static constexpr int kWarps = 4, kCtas = 4, kSteps = 16;
+struct Shape<2, false, false> {
+    static constexpr int kWarps = 8, kCtas = 2, kSteps = 16;
 };
 template <>
-struct Shape<1, true> {
+struct Shape<2, true, false> {
+    static constexpr int kWarps = 8, kCtas = 2, kSteps = 8;
+};
+template <bool TMA>
+struct Shape<1, false, TMA> {
+    static constexpr int kWarps = 4, kCtas = 4, kSteps = 16;
+};
+template <bool TMA>
+struct Shape<1, true, TMA> {
     static constexpr int kWarps = 8, kCtas = 2, kSteps = 8;
 };
 constexpr int kStepThreads = 128;
@@ -537,15 +549,15 @@ __device__ __forceinline__ void put_edge(float *to, const Group<V> &g, const Lan
 }
 
 template <typename G, typename Hy, int V, int L, Rows ROWS>
-__global__ void __launch_bounds__(32 * Shape<V, false>::kWarps, Shape<V, false>::kCtas)
+__global__ void __launch_bounds__(32 * Shape<V, false, ROWS == kTma>::kWarps, (Shape<V, false, ROWS == kTma>::kCtas))
     glr_forward_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_h,
                        const __grid_constant__ ScanParams p) {
     if (p.cluster > 1 && !launch_shape_ok(p.err, p.cluster, gridDim.x, 0x601u)) return;
     constexpr bool TMA = ROWS == kTma;
     using Tiles = ForwardTiles<G, Hy, V, L, ROWS>;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ FoldBuffers<V, Shape<V, false>::kWarps> folds;
-    __shared__ uint64_t full_all[Shape<V, false>::kWarps][kStages];
+    __shared__ FoldBuffers<V, Shape<V, false, ROWS == kTma>::kWarps> folds;
+    __shared__ uint64_t full_all[Shape<V, false, ROWS == kTma>::kWarps][kStages];
     const WaitCtx wait{p.timeout_ns, p.err, &folds.abort};
     const Warp w(p);
     Tiles &mine = reinterpret_cast<Tiles *>(smem)[w.warp];
@@ -680,7 +692,7 @@ __global__ void __launch_bounds__(32 * Shape<V, false>::kWarps, Shape<V, false>:
 }
 
 template <typename G, typename Hy, int V, int L, Rows ROWS>
-__global__ void __launch_bounds__(32 * Shape<V, true>::kWarps, Shape<V, true>::kCtas)
+__global__ void __launch_bounds__(32 * Shape<V, true, ROWS == kTma>::kWarps, (Shape<V, true, ROWS == kTma>::kCtas))
     glr_backward_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_h,
                         const __grid_constant__ CUtensorMap tm_dh, const __grid_constant__ CUtensorMap tm_dg,
                         const __grid_constant__ ScanParams p) {
@@ -688,8 +700,8 @@ __global__ void __launch_bounds__(32 * Shape<V, true>::kWarps, Shape<V, true>::k
     constexpr bool TMA = ROWS == kTma;
     using Tiles = BackwardTiles<G, Hy, V, L, ROWS>;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ FoldBuffers<V, Shape<V, true>::kWarps> folds;
-    __shared__ uint64_t full_all[Shape<V, true>::kWarps][kStages];
+    __shared__ FoldBuffers<V, Shape<V, true, ROWS == kTma>::kWarps> folds;
+    __shared__ uint64_t full_all[Shape<V, true, ROWS == kTma>::kWarps][kStages];
     const WaitCtx wait{p.timeout_ns, p.err, &folds.abort};
     const Warp w(p);
     Tiles &mine = reinterpret_cast<Tiles *>(smem)[w.warp];
@@ -1103,7 +1115,7 @@ int scan_shape(const void *fn, const GlrDesc &d, int smem, const DeviceState &ds
 
 template <typename G, typename Hy, int V, Rows ROWS>
 int forward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
-    using S = Shape<V, false>;
+    using S = Shape<V, false, ROWS == kTma>;
     constexpr int L = S::kSteps;
     const auto fn = glr_forward_kernel<G, Hy, V, L, ROWS>;
     ScanParams p{};
@@ -1121,7 +1133,7 @@ int forward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
 
 template <typename G, typename Hy, int V, Rows ROWS>
 int backward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
-    using S = Shape<V, true>;
+    using S = Shape<V, true, ROWS == kTma>;
     constexpr int L = S::kSteps;
     const auto fn = glr_backward_kernel<G, Hy, V, L, ROWS>;
     ScanParams p{};
