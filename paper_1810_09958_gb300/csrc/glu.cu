@@ -81,6 +81,39 @@ __device__ __forceinline__ void tile_coords(int tile, const GluParams &p, int &m
     nt = local / gm;
 }
 
+// ---- issue of the pair's MMAs.  A whole warp runs the loop and one elected lane
+// issues, so that addresses stay in uniform registers, and a matrix descriptor is
+// two words of which only the lower one changes: with 64-bit descriptors built by
+// one lane, the issuing thread took 640 cycles a 64-deep block whatever the
+// tile's width, more than the 512 of the MMAs of the widest.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(p));
+    return p != 0;
+}
+
+// The words of sdesc_sw128 (ptx.cuh): K-major operands 16 and MN-major ones 8192
+// bytes between their chunks, 1024 between groups of eight rows or k.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t saddr, bool mn) {
+    return (saddr >> 4) | ((mn ? 8192u >> 4 : 16u >> 4) << 16);
+}
+__device__ __forceinline__ void umma_pair_words(uint32_t d_tmem, uint32_t a_low, uint32_t b_low, uint32_t idesc,
+                                                uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 a, {%1, %4};\n\t"
+        "mov.b64 b, {%2, %4};\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_low), "r"(b_low), "r"(idesc), "r"(kDescHigh), "r"(accumulate)
+        : "memory");
+}
+
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     uint32_t w;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
@@ -226,6 +259,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             int stage = 0;
             uint32_t phase = 0;
             bool ok = true;
+            const uint32_t full_at = mapa_shared(smem_u32(full), 0u);
             for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
                 const Item it = item(tile);
                 const int nt = it.nt;
@@ -239,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         break;
                     }
                     if (leader) mbar_arrive_expect_tx(&full[stage], 2u * (kAStage + kBStage));
-                    const uint32_t fb = mapa_shared(smem_u32(&full[stage]), 0u);
+                    const uint32_t fb = full_at + 8 * stage;
                     uint8_t *a = sA + static_cast<size_t>(stage) * kAStage;
                     uint8_t *b = sB + static_cast<size_t>(stage) * kBStage;
                     const int k0 = kb * kBK;
@@ -266,13 +300,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
     } else if (warp == 1) {
         // ------------------------------------------------ MMA issuer (first CTA)
-        if (lane == 0 && leader) {
+        if (leader) {
             const uint32_t idesc = idesc_bf16_f32(kPM, BN, A_MN, B_MN);
+            const bool one = elect_one();
+            constexpr uint32_t kStepA = (A_MN ? 2048 : 32) >> 4, kStepB = (B_MN ? 2048 : 32) >> 4;
+            const uint32_t a_first = desc_low(smem_u32(sA), A_MN), b_first = desc_low(smem_u32(sB), B_MN);
             int stage = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0;
             bool ok = true, issued = false;
             for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
-                if (!bounded_wait<true>(&tempty[acc], acc_phase ^ 1u, w, SITE_U_TEMPTY)) {
+                if (!warp_wait<true>(&tempty[acc], acc_phase ^ 1u, w, SITE_U_TEMPTY)) {
                     ok = false;
                     break;
                 }
@@ -281,37 +318,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const Item it = item(tile);
                 const int kbs = it.kb1 - it.kb0;
                 for (int kb = 0; kb < kbs; ++kb) {
-                    if (!bounded_wait<true>(&full[stage], phase, w, SITE_U_FULL)) {
+                    if (!warp_wait<true>(&full[stage], phase, w, SITE_U_FULL)) {
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t a0 = smem_u32(sA + static_cast<size_t>(stage) * kAStage);
-                    const uint32_t b0 = smem_u32(sB + static_cast<size_t>(stage) * kBStage);
+                    const uint32_t a = a_first + stage * (kAStage >> 4), b = b_first + stage * (kBStage >> 4);
+                    if (one) {
 #pragma unroll
-                    for (int k = 0; k < kBK / 16; ++k) {
-                        const uint64_t ad =
-                            A_MN ? sdesc_sw128(a0 + k * 2048, 8192, 1024) : sdesc_sw128(a0 + k * 32, 16, 1024);
-                        const uint64_t bd =
-                            B_MN ? sdesc_sw128(b0 + k * 2048, 8192, 1024) : sdesc_sw128(b0 + k * 32, 16, 1024);
-                        umma_bf16_pair(d, ad, bd, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                        for (int k = 0; k < kBK / 16; ++k)
+                            umma_pair_words(d, a + k * kStepA, b + k * kStepB, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                        umma_commit_pair(&empty[stage], kBoth);
                     }
                     issued = true;
-                    umma_commit_pair(&empty[stage], kBoth);
                     if (++stage == ST) {
                         stage = 0;
                         phase ^= 1u;
                     }
                 }
                 if (!ok) break;
-                umma_commit_pair(&tfull[acc], kBoth);
+                if (one) umma_commit_pair(&tfull[acc], kBoth);
                 if (++acc == 2) {
                     acc = 0;
                     acc_phase ^= 1u;
                 }
             }
             // Every MMA of this thread has completed before TMEM can be freed.
-            if (issued) {
+            if (issued && one) {
                 umma_commit_pair(mq, 0x1);
                 drain_wait(mq, 0, p.timeout_ns);
             }
