@@ -255,27 +255,28 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool aborted = false;
     if (warp == 0) {
         // ------------------------------------------------ TMA producer (both CTAs)
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            const uint32_t full_at = mapa_shared(smem_u32(full), 0u);
-            for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
-                const Item it = item(tile);
-                const int nt = it.nt;
-                const int arow = it.mt * kPM + static_cast<int>(rank) * kHalf;
-                // Projections: this CTA's rows of W are the tile's gate rows or its up rows.
-                const int bcol = ROLE == PRODUCT || ROLE == PRODUCT_FEW ? nt * BN + static_cast<int>(rank) * kBHalf
-                                                 : nt * kBHalf + (leader ? 0 : p.F);
-                for (int kb = it.kb0; kb < it.kb1; ++kb) {
-                    if (!bounded_wait<true>(&empty[stage], phase ^ 1u, w, SITE_U_EMPTY)) {
-                        ok = false;
-                        break;
-                    }
+        const bool one = elect_one();
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        const uint32_t full_at = mapa_shared(smem_u32(full), 0u);
+        for (int tile = pair; ok && tile < num_tiles; tile += num_pairs) {
+            const Item it = item(tile);
+            const int nt = it.nt;
+            const int arow = it.mt * kPM + static_cast<int>(rank) * kHalf;
+            // Projections: this CTA's rows of W are the tile's gate rows or its up rows.
+            const int bcol = ROLE == PRODUCT || ROLE == PRODUCT_FEW ? nt * BN + static_cast<int>(rank) * kBHalf
+                                                                    : nt * kBHalf + (leader ? 0 : p.F);
+            for (int kb = it.kb0; kb < it.kb1; ++kb) {
+                if (!warp_wait<true>(&empty[stage], phase ^ 1u, w, SITE_U_EMPTY)) {
+                    ok = false;
+                    break;
+                }
+                if (one) {
                     if (leader) mbar_arrive_expect_tx(&full[stage], 2u * (kAStage + kBStage));
                     const uint32_t fb = full_at + 8 * stage;
-                    uint8_t *a = sA + static_cast<size_t>(stage) * kAStage;
-                    uint8_t *b = sB + static_cast<size_t>(stage) * kBStage;
+                    uint8_t *a = sA + stage * kAStage;
+                    uint8_t *b = sB + stage * kBStage;
                     const int k0 = kb * kBK;
                     if (A_MN) {
                         tma_load_2d_pair(&tmA, fb, a, arow, k0);
@@ -289,14 +290,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                     } else {
                         tma_load_2d_pair(&tmB, fb, b, k0, bcol);
                     }
-                    if (++stage == ST) {
-                        stage = 0;
-                        phase ^= 1u;
-                    }
+                }
+                if (++stage == ST) {
+                    stage = 0;
+                    phase ^= 1u;
                 }
             }
-            aborted = !ok;
         }
+        aborted = !ok;
         __syncwarp();
     } else if (warp == 1) {
         // ------------------------------------------------ MMA issuer (first CTA)
