@@ -621,11 +621,12 @@ int project_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     return pair_launch<ROLE, BN, false, false>(p, a, b, c, c2, ds, s);
 }
 
-// 256 tokens x 128, 64 or 32 features a tile.  A round of tiles takes much the
-// same time at every width (0.31 us a 64-wide block of D), so narrower tiles are
-// taken only where all of them are one round.  Measured, us at 32 / 64 / 128
-// features: 100 x 4096 x 512 21.7 / 22.4 / 23.4, 200 x 1760 x 4096 21.0 / 13.8 /
-// 14.5, 2000 x 2560 x 7680 311 / 163 / 94.
+// 256 tokens x 128, 64 or 32 features a tile: a round of narrow tiles takes less
+// time than one of wide ones, but not in proportion (a block's loads and issue
+// cost the same), so they are taken where all of them are one round.  Measured,
+// us at 32 / 64 / 128 features: 100 x 4096 x 1024 14.6 / 15.6 / 22.6, 200 x 1760 x
+// 4096 14.6 / 11.2 / 14.1, 700 x 2560 x 3000 32 / 21 / 19, 2000 x 2560 x 7680 184 /
+// 102 / 87.
 template <Role ROLE>
 int project(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
     const int pairs = std::max(1, gemm_cluster_capacity(ds, 2));
@@ -865,24 +866,30 @@ struct Cut {
     }
 };
 
-// Rounds are counted in 64-wide blocks of K: a round of tiles takes the same time
-// at every width (a stage's loads do, measured 0.31 us at 64 to 256 columns), so
-// wide tiles are taken unless narrower ones need no more rounds; a last round
-// with less than half the pairs busy is split over K, which costs about 16
-// blocks' time for its parts.
+// Estimated time, ns: a 64-wide block of K takes a pair 270, 215 or 165 at widths
+// 256, 192 and 128 (the wide one is the tensor cores' rate, the narrow ones the
+// issuing threads'), a round of tiles 800 beside its blocks, and parts 4500 (their
+// sums are a kernel of their own).  A last round with less than half the pairs
+// busy may be split over K.  Measured against this choice, dx with its
+// projections, us at 128 / 192 / 256 whole and as chosen: 360 x 920 x 1744 17.6 /
+// 19.8 / 20.2 and 17.6; 200 x 1760 x 8192 37 / 41 / 50 and 30; 4096 x 2560 x 15360
+// 395 / 358 / 386 and 345.
 Cut cut_product(int64_t M, int N, int64_t K) {
     const int kb = tiles_of(K, kBK);
+    constexpr int64_t kRound = 800, kParts = 4500;
     Cut best{};
     int64_t best_cost = 0;
-    for (const int width : {256, 192, 128}) {
+    const int64_t block_ns[3] = {270, 215, 165};
+    for (int i = 0; i < 3; ++i) {
+        const int width = 256 - 64 * i;
         const int64_t tiles = static_cast<int64_t>(tiles_of(M, kPM)) * tiles_of(N, width);
-        const int64_t rest = tiles % kPairs;
+        const int64_t rest = tiles % kPairs, whole = kb * block_ns[i] + kRound;
         Cut c{width, static_cast<int>(std::min<int64_t>(tiles, 0x3fffffff)), 0, 1, kb};
-        int64_t cost = (tiles + kPairs - 1) / kPairs * kb;
+        int64_t cost = (tiles + kPairs - 1) / kPairs * whole;
         const int splits = rest ? static_cast<int>(std::min<int64_t>({kPairs / rest, kMaxSplits, kb / 8})) : 1;
         if (splits > 1) {
             const int kb_split = tiles_of(kb, splits);
-            const int64_t split_cost = tiles / kPairs * kb + kb_split + 16;
+            const int64_t split_cost = tiles / kPairs * whole + kb_split * block_ns[i] + kRound + kParts;
             if (split_cost < cost) {
                 cost = split_cost;
                 c = Cut{width, static_cast<int>(tiles - rest), static_cast<int>(rest), tiles_of(kb, kb_split), kb_split};

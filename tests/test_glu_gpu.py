@@ -141,7 +141,7 @@ def test_backward_shapes(T, D, F):
 
 
 @pytest.mark.parametrize("T,D,F", [(300, 4360, 1400), (270, 2056, 520), (129, 264, 4096), (128, 520, 2048),
-                                   (2300, 1032, 264), (90, 8, 4096), (1300, 520, 1536 + 8)])
+                                   (2300, 1032, 264), (90, 8, 4096), (1300, 520, 1536 + 8), (2400, 2056, 2048)])
 def test_backward_split_sums(T, D, F):
     """Shapes whose products leave a round of tiles part empty, so that tiles are
     summed in parts: whole rounds before them, none before them, edges in them."""
