@@ -16,7 +16,8 @@
 // a cluster walks its channels' time axis in rounds of (CTAs x warps x L)
 // steps, then takes the next channels (the grid is no larger than what is
 // resident).  Each warp has its own ring of tiles in shared memory, filled by
-// TMA (where rows are not on 16-byte boundaries: by asynchronous copies), so the loads of later rounds stay in flight
+// TMA (where rows are not on 16-byte boundaries: by asynchronous copies), so the
+// loads of later rounds stay in flight
 // while a round is folded; states leave through shared memory and TMA as well.
 // With gates loaded straight into registers the forward kernel spent 34
 // instructions an element, half of them addresses, and stopped at 55% of the
@@ -86,7 +87,7 @@ struct Shape<1, true, TMA> {
     static constexpr int kWarps = 8, kCtas = 2, kSteps = 8;
 };
 constexpr int kStepThreads = 128;
-constexpr int kWalkBlock = 8;
+constexpr int kWalkBlock = 8, kWalkBack = 4;  // steps of a block, forward and backward
 
 // V neighbouring elements, moved as one word.
 template <int BYTES>
@@ -548,6 +549,11 @@ __device__ __forceinline__ void put_edge(float *to, const Group<V> &g, const Lan
         if (i < g.left) to[g.chain + i] = v[i];
 }
 
+// Forward.  Bound by HBM where sequences are long (65536 x 1 x 2560 bf16 169 us,
+// 5.9 TB/s, 0.87 of the copy bandwidth), by the chain of one round's folds
+// through a cluster where they are short (128 x 32 x 1024, fp32 gates, 9.8 us,
+// 0.64), and without TMA by the instructions that copy and store words
+// (777 x 6 x 1001, fp32, ragged, 13.9 us, 0.33).
 template <typename G, typename Hy, int V, int L, Rows ROWS>
 __global__ void __launch_bounds__(32 * Shape<V, false, ROWS == kTma>::kWarps, (Shape<V, false, ROWS == kTma>::kCtas))
     glr_forward_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_h,
@@ -691,6 +697,9 @@ __global__ void __launch_bounds__(32 * Shape<V, false, ROWS == kTma>::kWarps, (S
     exchange_end(folds, p.cluster);
 }
 
+// Backward: four values a step in, two out.  Bound by HBM: 4096 x 8 x 1024 bf16
+// 63 us (6.4 TB/s, 0.94 of the copy bandwidth), 20001 x 2 x 1760 with fp32 gates,
+// ragged, 194 us (0.91).
 template <typename G, typename Hy, int V, int L, Rows ROWS>
 __global__ void __launch_bounds__(32 * Shape<V, true, ROWS == kTma>::kWarps, (Shape<V, true, ROWS == kTma>::kCtas))
     glr_backward_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_h,
@@ -870,117 +879,146 @@ __global__ void __launch_bounds__(32 * Shape<V, true, ROWS == kTma>::kWarps, (Sh
 }
 
 // Few steps, or channels enough to fill the GPU by themselves: one thread walks
-// the time of its V channels, eight steps' loads in flight.
+// the time of its V channels, a block of steps' loads in flight.  Bound by HBM
+// where the gates are fp32, by the instructions of an element in bf16: 8 x 2000 x
+// 2048 bf16 forward 43 us (0.79 of the copy bandwidth), backward 80 us (0.82);
+// 96 x 2000 x 1024 188 us (0.94) and 371 us (0.95), with fp32 gates 278 us (1.05)
+// and 574 us (1.01).  Blocks of eight steps backward, whose four values a step
+// leave a third fewer threads in the registers, took 8 x 2000 x 2048 91 us.
+struct Walker {
+    int64_t b, chain;  // sequence, first channel of it all
+    int len;
+    __device__ __forceinline__ Walker(const GlrDesc &d, int64_t i, int V) {
+        const int per = d.hidden / V;  // (a row of `per` threads is one of `hidden` channels)
+        b = i >> 32 ? i / per : static_cast<uint32_t>(i) / static_cast<uint32_t>(per);
+        chain = i * V;
+        len = d.lengths ? min(max(d.lengths[b], 0), d.T) : d.T;
+    }
+};
+template <int V>
+__device__ __forceinline__ Lane<V> walk_edge(const float *from, int64_t chain) {
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = from ? from[chain + i] : 0.0f;
+    return Lane<V>(v);
+}
+template <int V>
+__device__ __forceinline__ void walk_edge(float *to, int64_t chain, const Lane<V> &x) {
+    float v[V];
+    x.get(v);
+#pragma unroll
+    for (int i = 0; i < V; ++i) to[chain + i] = v[i];
+}
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load_pack(const T *p) {
+    Pack<T, V> v;
+    v.w = *reinterpret_cast<const typename Pack<T, V>::W *>(p);
+    return v;
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_pack(T *p, const Lane<V> &x) {
+    Pack<T, V> v;
+    narrow<T, V>(v, x);
+    *reinterpret_cast<typename Pack<T, V>::W *>(p) = v.w;
+}
+
 template <typename G, typename Hy, int V>
-__global__ void __launch_bounds__(kStepThreads)
+__global__ void __launch_bounds__(kStepThreads, V == 1 ? 8 : 6)
     glr_walk_forward_kernel(const __grid_constant__ GlrDesc d, int64_t threads) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kStepThreads + threadIdx.x;
     if (i >= threads) return;
     dependent_start();
-    const int per = d.hidden / V;
-    const int64_t b = i / per, chain = i * V;  // (a row of `per` threads is one of `hidden` channels)
-    const int64_t step = static_cast<int64_t>(d.batch) * d.hidden;
-    int len = d.T;
-    if (d.lengths) len = min(max(d.lengths[b], 0), d.T);
-    float h[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = d.h0 ? d.h0[chain + v] : 0.0f;
-    const G *g = static_cast<const G *>(d.g) + chain + b * d.hidden;
-    Hy *out = static_cast<Hy *>(d.h_out) + chain;
-    for (int t = 0; t < d.T; t += kWalkBlock) {
+    const Walker w(d, i, V);
+    const int hidden = d.hidden;
+    const int64_t step = static_cast<int64_t>(d.batch) * hidden;
+    Lane<V> h = walk_edge<V>(d.h0, w.chain);
+    const G *g = static_cast<const G *>(d.g) + w.chain + w.b * hidden;
+    Hy *out = static_cast<Hy *>(d.h_out) + w.chain;
+    const auto block = [&](int t, bool whole) {
         Pack<G, V> z[kWalkBlock], n[kWalkBlock];
 #pragma unroll
-        for (int k = 0; k < kWalkBlock; ++k)
-            if (t + k < len) {
-                const G *q = g + 2 * step * (t + k);
-                z[k].w = *reinterpret_cast<const typename Pack<G, V>::W *>(q);
-                n[k].w = *reinterpret_cast<const typename Pack<G, V>::W *>(q + d.hidden);
+        for (int k = 0; k < kWalkBlock; ++k, g += 2 * step)
+            if (whole || t + k < w.len) {
+                z[k] = load_pack<G, V>(g);
+                n[k] = load_pack<G, V>(g + hidden);
             }
 #pragma unroll
-        for (int k = 0; k < kWalkBlock; ++k)
-            if (t + k < d.T) {
-                Pack<Hy, V> o;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    if (t + k < len) {
-                        const Gate s = gate(to_f32(z[k].v[v]));
-                        h[v] = s.keep * h[v] + s.take * to_f32(n[k].v[v]);
-                    }
-                    o.v[v] = from_f32<Hy>(t + k < len ? h[v] : 0.0f);
-                }
-                *reinterpret_cast<typename Pack<Hy, V>::W *>(out + step * (t + k)) = o.w;
+        for (int k = 0; k < kWalkBlock; ++k, out += step) {
+            if (!whole && t + k >= d.T) break;
+            if (whole || t + k < w.len) {
+                const Gates<V> s(widen_from_minus_87<G, V>(z[k]));
+                h = fma(s.keep, h, mul(s.take, widen<G, V>(n[k])));
+                store_pack<Hy, V>(out, h);
+            } else {
+                store_pack<Hy, V>(out, Lane<V>(0.0f));
             }
-    }
-    if (d.h_last) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) d.h_last[chain + v] = h[v];
-    }
+        }
+    };
+    int t = 0;
+#pragma unroll 1
+    for (; t + kWalkBlock <= w.len; t += kWalkBlock) block(t, true);
+#pragma unroll 1
+    for (; t < d.T; t += kWalkBlock) block(t, false);
+    if (d.h_last) walk_edge<V>(d.h_last, w.chain, h);
 }
 
 template <typename G, typename Hy, int V>
-__global__ void __launch_bounds__(kStepThreads)
+__global__ void __launch_bounds__(kStepThreads, V == 1 ? 8 : 6)
     glr_walk_backward_kernel(const __grid_constant__ GlrDesc d, int64_t threads) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kStepThreads + threadIdx.x;
     if (i >= threads) return;
     dependent_start();
-    const int per = d.hidden / V;
-    const int64_t b = i / per, chain = i * V;
-    const int64_t step = static_cast<int64_t>(d.batch) * d.hidden;
-    int len = d.T;
-    if (d.lengths) len = min(max(d.lengths[b], 0), d.T);
-    float e[V], h0[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        e[v] = d.dh_last ? d.dh_last[chain + v] : 0.0f;
-        h0[v] = d.h0 ? d.h0[chain + v] : 0.0f;
-    }
-    const G *g = static_cast<const G *>(d.g) + chain + b * d.hidden;
-    G *dg = static_cast<G *>(d.dg) + chain + b * d.hidden;
-    const Hy *hs = static_cast<const Hy *>(d.h_in) + chain, *dh = static_cast<const Hy *>(d.dh_out) + chain;
+    const Walker w(d, i, V);
+    const int hidden = d.hidden;
+    const int64_t step = static_cast<int64_t>(d.batch) * hidden;
+    Lane<V> e = walk_edge<V>(d.dh_last, w.chain);
+    const Lane<V> h0 = walk_edge<V>(d.h0, w.chain);
     const bool has_dh = d.dh_out != nullptr;
-    for (int t = d.T - 1; t >= 0; t -= kWalkBlock) {
-        Pack<G, V> z[kWalkBlock], n[kWalkBlock];
-        Pack<Hy, V> before[kWalkBlock], own[kWalkBlock];
+    const int64_t at_g = w.chain + w.b * hidden;
+    const auto block = [&](int t, bool whole) {  // steps t, t - 1, ...
+        Pack<G, V> z[kWalkBack], n[kWalkBack];
+        Pack<Hy, V> before[kWalkBack], own[kWalkBack];
+        const G *g = static_cast<const G *>(d.g) + at_g + 2 * step * t;
+        const Hy *hs = static_cast<const Hy *>(d.h_in) + w.chain + step * (t - 1);
+        const Hy *dh = static_cast<const Hy *>(d.dh_out) + w.chain + step * t;
 #pragma unroll
-        for (int k = 0; k < kWalkBlock; ++k)
-            if (t - k >= 0 && t - k < len) {
-                const G *q = g + 2 * step * (t - k);
-                z[k].w = *reinterpret_cast<const typename Pack<G, V>::W *>(q);
-                n[k].w = *reinterpret_cast<const typename Pack<G, V>::W *>(q + d.hidden);
-                if (t - k > 0)
-                    before[k].w = *reinterpret_cast<const typename Pack<Hy, V>::W *>(hs + step * (t - k - 1));
-                if (has_dh) own[k].w = *reinterpret_cast<const typename Pack<Hy, V>::W *>(dh + step * (t - k));
+        for (int k = 0; k < kWalkBack; ++k, g -= 2 * step, hs -= step, dh -= step)
+            if (whole || (t - k >= 0 && t - k < w.len)) {
+                z[k] = load_pack<G, V>(g);
+                n[k] = load_pack<G, V>(g + hidden);
+                if (whole || t - k > 0) before[k] = load_pack<Hy, V>(hs);
+                if (has_dh) own[k] = load_pack<Hy, V>(dh);
             }
+        G *dg = static_cast<G *>(d.dg) + at_g + 2 * step * t;
 #pragma unroll
-        for (int k = 0; k < kWalkBlock; ++k)
-            if (t - k >= 0) {
-                Pack<G, V> dz, dn;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    float a = 0.0f, c = 0.0f;
-                    if (t - k < len) {
-                        const Gate s = gate(to_f32(z[k].v[v]));
-                        const float prior = t - k > 0 ? to_f32(before[k].v[v]) : h0[v];
-                        const float all = (has_dh ? to_f32(own[k].v[v]) : 0.0f) + e[v];
-                        a = all * (prior - to_f32(n[k].v[v])) * (s.keep * s.take);
-                        c = all * s.take;
-                        e[v] = s.keep * all;
-                    }
-                    dz.v[v] = from_f32<G>(a);
-                    dn.v[v] = from_f32<G>(c);
-                }
-                G *q = dg + 2 * step * (t - k);
-                *reinterpret_cast<typename Pack<G, V>::W *>(q) = dz.w;
-                *reinterpret_cast<typename Pack<G, V>::W *>(q + d.hidden) = dn.w;
+        for (int k = 0; k < kWalkBack; ++k, dg -= 2 * step) {
+            if (!whole && t - k < 0) break;
+            Lane<V> dz(0.0f), dn(0.0f);
+            if (whole || t - k < w.len) {
+                const Gates<V> s(widen_from_minus_87<G, V>(z[k]));
+                const Lane<V> prior = whole || t - k > 0 ? widen<Hy, V>(before[k]) : h0;
+                const Lane<V> all = has_dh ? add(widen<Hy, V>(own[k]), e) : e;
+                dz = mul(all, mul(fma(widen<G, V>(n[k]), Lane<V>(-1.0f), prior), mul(s.keep, s.take)));
+                dn = mul(all, s.take);
+                e = mul(s.keep, all);
             }
+            store_pack<G, V>(dg, dz);
+            store_pack<G, V>(dg + hidden, dn);
+        }
+    };
+#pragma unroll 1
+    for (int t = d.T - 1; t >= 0; t -= kWalkBack) {
+        if (t < w.len && t >= kWalkBack)
+            block(t, true);
+        else
+            block(t, false);
     }
-    if (d.dh0) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) d.dh0[chain + v] = e[v];
-    }
+    if (d.dh0) walk_edge<V>(d.dh0, w.chain, e);
 }
 
-// One token a sequence: one thread per V channels.
+// One token a sequence: one thread per V channels.  Bound by HBM, a few sequences
+// by the launch: 4096 sequences of 2048 bf16 19.9 us (5.9 TB/s, 0.87 of the copy
+// bandwidth), 32 of 1024 1.3 us.
 template <typename G, typename Hy, int V>
 __global__ void __launch_bounds__(kStepThreads)
     glr_step_kernel(int64_t threads, int hidden, int slots, const G *g, const int32_t *slot_ids, const float *state,
@@ -1151,13 +1189,17 @@ int backward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
                             "launch glr_backward_kernel", tg, th, tdh, tdg, p);
 }
 
-// Whether walking beats the scan.  Measured forward, us, walk against scan, 1024
-// bf16 channels: 8 steps of 300 sequences 5.5 / 14.5, 16 steps 8.4 / 14.5 and
-// 96 steps 50 / 37; 96 steps of 1500 sequences 185 / 181 (fp32 gates 223 / 345).
-// Without TMA the scan is slower: 96 steps of 300 sequences of 1023 channels
-// 49 / 95, of 16 sequences 12.9 / 8.5.
+// Whether walking beats the scan.  Measured, us, walk against scan, bf16 with rows
+// of 1024 channels, forward and backward: 12 steps of 64 sequences 3.3 / 5.1 and
+// 4.4 / 5.2; 32 steps of 64 6.2 / 5.9 and 11 / 8, of 128 7.7 / 9.2 and 13.4 / 12.9;
+// 96 steps of 300 36 / 36 and 69 / 66, of 600 61 / 67 and 118 / 126.  Without TMA the
+// scan is slower, rows of 1022: 96 steps of 16 sequences 8.5 / 4.5 and 23 / 8.9, of
+// 64 15.1 / 15.4 and 28 / 32; 300 steps of 64 42 / 48 and 78 / 85.
 bool walk(const GlrDesc &d, bool tma) {
-    return d.T <= 16 || static_cast<int64_t>(d.batch) * d.hidden >= (tma ? 1 << 20 : 1 << 17);
+    const int64_t channels = static_cast<int64_t>(d.batch) * d.hidden;
+    if (d.T <= 16) return true;
+    if (!tma) return channels >= 3 << 14;
+    return channels >= 1 << 19 || (d.T <= 32 && channels >= 1 << 17);
 }
 
 int walk_launch(void (*fn)(const GlrDesc, int64_t), const GlrDesc &d, int V, cudaStream_t s, const char *what) {
@@ -1180,7 +1222,7 @@ int glr_forward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
         if (walk(d, tma)) {
             const bool two = vector_ok(d.hidden, 2, d.g_type, d.g) && vector_ok(d.hidden, 2, d.h_type, d.h_out);
             return walk_launch(two ? glr_walk_forward_kernel<G, Hy, 2> : glr_walk_forward_kernel<G, Hy, 1>, d,
-                                two ? 2 : 1, s, "launch glr_walk_forward_kernel");
+                               two ? 2 : 1, s, "launch glr_walk_forward_kernel");
         }
         if (tma) return forward_launch<G, Hy, V, kTma>(d, ds, s);
         if constexpr (V == 2) {
@@ -1202,7 +1244,7 @@ int glr_backward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
             const bool two = vector_ok(d.hidden, 2, d.g_type, d.g) && vector_ok(d.hidden, 2, d.g_type, d.dg) &&
                              vector_ok(d.hidden, 2, d.h_type, d.h_in) && vector_ok(d.hidden, 2, d.h_type, d.dh_out);
             return walk_launch(two ? glr_walk_backward_kernel<G, Hy, 2> : glr_walk_backward_kernel<G, Hy, 1>, d,
-                                two ? 2 : 1, s, "launch glr_walk_backward_kernel");
+                               two ? 2 : 1, s, "launch glr_walk_backward_kernel");
         }
         if (tma) return backward_launch<G, Hy, V, kTma>(d, ds, s);
         if constexpr (V == 2) {

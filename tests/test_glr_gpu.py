@@ -188,6 +188,31 @@ def test_few_steps_and_many_channels(T, B, H, lengths, gt, ht):
     check_both(T, B, H, gt, ht, seed=T + B, lengths=lengths)
 
 
+@pytest.mark.parametrize("gt,ht", TYPES)
+@pytest.mark.parametrize("T,B,H,lengths", [(32, 128, 1024, None), (33, 128, 1024, None), (45, 50, 1001, "ragged"),
+                                           (41, 48, 1026, "ragged"), (30, 47, 1021, "ragged"), (25, 1025, 512, "ragged")])
+def test_either_side_of_the_choice(T, B, H, lengths, gt, ht):
+    check_both(T, B, H, gt, ht, seed=T + H,
+               lengths=lengths and [(7 * b) % (T + 1) for b in range(B)])
+
+
+@pytest.mark.parametrize("T", [3, 40])
+def test_gates_beyond_every_exponent(T):
+    """z = 0 and z = 1 from gates as large as they get, for few steps and many."""
+    import torch
+    B, H = 2, 64
+    for gate, want in ((-200.0, 3.0), (-float("inf"), 3.0), (200.0, 0.5), (float("inf"), 0.5)):
+        g = torch.empty(T, B, 2 * H, device="cuda")
+        g[:, :, :H], g[:, :, H:] = gate, 3.0
+        h0 = torch.full((B, H), 0.5, device="cuda")
+        out, last = torch.empty(T, B, H, device="cuda"), torch.empty(B, H, device="cuda")
+        isam.glr_forward(T, B, H, g, h0, None, out, last)
+        isam.sync()
+        # 1 - z is a product of two numbers good to 2^-22 each.
+        assert torch.allclose(out, torch.full_like(out, want), rtol=1e-6, atol=0.0)
+        assert torch.allclose(last, torch.full_like(last, want), rtol=1e-6, atol=0.0)
+
+
 def test_saturated_gates():
     """z = 1 to the last bit: the state stays h0 (what is taken of n, e^-40,
     is below a unit of it); z = 0: the state is the candidate."""
