@@ -17,9 +17,8 @@
 // steps, then takes the next channels (the grid is no larger than what is
 // resident).  Each warp has its own ring of tiles in shared memory, filled by
 // TMA (where rows are not on 16-byte boundaries: by asynchronous copies), so the
-// loads of later rounds stay in flight
-// while a round is folded; states leave through shared memory and TMA as well.
-// With gates loaded straight into registers the forward kernel spent 34
+// loads of later rounds stay in flight while a round is folded; states leave
+// through shared memory and TMA as well.  With gates loaded straight into registers the forward kernel spent 34
 // instructions an element, half of them addresses, and stopped at 55% of the
 // copy bandwidth.  Folds pass between warps through shared memory, between
 // CTAs through distributed shared memory (asynchronous stores counted on an

@@ -169,6 +169,17 @@ __device__ __forceinline__ void stage32(uint8_t *tile, int lane, int half, const
     }
 }
 
+// One warp of each CTA issues TMA, one of the pair the MMAs, four read the
+// accumulators (two of them, so that a tile's epilogue runs beside the next one's
+// MMAs).  Both issuing warps stay whole and elect a lane at each instruction, with
+// descriptors advanced as 32-bit words: from a single diverged thread a 64-deep
+// block took 644 cycles at every width, more than its MMAs (8192 x 4096 x 8192
+// 558 us, 200 x 1760 x 4096 13.8).  Bound by the tensor cores where tiles fill the
+// GPU: 8192 x 4096 x 8192 forward 542 us, 2030 TFLOP/s, 1.03 of the measured bf16
+// burst; 4096 x 2560 x 7680 backward, three launches of this kernel and one sum,
+// 496 to 524 us (box to box), 0.93 to 0.99.  By the chain of first loads, one round
+// of blocks and the epilogue where they do not: 200 x 1760 x 4096 11.7 us, 0.39 of
+// reading its bytes.
 template <Role ROLE, int BN, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kThreads, 1)
     glu_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -681,7 +692,8 @@ __device__ __forceinline__ float act_of(int act, float a, float &da) {
 // shared memory as a whole, rows 64 bytes off a multiple of 128.  The order of k
 // inside a product does not matter: lane 4 r + t holds eight consecutive k of rows
 // r and 8 + r, and of token r, sixteen bytes each, which are two instructions'
-// operands.
+// operands.  Bound by reading W: 1 x 2560 x 7680 16.5 us, 4.8 TB/s, 0.70 of the copy
+// bandwidth; 32 tokens 19.3 us.
 template <int NT, bool BACK>
 __global__ void __launch_bounds__(32 * kFewWarps, 1)
     glu_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ FewParams p) {
@@ -913,7 +925,8 @@ __device__ __forceinline__ float4 sum_parts(const float4 *at, int64_t step, int 
     return v;
 }
 
-// The split tiles' parts added in order, to bf16: four columns a thread.
+// The split tiles' parts added in order, to bf16: four columns a thread.  Bound by
+// reading the parts from L2 (2048 x 2560 of K 15360: 8.7 us under a profiler).
 __global__ void __launch_bounds__(kSumThreads)
     glu_sum_tiles_kernel(const __grid_constant__ GluParams p, int width, uint16_t *out) {
     dependent_start();
@@ -932,7 +945,8 @@ __global__ void __launch_bounds__(kSumThreads)
     *reinterpret_cast<uint2 *>(out + row * p.N + col) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
 }
 
-// parts [splits][quads * 4] added in order, to bf16.
+// parts [splits][quads * 4] added in order, to bf16 (bound by its launch: at most
+// 128 rows).
 __global__ void __launch_bounds__(kSumThreads) glu_sum_kernel(int64_t quads, int splits, const float4 *parts, uint2 *out) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kSumThreads + threadIdx.x;
     if (i >= quads) return;
@@ -1017,8 +1031,8 @@ __global__ void __launch_bounds__(kOuterThreads)
     unsigned long long sum[kOuterRows][4] = {};
 #pragma unroll 4
     for (int t = 0; t < T; ++t) {
-        const uint4 xv = __ldg(reinterpret_cast<const uint4 *>(x + static_cast<int64_t>(t) * D + col));
-        const uint4 dv = __ldg(reinterpret_cast<const uint4 *>(d + t * F2 + row0));  // 2F is a multiple of 16
+        const uint4 xv = *reinterpret_cast<const uint4 *>(x + static_cast<int64_t>(t) * D + col);
+        const uint4 dv = *reinterpret_cast<const uint4 *>(d + t * F2 + row0);  // 2F is a multiple of 16
         const uint32_t xw[4] = {xv.x, xv.y, xv.z, xv.w}, dw[4] = {dv.x, dv.y, dv.z, dv.w};
         unsigned long long xp[4];
 #pragma unroll
