@@ -867,7 +867,7 @@ int gated(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
 constexpr int kPairs = 76;  // of a GB300; the workspace's size does not ask the device
 constexpr int kMaxSplits = 16;
 constexpr int kFewColumns = 128;  // tokens of dx's transposed product
-constexpr int kOuterTokens = 16;  // tokens of dW as sums of outer products
+constexpr int kOneTokens = 4, kOuterTokens = 32;  // most tokens of dW as sums of outer products
 constexpr int kSumThreads = 256;
 
 // How a product M x N over K is cut: tile width, whole tiles, parts of the others.
@@ -1018,17 +1018,18 @@ int few_product_launch(const GluDesc &d, const uint16_t *dg, float *parts, Devic
                             reinterpret_cast<uint2 *>(d.dx));
 }
 
-// dW for few tokens: a sum of T outer products, bound by writing dW.  A thread has
-// eight columns of eight rows; a token's eight x and its eight d (the same for the
-// whole block) make 64 products, two a packed instruction.
-constexpr int kOuterThreads = 128, kOuterRows = 8;
-__global__ void __launch_bounds__(kOuterThreads)
-    glu_outer_kernel(int T, int D, int64_t F2, const uint16_t *d, const uint16_t *x, uint16_t *dW) {
-    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kOuterRows;
-    const int col = (blockIdx.y * kOuterThreads + threadIdx.x) * 8;
+// dW for up to four tokens, bound by writing dW: a sum of T outer products in
+// registers.  A thread has eight columns of eight rows; a token's eight x and its
+// eight d (the same for the whole block) make 64 products, two a packed
+// instruction.  1 x 2560 x 7680: 18.2 us, what filling 79 MB takes (20).
+constexpr int kOneThreads = 128, kOneRows = 8;
+__global__ void __launch_bounds__(kOneThreads)
+    glu_outer_few_kernel(int T, int D, int64_t F2, const uint16_t *d, const uint16_t *x, uint16_t *dW) {
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kOneRows;
+    const int col = (blockIdx.y * kOneThreads + threadIdx.x) * 8;
     if (col >= D) return;
     dependent_start();
-    unsigned long long sum[kOuterRows][4] = {};
+    unsigned long long sum[kOneRows][4] = {};
 #pragma unroll 4
     for (int t = 0; t < T; ++t) {
         const uint4 xv = *reinterpret_cast<const uint4 *>(x + static_cast<int64_t>(t) * D + col);
@@ -1039,7 +1040,7 @@ __global__ void __launch_bounds__(kOuterThreads)
         for (int i = 0; i < 4; ++i)
             asm("mov.b64 %0, {%1, %2};" : "=l"(xp[i]) : "r"(xw[i] << 16), "r"(xw[i] & 0xffff0000u));
 #pragma unroll
-        for (int r = 0; r < kOuterRows; ++r) {
+        for (int r = 0; r < kOneRows; ++r) {
             const uint32_t v = r & 1 ? dw[r / 2] & 0xffff0000u : dw[r / 2] << 16;
             unsigned long long dd;
             asm("mov.b64 %0, {%1, %1};" : "=l"(dd) : "r"(v));
@@ -1048,7 +1049,7 @@ __global__ void __launch_bounds__(kOuterThreads)
         }
     }
 #pragma unroll
-    for (int r = 0; r < kOuterRows; ++r) {
+    for (int r = 0; r < kOneRows; ++r) {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -1057,6 +1058,74 @@ __global__ void __launch_bounds__(kOuterThreads)
             w[i] = pack2(lo, hi);
         }
         __stcs(reinterpret_cast<uint4 *>(dW + (row0 + r) * D + col), make_uint4(w[0], w[1], w[2], w[3]));
+    }
+}
+
+// dW for 5 to 32 tokens, bound by writing dW: m16n8k16 on tiles of 16 features x 512
+// columns, whose tokens are all in shared memory (four CTAs an SM write while
+// others load).  Both operands have tokens outside, so their fragments are
+// transposed loads; a token's chunks of 16 bytes are rotated by its number, so that
+// eight tokens' touch every bank once.  Rounded to bf16 once, results leave through
+// shared memory, half a kilobyte of a row an instruction.  2560 x 7680, us, here /
+// sums in registers / SM pairs: 4 tokens 25.0 / 21.5 / 27.7, 8 tokens 24.6 / 27.8 /
+// 27.7, 16 tokens 24.6 / 42 / 27.7, 32 tokens 29.7 / - / 27.2; 512 x 1024 1.8 / 1.6 /
+// 3.6, 1.8 / 2.5 / 3.5, 2.3 / 4.2 / 3.9, 3.4 / - / 3.7.
+constexpr int kOuterThreads = 256, kOuterF = 16, kOuterCols = 512;
+constexpr int outer_smem(int T) { return (T + 15) / 16 * 16 * 2 * (kOuterF + kOuterCols) + 8 * kOuterF * 128; }
+__global__ void __launch_bounds__(kOuterThreads, 4)
+    glu_outer_kernel(int T, int D, int64_t F2, int tile_cols, const uint16_t *d, const uint16_t *x, uint16_t *dW) {
+    extern __shared__ __align__(128) uint8_t outer_raw[];
+    constexpr int kX = 2 * kOuterCols, kD = 2 * kOuterF;  // bytes of a token
+    const int tokens = (T + 15) & ~15;
+    const uint32_t xs = smem_u32(outer_raw), ds = xs + tokens * kX;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    uint8_t *results = outer_raw + tokens * (kX + kD);  // [8 warps][16 features][64 columns]
+    const uint32_t ft = blockIdx.x / tile_cols;
+    const int64_t f0 = static_cast<int64_t>(ft) * kOuterF;
+    const int c0 = static_cast<int>(blockIdx.x - ft * tile_cols) * kOuterCols;
+    const auto bring = [&](uint32_t to, const uint16_t *from, bool in) {
+        if (in)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+        else
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0u) : "memory");
+    };
+    dependent_start();
+    for (int i = threadIdx.x; i < tokens * (kX / 16); i += kOuterThreads) {
+        const int t = i / (kX / 16), c = i % (kX / 16);
+        bring(xs + t * kX + 16 * (c ^ (t & 7)), x + static_cast<int64_t>(t) * D + c0 + 8 * c, t < T && c0 + 8 * c < D);
+    }
+    for (int i = threadIdx.x; i < tokens * (kD / 16); i += kOuterThreads) {  // (2F is a multiple of 16)
+        const int t = i / (kD / 16), c = i % (kD / 16);
+        bring(ds + t * kD + 16 * (c ^ (t / 4 & 1)), d + t * F2 + f0 + 8 * c, t < T);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+    const int at = lane & 7, hi = lane >> 4, lo = (lane >> 3) & 1;
+    float sum[8][4] = {};
+    for (int t = 0; t < tokens; t += 16) {
+        uint32_t a[4], b[4];
+        // Blocks: features lo, tokens hi; tokens lo, columns hi.
+        ldmatrix4_trans(a, ds + (t + 8 * hi + at) * kD + 16 * (lo ^ (at / 4)));
+#pragma unroll
+        for (int n = 0; n < 8; n += 2) {
+            ldmatrix4_trans(b, xs + (t + 8 * lo + at) * kX + 16 * ((8 * warp + n + hi) ^ at));
+            mma_16x8x16<false>(sum[n], a, b[0], b[1]);
+            mma_16x8x16<false>(sum[n + 1], a, b[2], b[3]);
+        }
+    }
+    const int r = lane / 4, q = lane % 4;
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            *reinterpret_cast<uint32_t *>(results + (warp * kOuterF + 8 * h + r) * 128 + 16 * (n ^ r) + 4 * q) =
+                pack2(sum[n][2 * h], sum[n][2 * h + 1]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kOuterF / 4; ++i) {
+        const int row = i / 2 * 8 + warp, w = i % 2 * 4 + lane / 8, c = c0 + 64 * w + 8 * (lane % 8);
+        const uint4 v = *reinterpret_cast<const uint4 *>(results + (w * kOuterF + row) * 128 + 16 * ((lane % 8) ^ (row & 7)));
+        if (c < D) __stcs(reinterpret_cast<uint4 *>(dW + (f0 + row) * D + c), v);
     }
 }
 
@@ -1089,11 +1158,21 @@ int glu_backward_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
                                   : product<false>(d.T, d.D, F2, dg, d.W, d.dx, parts, ds, s);
         if (rc) return rc;
     }
-    if (d.dW && d.T <= kOuterTokens) {
-        const int cols = tiles_of(d.D, 8 * kOuterThreads);
+    if (d.dW && d.T <= kOneTokens) {
+        const int cols = tiles_of(d.D, 8 * kOneThreads);
         if (cols > 65535) return set_error(ISAM_ERR_UNSUPPORTED, "isam_glu_backward: D (%d) is too large", d.D);
-        return launch_dependent(glu_outer_kernel, dim3(static_cast<unsigned>(F2 / kOuterRows), static_cast<unsigned>(cols)),
-                                kOuterThreads, 0, s, 1, "launch glu_outer_kernel", d.T, d.D, F2, dg, d.x, d.dW);
+        return launch_dependent(glu_outer_few_kernel, dim3(static_cast<unsigned>(F2 / kOneRows), static_cast<unsigned>(cols)),
+                                kOneThreads, 0, s, 1, "launch glu_outer_few_kernel", d.T, d.D, F2, dg, d.x, d.dW);
+    }
+    if (d.dW && d.T <= kOuterTokens) {
+        const int cols = tiles_of(d.D, kOuterCols);
+        const int64_t tiles = F2 / kOuterF * cols;
+        if (tiles > 0x7fffffffLL) return set_error(ISAM_ERR_UNSUPPORTED, "isam_glu_backward: dW is too large");
+        rc = ensure_smem_optin(reinterpret_cast<const void *>(glu_outer_kernel), outer_smem(kOuterTokens), ds.device,
+                               "cudaFuncSetAttribute(feed-forward dW)");
+        if (rc) return rc;
+        return launch_dependent(glu_outer_kernel, dim3(static_cast<unsigned>(tiles)), kOuterThreads, outer_smem(d.T), s, 1,
+                                "launch glu_outer_kernel", d.T, d.D, F2, cols, dg, d.x, d.dW);
     }
     if (d.dW) return product<true>(F2, d.D, d.T, dg, d.x, d.dW, parts, ds, s);
     return ISAM_OK;

@@ -22,6 +22,15 @@ __device__ __forceinline__ void mma_16x8x16(float (&c)[4], const uint32_t (&a)[4
     }
 }
 
+// Four 8 x 8 blocks of 16-bit elements, transposed: lane 8 i + r gives the address of
+// row r of block i; lane 4 c + t gets rows 2 t and 2 t + 1 of column c of each.
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&v)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                 : "r"(at)
+                 : "memory");
+}
+
 // Sixteen bytes of shared memory by 32-bit address.
 __device__ __forceinline__ uint4 lds16(uint32_t at) {
     uint4 v;

@@ -148,6 +148,12 @@ def test_backward_split_sums(T, D, F):
     check_backward(T, D, F, "silu", seed=T + D)
 
 
+@pytest.mark.parametrize("T", [3, 4, 5, 6, 15, 16, 18, 31, 32])
+@pytest.mark.parametrize("D,F", [(8, 8), (504, 24), (520, 1000), (1032, 136), (2048, 64)])
+def test_backward_few_tokens(T, D, F):
+    check_backward(T, D, F, "silu", seed=T + F)
+
+
 @pytest.mark.parametrize("want", [("dx",), ("dW",), ()])
 def test_backward_of_one_operand(want):
     check_backward(70, 72, 40, "silu", want=want)
