@@ -15,7 +15,8 @@
  *   - The library owns small internal workspaces (an error word per device,
  *     the GRU's input-projection buffer, its hidden-state exchange buffer and
  *     step counter).  They are allocated on first use, reused, and released
- *     by isam_shutdown().
+ *     by isam_shutdown().  isam_glu_backward's workspace grows with the call
+ *     and is the caller's.
  *
  * Execution
  *   - Every compute call is asynchronous on the stream set by

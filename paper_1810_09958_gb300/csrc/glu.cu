@@ -692,8 +692,9 @@ __device__ __forceinline__ float act_of(int act, float a, float &da) {
 // shared memory as a whole, rows 64 bytes off a multiple of 128.  The order of k
 // inside a product does not matter: lane 4 r + t holds eight consecutive k of rows
 // r and 8 + r, and of token r, sixteen bytes each, which are two instructions'
-// operands.  Bound by reading W: 1 x 2560 x 7680 16.5 us, 4.8 TB/s, 0.70 of the copy
-// bandwidth; 32 tokens 19.3 us.
+// operands.  Bound by reading W: 1 x 2560 x 7680 16.0 us, 4.9 TB/s, 0.72 of the copy
+// bandwidth (960 groups on 304 teams leave a part round), 1 x 5120 x 13824 44.4 us,
+// 0.94; 16 tokens 2560 x 7680 17.4 us.
 template <int NT, bool BACK>
 __global__ void __launch_bounds__(32 * kFewWarps, 1)
     glu_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ FewParams p) {
@@ -820,13 +821,16 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1)
     }
 }
 
-// Stages of a warp's ring beside x, 0 where x does not fit.
+// Stages of a warp's ring beside x, 0 where x does not fit.  Three already hold
+// 96 KB an SM in flight, and more spread the reads over more of memory at once:
+// 2 / 3 / 4 stages 17.2 / 16.1 / 16.3 us (1 x 2560 x 7680), 46.7 / 44.4 / 53.9
+// (1 x 5120 x 13824).
 template <int NT>
 int few_stages(int T, int D) {
     const int64_t x = static_cast<int64_t>(tiles_of(D, kBK) * 128 + 64) * T;
     const int64_t left = kFewSmem - 1024 - x - kFewWarps * few_part<NT>();
     const int64_t st = left / (kFewWarps * kFewBlock);
-    return st < 2 ? 0 : static_cast<int>(std::min<int64_t>(st, 4));
+    return st < 2 ? 0 : static_cast<int>(std::min<int64_t>(st, 3));
 }
 
 template <int NT, bool BACK>
