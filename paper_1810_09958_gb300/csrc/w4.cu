@@ -51,8 +51,9 @@ __global__ void __launch_bounds__(kThreads)
 }
 
 constexpr int kTileBytes = 1024;  // codes of 16 rows x 128 k
-constexpr int kStages = 2;        // of a warp's ring
+constexpr int kMaxStages = 4;     // of a warp's ring
 constexpr int kMaxSmem = 224 * 1024;
+constexpr int kMostPer = 4;       // tiles of a warp in a stage
 
 // Bulk copy of global memory into shared memory, counted on a barrier.
 __device__ __forceinline__ void copy(uint32_t to, const void *from, uint32_t bytes, uint32_t bar) {
@@ -103,6 +104,8 @@ struct W4Params {
     int groups;     // of 16 RB rows
     int team;       // warps that share the K of a group
     int per;        // k tiles of a warp in a stage
+    int stages;     // of a team's ring
+    int copies;     // of a team's sums: two save a barrier a group, one leaves more to the ring
     int x_stride;   // bytes of a token's row of x in shared memory
     const uint16_t *x;
     const uint8_t *tiled;
@@ -116,9 +119,15 @@ template <int GROUP, int RB>
 constexpr int tile_bytes() {
     return RB * (kTileBytes + 32 * (128 / GROUP));
 }
+// Words between tokens of a warp's sums: four more than rows, and a store touches
+// every bank once.  (Two blocks of rows: their memory is better left to the L1 cache.)
+template <int RB>
+constexpr int part_step() {
+    return RB == 1 ? 20 : 32;
+}
 template <int NT, int RB>
-constexpr int part_bytes() {  // a warp's sums, twice
-    return 2 * 8 * NT * 16 * RB * 4;
+constexpr int part_bytes() {  // a warp's sums
+    return 8 * NT * part_step<RB>() * 4;
 }
 
 // One CTA an SM.  A team of its warps takes 16 RB rows by 8 NT tokens at a time;
@@ -138,25 +147,27 @@ constexpr int part_bytes() {  // a warp's sums, twice
 //
 // Bound: reading the codes, and beside it the instructions that make them bf16
 // (nine for eight codes) and scale sums.  32001 x 8192, groups of 32: one token
-// 27.9 us, 5.3 TB/s, 0.78 of the copy bandwidth, eight 33.5 us, 0.65 (issue slots
-// 60% full); 4096 x 4096, groups of 128, one token 4.5 us, a launch and one
-// stage's latency.
+// 27.4 us, 5.4 TB/s, 0.79 of the copy bandwidth, eight 33.5 us, 0.65 (issue slots
+// 60% full); 4096 x 4096, groups of 128, one token 4.4 us, a launch and one
+// stage's latency.  More tokens leave less memory to the ring, and wait for shared
+// memory and their sums: 16 x 57344 x 4096 39 us, 0.48; 32 x 57344 x 2048 43, 0.24.
 template <int NT, int GROUP, int RB, bool XS, int WARPS>
 __global__ void __launch_bounds__(32 * (WARPS + 1), 1) gemv_w4_kernel(const __grid_constant__ W4Params p) {
-    constexpr int kPer = 128 / GROUP, kRows = 16 * RB, kSize = kRows * 8 * NT;
+    constexpr int kPer = 128 / GROUP, kRows = 16 * RB, kStep = part_step<RB>(), kSize = part_bytes<NT, RB>() / 4;
     // Word blocks of one scale summed before it applies (all of a tile's would cost
     // registers where rows and tokens are many).
     constexpr int kSpan = RB * NT > 2 ? 1 : GROUP / 32;
     constexpr int kBlock = kTileBytes + 32 * kPer;  // codes and scales of one tile
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ uint64_t full[WARPS][kStages], empty[WARPS][kStages];  // of each team
+    __shared__ uint64_t full[WARPS][kMaxStages], empty[WARPS][kMaxStages];  // of each team
     __shared__ int abort_flag;
+    const int stages = XS ? p.stages : 2, copies = XS ? p.copies : 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int teams = WARPS / p.team, tiles = p.team * p.per;  // of a stage
     const int stage_bytes = tiles * RB * kBlock;
-    uint8_t *xs = smem + WARPS * part_bytes<NT, RB>() + teams * kStages * stage_bytes;
+    uint8_t *xs = smem + WARPS * copies * part_bytes<NT, RB>() + teams * stages * stage_bytes;
     if (threadIdx.x < teams)
-        for (int i = 0; i < kStages; ++i) {
+        for (int i = 0; i < stages; ++i) {
             mbar_init(&full[threadIdx.x][i], 1);
             mbar_init(&empty[threadIdx.x][i], p.team);
         }
@@ -171,7 +182,7 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) gemv_w4_kernel(const __gr
     if (warp == WARPS) {
         // A stage: for each block of rows its tiles' codes, then their scales.
         if (lane == 0) {
-            const uint32_t ring = smem_u32(smem + WARPS * part_bytes<NT, RB>());
+            const uint32_t ring = smem_u32(smem + WARPS * copies * part_bytes<NT, RB>());
             int stage = 0;
             uint32_t phase = 1;
             bool ok = true;
@@ -186,7 +197,7 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) gemv_w4_kernel(const __gr
                             break;
                         }
                         const uint32_t bar = smem_u32(&full[team][stage]);
-                        uint32_t to = ring + (team * kStages + stage) * stage_bytes;
+                        uint32_t to = ring + (team * stages + stage) * stage_bytes;
                         const int rows = RB == 1 ? 1 : min(RB, blocks - g * RB);
                         mbar_arrive_expect_tx(&full[team][stage], rows * n * kBlock);
                         for (int b = 0; b < rows; ++b) {
@@ -196,7 +207,7 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) gemv_w4_kernel(const __gr
                             to += tiles * kBlock;
                         }
                     }
-                    if (++stage == kStages) {
+                    if (++stage == stages) {
                         stage = 0;
                         phase ^= 1u;
                     }
@@ -205,8 +216,8 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) gemv_w4_kernel(const __gr
         __syncwarp();
     } else {
         const int team = warp / p.team, member = warp - team * p.team;
-        const uint32_t ring = smem_u32(smem + WARPS * part_bytes<NT, RB>()) + team * kStages * stage_bytes;
-        float *part = reinterpret_cast<float *>(smem) + team * p.team * 2 * kSize;
+        const uint32_t ring = smem_u32(smem + WARPS * copies * part_bytes<NT, RB>()) + team * stages * stage_bytes;
+        float *part = reinterpret_cast<float *>(smem) + team * p.team * copies * kSize;
         const int r = lane >> 2, t = lane & 3;
         if (XS) {
             // x, and zeros behind K up to whole tiles.
@@ -300,30 +311,34 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) gemv_w4_kernel(const __gr
                 }
                 __syncwarp();  // every lane has read the stage
                 if (lane == 0) mbar_arrive(&empty[team][stage]);
-                if (++stage == kStages) {
+                if (++stage == stages) {
                     stage = 0;
                     phase ^= 1u;
                 }
             }
-            float *mine = part + half * p.team * kSize;
+            float *mine = part + (copies == 2 ? half * p.team * kSize : 0);
 #pragma unroll
             for (int b = 0; b < RB; ++b)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        mine[member * kSize + (8 * n + 2 * t + (i & 1)) * kRows + 16 * b + r + 8 * (i >> 1)] = sum[b][n][i];
-            if (p.team == 1)
-                __syncwarp();
-            else
-                named_bar(1 + team, 32 * p.team);
-            for (int i = 32 * member + lane; i < kSize; i += 32 * p.team) {
-                const int m = i / kRows, n = g * kRows + i % kRows;
+                        mine[member * kSize + (8 * n + 2 * t + (i & 1)) * kStep + 16 * b + r + 8 * (i >> 1)] = sum[b][n][i];
+            const auto team_bar = [&]() {
+                if (p.team == 1)
+                    __syncwarp();
+                else
+                    named_bar(1 + team, 32 * p.team);
+            };
+            team_bar();
+            for (int i = 32 * member + lane; i < kRows * 8 * NT; i += 32 * p.team) {
+                const int m = i / kRows, row = i % kRows, n = g * kRows + row;
                 if (m >= p.M || n >= p.N) continue;
                 float v = 0.0f;
-                for (int q = 0; q < p.team; ++q) v += mine[q * kSize + i];
+                for (int q = 0; q < p.team; ++q) v += mine[q * kSize + m * kStep + row];
                 p.y[static_cast<int64_t>(m) * p.N + n] = 8.0f * v;  // (weights counted in eighths)
             }
+            if (copies == 1) team_bar();  // the sums have been read
         }
     }
     if (*static_cast<volatile int *>(&abort_flag)) {  // copies in flight get time to land
@@ -346,39 +361,49 @@ int gemv_launch(W4Params p, DeviceState &ds, cudaStream_t s) {
     // teams of up to eight; no more warps than tiles.
     p.team = p.groups <= ds.num_sms ? WARPS : 8;
     while (p.team > p.kt) p.team = p.team > 8 ? 8 : p.team / 2;
-    // As few stages of a group as give a warp at most four tiles in each (x from
-    // global memory: one, as the rest of the SM's memory caches it) and fit.
+    // Tiles of a warp in a stage: up to four, in at least two stages a group and two of
+    // the ring, which has up to four (x from global memory: one, in two stages, as the
+    // rest of the SM's memory caches x).  1, 2, 3, 4 at most, us: 1 x 32001 x 8192 40.3,
+    // 28.3, 30.2, 27.5; 8 x 14336 x 4096 10.7, 10.0, 10.0, 10.0.  A group in one stage of
+    // four took 8.9 for 8.4 on 1 x 14336 x 4096.
     const int x = XS ? p.x_stride * p.M : 0;
-    const int rest = kMaxSmem - x - WARPS * part_bytes<NT, RB>();
-    const int most = std::max(1, std::min(XS ? 4 : 1, rest / (WARPS * kStages * tile_bytes<GROUP, RB>())));
-    const int stages = (p.kt + p.team * most - 1) / (p.team * most);
-    p.per = (p.kt + p.team * stages - 1) / (p.team * stages);
-    const size_t smem = WARPS * (part_bytes<NT, RB>() + kStages * p.per * tile_bytes<GROUP, RB>()) + x;
+    const auto tiles = [&](int copies) {  // of a warp's ring
+        return (kMaxSmem - x - WARPS * copies * part_bytes<NT, RB>()) / (WARPS * tile_bytes<GROUP, RB>());
+    };
+    p.copies = !XS || tiles(2) >= 4 ? 2 : 1;
+    const int fit = tiles(p.copies);
+    const int own = (p.kt + p.team - 1) / p.team;  // tiles of a warp in a group
+    const int most = XS ? std::max(1, std::min({kMostPer, (own + 1) / 2, fit / 2})) : 1;
+    const int visits = (p.kt + p.team * most - 1) / (p.team * most);
+    p.per = (p.kt + p.team * visits - 1) / (p.team * visits);
+    p.stages = XS ? std::min(kMaxStages, fit / p.per) : 2;
+    const size_t smem = WARPS * (p.copies * part_bytes<NT, RB>() + p.stages * p.per * tile_bytes<GROUP, RB>()) + x;
     return launch_dependent(fn, dim3(grid), 32 * (WARPS + 1), smem, s, 1, "launch gemv_w4_kernel", p);
 }
 
-// x goes to shared memory where it leaves room for the ring: RB and WARPS of the
-// kernel that has it there, and of the one that reads it through the L1 cache
-// (two blocks of rows share what is read).  Measured, us, with (RB, warps):
-// 16 x 14336 x 4096 (fits) (1, 16) 14.3, (2, 8) 15.8; 16 x 8192 x 8192 (does not)
-// 25.9, 20.6; 32 x 14336 x 2048 (fits) (1, 8) 14.6, (2, 8) 16.7, (1, 16) 20.3;
-// 32 x 8192 x 8192 (does not) 43.0, 37.9, 52.2.
-template <int NT, int GROUP, int RB, int WARPS, int RB_L1, int WARPS_L1>
-int gemv_x(W4Params p, DeviceState &ds, cudaStream_t s) {
+// x goes to shared memory where it leaves room for two tiles a warp, with 16 warps
+// or (17 to 32 tokens) 8; else it is read through the L1 cache by a kernel whose
+// two blocks of rows share what is read.
+template <int NT, int GROUP, int WARPS>
+bool x_fits(W4Params &p) {
     p.x_stride = p.kt * 256 + 64;
-    const int64_t rest = WARPS * (kStages * tile_bytes<GROUP, RB>() + part_bytes<NT, RB>());
-    if (static_cast<int64_t>(p.x_stride) * p.M + rest <= kMaxSmem) return gemv_launch<NT, GROUP, RB, true, WARPS>(p, ds, s);
-    return gemv_launch<NT, GROUP, RB_L1, false, WARPS_L1>(p, ds, s);
+    const int64_t rest = WARPS * (2 * tile_bytes<GROUP, 1>() + part_bytes<NT, 1>());
+    return static_cast<int64_t>(p.x_stride) * p.M + rest <= kMaxSmem;
 }
 
+// Measured, us, with (RB, warps): 16 x 14336 x 4096 (x fits) (1, 16) 13.0, (2, 8) 15.8;
+// 16 x 8192 x 8192 (it does not) 25.9, 20.4; 32 x 14336 x 2048 (fits) (1, 16) 13.7, (1, 8)
+// 15.5; 20 x 16384 x 4096 (fits 8 warps) (1, 8) 23.7, (2, 8) 37; 32 x 8192 x 8192 (does
+// not) (1, 8) 43, (2, 8) 35.7, (2, 16) 52.
 template <int NT, int GROUP>
-int gemv_rows(const W4Params &p, DeviceState &ds, cudaStream_t s) {
+int gemv_rows(W4Params p, DeviceState &ds, cudaStream_t s) {
+    if (x_fits<NT, GROUP, 16>(p)) return gemv_launch<NT, GROUP, 1, true, 16>(p, ds, s);
     if constexpr (NT == 1) {
-        return gemv_x<1, GROUP, 1, 16, 1, 16>(p, ds, s);
-    } else if constexpr (NT == 2) {
-        return gemv_x<2, GROUP, 1, 16, 2, 8>(p, ds, s);
+        return gemv_launch<NT, GROUP, 1, false, 16>(p, ds, s);
     } else {
-        return gemv_x<4, GROUP, 1, 8, 2, 8>(p, ds, s);
+        if constexpr (NT == 4)
+            if (x_fits<NT, GROUP, 8>(p)) return gemv_launch<NT, GROUP, 1, true, 8>(p, ds, s);
+        return gemv_launch<NT, GROUP, 2, false, 8>(p, ds, s);
     }
 }
 
@@ -406,7 +431,7 @@ int w4_pack_launch(int N, int K, int group, const uint8_t *codes, const uint16_t
 
 int gemv_w4_launch(int M, int N, int K, int group, const uint16_t *x, const uint8_t *tiled, const uint16_t *scales,
                    float *y, DeviceState &ds, cudaStream_t s) {
-    const W4Params p{M, N, K, (K + 127) / 128, 0, 0, 0, 0, x, tiled, scales, y, wait_timeout_ns(), ds.err_word};
+    const W4Params p{M, N, K, (K + 127) / 128, 0, 0, 0, 0, 0, 0, x, tiled, scales, y, wait_timeout_ns(), ds.err_word};
     if (M <= 8) return gemv_group<1>(p, group, ds, s);
     if (M <= 16) return gemv_group<2>(p, group, ds, s);
     return gemv_group<4>(p, group, ds, s);

@@ -108,6 +108,13 @@ def test_x_that_fits_and_x_that_does_not(M, N, K, group):
     check(M, N, K, group, seed=M + N + K)
 
 
+@pytest.mark.parametrize("M,N,K,group", [(1, 7600, 136, 32), (8, 5200, 1544, 128), (13, 5200, 4104, 64),
+                                         (16, 5000, 4096, 64), (16, 7500, 200, 32), (20, 5000, 4000, 32),
+                                         (32, 7400, 1000, 128), (32, 5000, 2048, 64), (29, 5100, 3080, 128)])
+def test_several_groups_of_rows_a_team(M, N, K, group):
+    check(M, N, K, group, seed=N + K)
+
+
 @pytest.mark.parametrize("M,N,K,group", [(1, 160, 1024, 32), (8, 1001, 520, 64), (32, 64, 2048, 128), (3, 7, 40, 32)])
 def test_integer_data_is_exact(M, N, K, group):
     check(M, N, K, group, seed=77, exact=True)
