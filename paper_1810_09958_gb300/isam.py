@@ -125,14 +125,19 @@ def _dev(t, dtype, numel, name):
 _raw_stream = None
 
 
-def _use_current_stream(lib):
+def _stream_getter():
     global _raw_stream
     import torch
     if _raw_stream is None:
         # Where torch has it, 3 us cheaper than building a Stream object.
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _raw_stream = raw if raw else lambda _: torch.cuda.current_stream().cuda_stream
-    lib.isam_set_stream(_raw_stream(torch.cuda.current_device()))
+    return _raw_stream
+
+
+def _use_current_stream(lib):
+    import torch
+    lib.isam_set_stream(_stream_getter()(torch.cuda.current_device()))
 
 
 def sync() -> None:
@@ -393,18 +398,16 @@ class _Call:
     __slots__ = ("lib", "torch", "device")
 
     def __init__(self):
-        global _torch
         if _torch is None:
-            import torch
-            _torch = torch
+            _first_call()
         self.torch = _torch
-        self.lib = _lib if _lib is not None else load()
-        self.device = _torch.cuda.current_device() if _torch.cuda.is_initialized() else -1
+        self.lib = _lib
+        self.device = _current_device()
 
     def ptr(self, t, dtype, numel, name):
         """The address of a tensor that is what it has to be."""
-        if not (t.is_cuda and t.dtype == dtype and t.numel() == numel and t.is_contiguous()
-                and t.get_device() == self.device):
+        # (a CPU tensor's device is -1, which no current device is)
+        if not (t.dtype is dtype and t.get_device() == self.device and t.numel() == numel and t.is_contiguous()):
             _dev(t, dtype, numel, name)
         return t.data_ptr()
 
@@ -413,20 +416,56 @@ class _Call:
 
     def kind(self, t, name):
         """ISAM_F32 or ISAM_BF16 of a tensor."""
-        if t.dtype == self.torch.bfloat16:
-            return 1
-        if t.dtype == self.torch.float32:
-            return 0
-        raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+        code = _kinds.get(t.dtype)
+        if code is None:
+            raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+        return code
 
     def run(self, fn, *args):
-        _use_current_stream(self.lib)
+        self.lib.isam_set_stream(_raw_stream(self.device))
         rc = fn(*args)
         if rc != ISAM_OK:
             check(rc)
 
 
 _torch = None
+_kinds = {}
+
+
+def _current_device():
+    """-2 until torch has set CUDA up: no tensor is on a device then."""
+    global _current_device
+    if not _torch.cuda.is_initialized():
+        return -2
+    # Where torch has it, without torch's check that CUDA is set up.
+    _current_device = getattr(_torch._C, "_cuda_getDevice", _torch.cuda.current_device)
+    return _current_device()
+
+
+def _with_workspace(device, size, call):
+    """call(address of `size` bytes of torch's allocator on the current stream,
+    given back behind the call, to later work of that stream)."""
+    # Where torch has it: 1 us a call, a tensor 5 to 8.
+    alloc = getattr(_torch._C, "_cuda_cudaCachingAllocator_raw_alloc", None)
+    free = getattr(_torch._C, "_cuda_cudaCachingAllocator_raw_delete", None)
+    if alloc is None or free is None:
+        held = _torch.empty(size, dtype=_torch.uint8, device=f"cuda:{device}")
+        call(held.data_ptr())
+        return
+    at = alloc(size, _raw_stream(device))
+    try:
+        call(at)
+    finally:
+        free(at)
+
+
+def _first_call():
+    global _torch
+    import torch
+    load()
+    _stream_getter()
+    _kinds.update({torch.float32: 0, torch.bfloat16: 1})
+    _torch = torch
 
 
 def glr_forward(T, batch, hidden, g, h0, lengths, h_out, h_last=None) -> None:
@@ -503,7 +542,8 @@ def glu_backward(T, D, F, act, x, W, dh, dx, dW, workspace=None) -> None:
     out = (c.opt(dx, bf16, T * D, "dx"), c.opt(dW, bf16, 2 * F * D, "dW"))
     need = glu_backward_workspace(T, D, F)
     if workspace is None:
-        workspace = c.torch.empty(need, dtype=u8, device=x.device)
+        _with_workspace(c.device, need, lambda ws: c.run(c.lib.isam_glu_backward, T, D, F, code, *args, ws, *out))
+        return
     ws = c.ptr(workspace, u8, workspace.numel(), "workspace")
     if workspace.numel() < need:
         raise ValueError(f"workspace has {workspace.numel()} bytes, {need} are needed")

@@ -251,3 +251,42 @@ def test_captured_in_a_graph():
     torch.cuda.synchronize()
     for a, b in zip(want, (h, dx, dW)):
         assert torch.equal(a, b)
+
+
+def test_backward_takes_its_workspace_from_the_allocator():
+    """Without a workspace argument: the same bits, on another stream and in a
+    captured graph too, and nothing left allocated."""
+    import torch
+    T, D, F = 300, 520, 264
+    x, W, dh = (t.cuda() for t in operands(T, D, F, 5))
+    want = torch.empty_like(x), torch.empty_like(W)
+    ws = torch.empty(isam.glu_backward_workspace(T, D, F), dtype=torch.uint8, device="cuda")
+    isam.glu_backward(T, D, F, "silu", x, W, dh, *want, workspace=ws)
+    isam.sync()
+
+    def same(got):
+        return all(torch.equal(a, b) for a, b in zip(got, want))
+    before = torch.cuda.memory_allocated()
+    got = torch.zeros_like(x), torch.zeros_like(W)
+    held = torch.cuda.memory_allocated() - before
+    isam.glu_backward(T, D, F, "silu", x, W, dh, *got)
+    assert torch.cuda.memory_allocated() - before == held
+    isam.sync()
+    assert same(got)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for t in got:
+            t.zero_()
+        for _ in range(3):
+            isam.glu_backward(T, D, F, "silu", x, W, dh, *got)
+    side.synchronize()
+    assert same(got)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        isam.glu_backward(T, D, F, "silu", x, W, dh, *got)
+    for t in got:
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert same(got)
