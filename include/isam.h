@@ -561,7 +561,7 @@ int isam_glu_backward(int T, int D, int F, int act, const isam_bf16 *x, const is
  * isam_w4_pack: from codes [N][K/2] (byte k/2 of a row holds q of an even k in
  * its low half and of k + 1 in its high half) and scales [N][ceil(K/group)].
  *
- * 1 <= M <= 32, N >= 1, K >= 8 a multiple of 8; x, tiled and tiled_scales
+ * 1 <= M <= 32, 1 <= N <= 2^31 - 16, K >= 8 a multiple of 8; x, tiled and tiled_scales
  * 16-byte aligned, y 4-byte aligned, scales 2-byte aligned; else
  * ISAM_ERR_UNSUPPORTED.  ISAM_ERR_INVALID_ARG for sizes < 1, another group or
  * null pointers.  (q - 8) is exact in bf16, sums are fp32, and each group's sum

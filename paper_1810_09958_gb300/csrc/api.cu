@@ -620,6 +620,8 @@ int w4_validate(const char *name, int N, int K, int group) {
     if (group != 32 && group != 64 && group != 128)
         return set_error(ISAM_ERR_INVALID_ARG, "%s: group must be 32, 64 or 128", name);
     if (K % 8 != 0) return set_error(ISAM_ERR_UNSUPPORTED, "%s: K (%d) must be a multiple of 8", name, K);
+    // Rows are counted in whole tiles of 16, in 31 bits.
+    if (N > 0x7fffffff - 15) return set_error(ISAM_ERR_UNSUPPORTED, "%s: N (%d) is above 2^31 - 16", name, N);
     // The tiled words are counted in 64 bits, their blocks of 256 in 31.
     if (static_cast<int64_t>((N + 15LL) / 16) * ((K + 127LL) / 128) > 0x7fffffffLL)
         return set_error(ISAM_ERR_UNSUPPORTED, "%s: more than 2^31 weight tiles", name);

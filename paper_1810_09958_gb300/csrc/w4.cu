@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) gemv_w4_kernel(const __gr
     __syncthreads();
     dependent_start();
     const WaitCtx wait{p.timeout_ns, p.err, &abort_flag};
-    const int blocks = (p.N + 15) / 16;
+    const int blocks = (p.N - 1) / 16 + 1;
     const int stride = teams * gridDim.x;  // groups: team t's are t * gridDim.x + blockIdx.x and every stride-th
 
     if (warp == WARPS) {
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) gemv_w4_kernel(const __gr
                 uint32_t code_at = ring + stage * stage_bytes + k * kTileBytes + 16 * lane;
                 uint32_t scale_at = ring + stage * stage_bytes + tiles * kTileBytes + k * 32 * kPer + 2 * kPer * r;
                 const uint32_t code_end = code_at + max(n_tiles, 0) * kTileBytes;
-                uint32_t x_at = 256 * (k0 + k);  // bytes into a token's row
+                uint32_t x_at = 256u * static_cast<uint32_t>(k0 + k);  // bytes into a token's row, below 2^32
 #pragma unroll 1
                 for (; code_at != code_end; code_at += kTileBytes, scale_at += 32 * kPer, x_at += 256) {
                     uint4 code[RB][2];
@@ -355,7 +355,7 @@ int gemv_launch(W4Params p, DeviceState &ds, cudaStream_t s) {
     const int rc = ensure_smem_optin(reinterpret_cast<const void *>(fn), kMaxSmem, ds.device,
                                      "cudaFuncSetAttribute(4-bit product)");
     if (rc) return rc;
-    p.groups = ((p.N + 15) / 16 + RB - 1) / RB;
+    p.groups = (p.N - 1) / (16 * RB) + 1;
     const int grid = std::min(p.groups, ds.num_sms);
     // The whole CTA on one group where there are no more groups than SMs, else
     // teams of up to eight; no more warps than tiles.
@@ -386,9 +386,11 @@ int gemv_launch(W4Params p, DeviceState &ds, cudaStream_t s) {
 // two blocks of rows share what is read.
 template <int NT, int GROUP, int WARPS>
 bool x_fits(W4Params &p) {
-    p.x_stride = p.kt * 256 + 64;
+    const int64_t stride = p.kt * int64_t{256} + 64;  // (above 32 bits from K = 2^30 on)
     const int64_t rest = WARPS * (2 * tile_bytes<GROUP, 1>() + part_bytes<NT, 1>());
-    return static_cast<int64_t>(p.x_stride) * p.M + rest <= kMaxSmem;
+    if (stride * p.M + rest > kMaxSmem) return false;
+    p.x_stride = static_cast<int>(stride);
+    return true;
 }
 
 // Measured, us, with (RB, warps): 16 x 14336 x 4096 (x fits) (1, 16) 13.0, (2, 8) 15.8;
@@ -418,20 +420,20 @@ int gemv_group(const W4Params &p, int group, DeviceState &ds, cudaStream_t s) {
 
 int w4_pack_launch(int N, int K, int group, const uint8_t *codes, const uint16_t *scales, uint8_t *tiled,
                    uint16_t *tiled_scales, cudaStream_t s) {
-    const int nb = (N + 15) / 16, kt = (K + 127) / 128, per = 128 / group;
+    const int nb = (N - 1) / 16 + 1, kt = (K - 1) / 128 + 1, per = 128 / group;
     const int64_t words = static_cast<int64_t>(nb) * kt * 256, count = static_cast<int64_t>(nb) * kt * 16 * per;
     w4_pack_codes_kernel<<<static_cast<unsigned>((words + kThreads - 1) / kThreads), kThreads, 0, s>>>(
         N, K, kt, words, codes, reinterpret_cast<uint32_t *>(tiled));
     const int rc = launch_status("launch w4_pack_codes_kernel");
     if (rc) return rc;
     w4_pack_scales_kernel<<<static_cast<unsigned>((count + kThreads - 1) / kThreads), kThreads, 0, s>>>(
-        N, (K + group - 1) / group, kt, per, count, scales, tiled_scales);
+        N, (K - 1) / group + 1, kt, per, count, scales, tiled_scales);
     return launch_status("launch w4_pack_scales_kernel");
 }
 
 int gemv_w4_launch(int M, int N, int K, int group, const uint16_t *x, const uint8_t *tiled, const uint16_t *scales,
                    float *y, DeviceState &ds, cudaStream_t s) {
-    const W4Params p{M, N, K, (K + 127) / 128, 0, 0, 0, 0, 0, 0, x, tiled, scales, y, wait_timeout_ns(), ds.err_word};
+    const W4Params p{M, N, K, (K - 1) / 128 + 1, 0, 0, 0, 0, 0, 0, x, tiled, scales, y, wait_timeout_ns(), ds.err_word};
     if (M <= 8) return gemv_group<1>(p, group, ds, s);
     if (M <= 16) return gemv_group<2>(p, group, ds, s);
     return gemv_group<4>(p, group, ds, s);

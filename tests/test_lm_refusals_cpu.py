@@ -127,3 +127,12 @@ def test_binding_refuses_what_it_can_see():
         isam.gemv_w4(1, 16, 64, 48, g, g, g, g)
     assert isam.w4_tiled_bytes(17, 129) == 2 * 2 * 1024
     assert isam.w4_tiled_scales(17, 129, 32) == 2 * 2 * 16 * 4
+
+
+@pytest.mark.parametrize("N", [2 ** 31 - 15, BIG])
+def test_w4_rows_beyond_whole_tiles(lib, N):
+    """Rows are counted in whole tiles of 16: the last 15 numbers of 31 bits are refused."""
+    assert lib.isam_w4_pack(N, 8, 32, P, P, P, P) == NO
+    assert b"isam_w4_pack: N" in lib.isam_last_error_string()
+    assert lib.isam_gemv_w4(1, N, 8, 32, P, P, P, P) == NO
+    assert b"isam_gemv_w4: N" in lib.isam_last_error_string()

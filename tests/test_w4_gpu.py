@@ -190,3 +190,31 @@ def test_weights_beyond_32_bits():
     w = lm_ref.dequantised(q, scales[-64:].double().cpu().numpy(), group)
     tol = (K / 16 + 32) * 2.0 ** -22 * (np.abs(x.double().numpy()) @ np.abs(w).T)
     assert (np.abs(y[:, -64:].double().cpu().numpy() - x.double().numpy() @ w.T) <= tol).all()
+
+
+@pytest.mark.parametrize("M,K", [(2, 2 ** 30 - 128), (2, 2 ** 30 - 8), (1, 2 ** 30), (2, 2 ** 30 + 264), (1, 2 ** 31 - 8)])
+def test_rows_of_x_beyond_32_bits(M, K):
+    """Rows of x of 2 and 4 GB: their size passes 31 and 32 bits.  x is zero but
+    in a few places, integers there, so that results are exact."""
+    import torch
+    N, group = 3, 128
+    gen = torch.Generator(device="cuda").manual_seed(K % 1000)
+    codes = torch.randint(0, 256, (N, K // 2), dtype=torch.uint8, device="cuda", generator=gen)
+    scales = torch.randint(0, 4, (N, -(-K // group)), device="cuda", generator=gen).sub_(2).float().exp2_().bfloat16()
+    tiled = torch.empty(isam.w4_tiled_bytes(N, K), dtype=torch.uint8, device="cuda")
+    ts = torch.empty(isam.w4_tiled_scales(N, K, group), dtype=torch.bfloat16, device="cuda")
+    isam.w4_pack(N, K, group, codes, scales, tiled, ts)
+    at = [0, 1, 129, K // 3, K // 2 - 1, K // 2, K - 130, K - 2, K - 1]
+    at += [k for k in (2 ** 29 - 1, 2 ** 29, 2 ** 30 - 1, 2 ** 30) if k < K and k not in at]
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    v = np.arange(1, len(at) + 1) * (1 + np.arange(M)[:, None])
+    x[:, at] = torch.from_numpy(v.astype(np.float32)).bfloat16().cuda()
+    y = Guarded(M * N, np.full(M * N, np.nan))
+    isam.gemv_w4(M, N, K, group, x, tiled, ts, y.t)
+    isam.sync()
+    k = torch.tensor(at, device="cuda")
+    pair = codes[:, k // 2].cpu().numpy()
+    q = np.where(np.array(at) % 2 == 0, pair & 15, pair >> 4).astype(np.float64)
+    w = (q - 8) * scales[:, k // group].double().cpu().numpy()
+    assert np.array_equal(y.numpy().astype(np.float64).reshape(M, N), v @ w.T)
+    assert y.guards_intact()
