@@ -520,10 +520,10 @@ enum { ISAM_ACT_SILU = 0, ISAM_ACT_GELU = 1, ISAM_ACT_RELU = 2, ISAM_ACT_SIGMOID
  * Two of Listing 4's matrix products share x, and the element-wise statements
  * after them run on the accumulators (fp32): neither projection reaches
  * memory.  The block's output projection is isam_gemm on h.
- * Any T, F >= 1, D a multiple of 8, x and W 16-byte aligned, h 2-byte
- * aligned; else ISAM_ERR_UNSUPPORTED.  ISAM_ERR_INVALID_ARG for sizes < 1, null
- * pointers or an unknown act.  Asynchronous on the stream set by
- * isam_set_stream.
+ * Any T >= 1, F up to 2^29, D a multiple of 8 up to 2^29, x and W 16-byte
+ * aligned, h 2-byte aligned; else ISAM_ERR_UNSUPPORTED.  ISAM_ERR_INVALID_ARG
+ * for sizes < 1, null pointers or an unknown act.  Asynchronous on the stream
+ * set by isam_set_stream.
  */
 int isam_glu_forward(int T, int D, int F, int act, const isam_bf16 *x, const isam_bf16 *W, isam_bf16 *h);
 
@@ -561,8 +561,8 @@ int isam_glu_backward(int T, int D, int F, int act, const isam_bf16 *x, const is
  * isam_w4_pack: from codes [N][K/2] (byte k/2 of a row holds q of an even k in
  * its low half and of k + 1 in its high half) and scales [N][ceil(K/group)].
  *
- * 1 <= M <= 32, 1 <= N <= 2^31 - 16, K >= 8 a multiple of 8; x, tiled and tiled_scales
- * 16-byte aligned, y 4-byte aligned, scales 2-byte aligned; else
+ * 1 <= M <= 32, 1 <= N <= 2^31 - 16, K >= 8 a multiple of 8; x, tiled and
+ * tiled_scales 16-byte aligned, y 4-byte aligned, scales 2-byte aligned; else
  * ISAM_ERR_UNSUPPORTED.  ISAM_ERR_INVALID_ARG for sizes < 1, another group or
  * null pointers.  (q - 8) is exact in bf16, sums are fp32, and each group's sum
  * is multiplied by its scale in fp32.  Asynchronous on the stream set by

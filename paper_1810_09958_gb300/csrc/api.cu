@@ -609,6 +609,9 @@ int glu_validate(const char *name, int T, int D, int F, int act, const void *x, 
         return set_error(ISAM_ERR_INVALID_ARG, "%s: unknown activation %d", name, act);
     if (!x || !W) return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
     if (D % 8 != 0) return set_error(ISAM_ERR_UNSUPPORTED, "%s: D (%d) must be a multiple of 8", name, D);
+    // A tile walks all of D while its epilogue waits: at 0.31 us a 64-deep block, beyond 2^29 takes longer than
+    // a wait may by default.
+    if (D > (1 << 29)) return set_error(ISAM_ERR_UNSUPPORTED, "%s: D (%d) is above 2^29", name, D);
     if (F > (1 << 29)) return set_error(ISAM_ERR_UNSUPPORTED, "%s: F (%d) is above 2^29", name, F);
     if (!aligned(x, 16) || !aligned(W, 16))
         return set_error(ISAM_ERR_UNSUPPORTED, "%s: x and W must be 16-byte aligned", name);

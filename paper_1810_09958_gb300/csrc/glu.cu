@@ -827,7 +827,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, 1)
 // (1 x 5120 x 13824).
 template <int NT>
 int few_stages(int T, int D) {
-    const int64_t x = static_cast<int64_t>(tiles_of(D, kBK) * 128 + 64) * T;
+    const int64_t x = (tiles_of(D, kBK) * int64_t{128} + 64) * T;
     const int64_t left = kFewSmem - 1024 - x - kFewWarps * few_part<NT>();
     const int64_t st = left / (kFewWarps * kFewBlock);
     return st < 2 ? 0 : static_cast<int>(std::min<int64_t>(st, 3));

@@ -136,3 +136,12 @@ def test_w4_rows_beyond_whole_tiles(lib, N):
     assert b"isam_w4_pack: N" in lib.isam_last_error_string()
     assert lib.isam_gemv_w4(1, N, 8, 32, P, P, P, P) == NO
     assert b"isam_gemv_w4: N" in lib.isam_last_error_string()
+
+
+@pytest.mark.parametrize("T", [1, 32, 200])
+@pytest.mark.parametrize("D", [2 ** 29 + 8, 2 ** 30 - 8, 2 ** 30, 2 ** 31 - 8])
+def test_glu_depths_beyond_the_limit(lib, T, D):
+    assert lib.isam_glu_forward(T, D, 8, 0, P, P, P) == NO
+    assert b"isam_glu_forward: D" in lib.isam_last_error_string()
+    assert lib.isam_glu_backward(T, D, 8, 0, P, P, P, P, P, P) == NO
+    assert b"isam_glu_backward: D" in lib.isam_last_error_string()
