@@ -135,12 +135,24 @@ def _stream_getter():
     return _raw_stream
 
 
-def _use_current_stream(lib):
+# The library's stream is one for the whole process: a thread holds this from
+# setting it to the end of the call that is to run there.
+_stream_lock = threading.Lock()
+
+
+def _on_current_stream(fn, *args):
+    """fn(*args), an entry of the library, on torch's current stream."""
     import torch
-    lib.isam_set_stream(_stream_getter()(torch.cuda.current_device()))
+    stream = _stream_getter()(torch.cuda.current_device())
+    with _stream_lock:
+        _lib.isam_set_stream(stream)
+        rc = fn(*args)
+    check(rc)
 
 
 def sync() -> None:
+    """isam_sync: waits for the stream of the last call (of any thread) and
+    raises what its kernels reported."""
     check(load().isam_sync())
 
 
@@ -155,9 +167,8 @@ def gemm(M, N, K, transA, transB, alpha, A, B, beta, C) -> None:
     _dev(A, torch.bfloat16, M * K, "A")
     _dev(B, torch.bfloat16, K * N, "B")
     _dev(C, torch.float32, M * N, "C")
-    _use_current_stream(lib)
-    check(lib.isam_gemm(M, N, K, int(transA), int(transB), float(alpha), _ptr(A), _ptr(B),
-                        float(beta), _ptr(C)))
+    _on_current_stream(lib.isam_gemm, M, N, K, int(transA), int(transB), float(alpha), _ptr(A), _ptr(B),
+                       float(beta), _ptr(C))
 
 
 def gemm_fp8(M, N, K, alpha, A, B, beta, C) -> None:
@@ -170,8 +181,7 @@ def gemm_fp8(M, N, K, alpha, A, B, beta, C) -> None:
             raise ValueError(f"{name} must hold E4M3 bytes (uint8 or float8_e4m3fn), got {t.dtype}")
         _dev(t, t.dtype, n, name)
     _dev(C, torch.float32, M * N, "C")
-    _use_current_stream(lib)
-    check(lib.isam_gemm_fp8(M, N, K, float(alpha), _ptr(A), _ptr(B), float(beta), _ptr(C)))
+    _on_current_stream(lib.isam_gemm_fp8, M, N, K, float(alpha), _ptr(A), _ptr(B), float(beta), _ptr(C))
 
 
 def _e4m3_dev(t, n, name):
@@ -197,8 +207,8 @@ def gemm_mxfp8(M, N, K, alpha, A, SA, B, SB, beta, C) -> None:
     _dev(SA, torch.uint8, mx_scale_bytes(M, K), "SA")
     _dev(SB, torch.uint8, mx_scale_bytes(N, K), "SB")
     _dev(C, torch.float32, M * N, "C")
-    _use_current_stream(lib)
-    check(lib.isam_gemm_mxfp8(M, N, K, float(alpha), _ptr(A), _ptr(SA), _ptr(B), _ptr(SB), float(beta), _ptr(C)))
+    _on_current_stream(lib.isam_gemm_mxfp8, M, N, K, float(alpha), _ptr(A), _ptr(SA), _ptr(B), _ptr(SB), float(beta),
+                       _ptr(C))
 
 
 class GroupedGemmMxfp8:
@@ -225,8 +235,7 @@ class GroupedGemmMxfp8:
 
     def __call__(self):
         lib = load()
-        _use_current_stream(lib)
-        check(lib.isam_gemm_grouped_mxfp8(self.n, *self.args))
+        _on_current_stream(lib.isam_gemm_grouped_mxfp8, self.n, *self.args)
 
 
 class GroupedGemm:
@@ -251,8 +260,7 @@ class GroupedGemm:
 
     def __call__(self):
         lib = load()
-        _use_current_stream(lib)
-        check(lib.isam_gemm_grouped(self.n, *self.args))
+        _on_current_stream(lib.isam_gemm_grouped, self.n, *self.args)
 
 
 class GroupedGemmFp8:
@@ -276,8 +284,7 @@ class GroupedGemmFp8:
 
     def __call__(self):
         lib = load()
-        _use_current_stream(lib)
-        check(lib.isam_gemm_grouped_fp8(self.n, *self.args))
+        _on_current_stream(lib.isam_gemm_grouped_fp8, self.n, *self.args)
 
 
 def gemm_grouped(problems) -> None:
@@ -312,9 +319,8 @@ def gru_forward(T, batch, hidden, x, W, U, b, h0, h_out, reset_before=False) -> 
     if h0 is not None:
         _dev(h0, torch.float32, batch * H, "h0")
     _dev(h_out, torch.float32, T * batch * H, "h_out")
-    _use_current_stream(lib)
     fn = lib.isam_gru_forward_reset_before if reset_before else lib.isam_gru_forward
-    check(fn(T, batch, H, _ptr(x), _ptr(W), _ptr(U), _ptr(b), _ptr(h0), _ptr(h_out)))
+    _on_current_stream(fn, T, batch, H, _ptr(x), _ptr(W), _ptr(U), _ptr(b), _ptr(h0), _ptr(h_out))
 
 
 def gru_forward_stack(layers, T, batch, hidden, x, W, U, b, h0, h_out, reset_before=False) -> None:
@@ -330,9 +336,8 @@ def gru_forward_stack(layers, T, batch, hidden, x, W, U, b, h0, h_out, reset_bef
     if h0 is not None:
         _dev(h0, torch.float32, L * batch * H, "h0")
     _dev(h_out, torch.float32, L * T * batch * H, "h_out")
-    _use_current_stream(lib)
-    check(lib.isam_gru_forward_stack(L, T, batch, H, int(bool(reset_before)), _ptr(x), _ptr(W),
-                                     _ptr(U), _ptr(b), _ptr(h0), _ptr(h_out)))
+    _on_current_stream(lib.isam_gru_forward_stack, L, T, batch, H, int(bool(reset_before)), _ptr(x), _ptr(W),
+                       _ptr(U), _ptr(b), _ptr(h0), _ptr(h_out))
 
 
 def dwsep_conv(N, H, W, Cin, Cout, x, dw_w, pw_w, out) -> None:
@@ -343,8 +348,7 @@ def dwsep_conv(N, H, W, Cin, Cout, x, dw_w, pw_w, out) -> None:
     _dev(dw_w, torch.bfloat16, 9 * Cin, "dw_w")
     _dev(pw_w, torch.bfloat16, Cin * Cout, "pw_w")
     _dev(out, torch.float32, N * H * W * Cout, "out")
-    _use_current_stream(lib)
-    check(lib.isam_dwsep_conv(N, H, W, Cin, Cout, _ptr(x), _ptr(dw_w), _ptr(pw_w), _ptr(out)))
+    _on_current_stream(lib.isam_dwsep_conv, N, H, W, Cin, Cout, _ptr(x), _ptr(dw_w), _ptr(pw_w), _ptr(out))
 
 
 def depthwise_conv3x3(N, H, W, C, x, dw_w, y) -> None:
@@ -354,8 +358,7 @@ def depthwise_conv3x3(N, H, W, C, x, dw_w, y) -> None:
     _dev(x, torch.bfloat16, N * H * W * C, "x")
     _dev(dw_w, torch.bfloat16, 9 * C, "dw_w")
     _dev(y, torch.bfloat16, N * H * W * C, "y")
-    _use_current_stream(lib)
-    check(lib.isam_depthwise_conv3x3(N, H, W, C, _ptr(x), _ptr(dw_w), _ptr(y)))
+    _on_current_stream(lib.isam_depthwise_conv3x3, N, H, W, C, _ptr(x), _ptr(dw_w), _ptr(y))
 
 
 _DWSEP_PLAN_KEYS = ("kernel", "rows_per_tile", "blocks", "block_cout")
@@ -422,8 +425,10 @@ class _Call:
         return code
 
     def run(self, fn, *args):
-        self.lib.isam_set_stream(_raw_stream(self.device))
-        rc = fn(*args)
+        stream = _raw_stream(self.device)
+        with _stream_lock:
+            self.lib.isam_set_stream(stream)
+            rc = fn(*args)
         if rc != ISAM_OK:
             check(rc)
 

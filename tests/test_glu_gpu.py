@@ -290,3 +290,47 @@ def test_backward_takes_its_workspace_from_the_allocator():
     graph.replay()
     torch.cuda.synchronize()
     assert same(got)
+
+
+def test_two_threads_on_streams_of_their_own():
+    """The backward pass with the allocator's workspace from two threads at once,
+    each reusing that memory between its calls: the bits of one thread alone."""
+    import threading
+    import torch
+    T, D, F = 300, 520, 264
+    ops = [[t.cuda() for t in operands(T, D, F, seed)] for seed in (11, 12)]
+    want = []
+    for x, W, dh in ops:
+        dx, dW = torch.empty_like(x), torch.empty_like(W)
+        isam.glu_backward(T, D, F, "silu", x, W, dh, dx, dW)
+        isam.sync()
+        want.append((dx, dW))
+    got, failed = [[], []], []
+
+    def work(i):
+        try:
+            torch.cuda.set_device(0)
+            x, W, dh = ops[i]
+            size = isam.glu_backward_workspace(T, D, F)
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(50):
+                    dx, dW = torch.empty_like(x), torch.empty_like(W)
+                    isam.glu_backward(T, D, F, "silu", x, W, dh, dx, dW)
+                    torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")  # takes what the call gave back
+                    got[i].append((dx, dW))
+                stream.synchronize()
+        except Exception as e:
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    torch.cuda.synchronize()
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    isam.sync()
+    assert not failed, failed
+    for outs, ref in zip(got, want):
+        assert len(outs) == 50
+        assert all(torch.equal(a, b) for o in outs for a, b in zip(o, ref))
