@@ -37,6 +37,25 @@ __device__ __forceinline__ Gate gate(float x) {
     return x >= 0.0f ? Gate{r, s} : Gate{s, r};
 }
 
+// P(-x), x >= 0, of the normal distribution, given e = exp(-x^2 / 2), to 4e-7 of itself
+// (x from 0 to 14, beside e's own error): (1 + erf(-x / sqrt 2)) / 2 comes in steps of
+// 3e-8, which is all of P from x = 5.4 on.  P(-x) / e falls from 1/2 like 1 / x, so it
+// is t (c0 + c1 t + ... + c7 t^7) with t = 1 / (1 + 0.305 x); the coefficients minimise
+// the largest relative error (least squares, reweighted), and 0.305 is the best of
+// the poles tried.  200 x 1760 x 4096 with GELU takes 11.5 us, with erfcf 13.5.
+__device__ __forceinline__ float normal_tail(float x, float e) {
+    const float t = __fdividef(1.0f, fmaf(0.305000007f, x, 1.0f));
+    float p = 0.0366991833f;
+    p = fmaf(p, t, -0.152988285f);
+    p = fmaf(p, t, 0.185716853f);
+    p = fmaf(p, t, -0.0379767828f);
+    p = fmaf(p, t, 0.121021651f);
+    p = fmaf(p, t, 0.103420876f);
+    p = fmaf(p, t, 0.122466817f);
+    p = fmaf(p, t, 0.121639736f);
+    return p * t * e;
+}
+
 // act(a) and its derivative.
 template <int ACT>
 __device__ __forceinline__ void activation(float a, float &v, float &dv) {
@@ -44,10 +63,12 @@ __device__ __forceinline__ void activation(float a, float &v, float &dv) {
         v = a > 0.0f ? a : (a != a ? a : 0.0f);
         dv = a > 0.0f ? 1.0f : 0.0f;
     } else if (ACT == ISAM_ACT_GELU) {
-        // a P(a) with P the normal distribution function, (1 + erf(a / sqrt 2)) / 2.
-        const float p = 0.5f + 0.5f * erff(a * 0.70710678118654752f);
+        // a P(a) with P the normal distribution function.
+        const float e = __expf(-0.5f * a * a);
+        const float q = normal_tail(fabsf(a), e);
+        const float p = a < 0.0f ? q : 1.0f - q;
         v = a * p;
-        dv = p + a * (0.39894228040143268f * __expf(-0.5f * a * a));
+        dv = p + a * (0.39894228040143268f * e);
     } else {
         const Gate s = gate(a);
         if (ACT == ISAM_ACT_SIGMOID) {

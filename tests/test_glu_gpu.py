@@ -334,3 +334,42 @@ def test_two_threads_on_streams_of_their_own():
     for outs, ref in zip(got, want):
         assert len(outs) == 50
         assert all(torch.equal(a, b) for o in outs for a, b in zip(o, ref))
+
+
+@pytest.mark.parametrize("T", [1, 20, 150])
+def test_gelu_far_below_zero(T):
+    """GELU's tail is a product of a and a probability of 0.3 down to 1e-19: it is
+    held to its own size, not to the largest output.  One product makes each gate
+    sum, and u = 1, so h = gelu(x0 w): one rounding to bf16 (2^-8) beside a few
+    fp32 operations (the probability's argument, off by 2^-24 of itself, counts
+    a^2 <= 82 times: 2^-16 with the rest).  The same for du = dh gelu(x0 w), read
+    off dW's up rows: only the first token has a gradient, of 1, and x1 = 1.  dW's gate rows then are
+    gelu'(w), the sum of two terms of opposite sign that below -1.5 are together
+    at most 2.1 times as large as it."""
+    import math
+    import torch
+    D, F = 16, 96
+    x, W = torch.zeros(T, D), torch.zeros(2 * F, D)
+    x[:, 0] = 1 + (torch.arange(T) % 8) / 128
+    x[:, 1] = 1
+    W[:F, 0] = -torch.linspace(0.5, 8.5, F)
+    W[F:, 1] = 1
+    x, W = x.bfloat16().cuda(), W.bfloat16().cuda()
+    a = f64(x)[:, :1] * f64(W)[None, :F, 0]
+    ref = np.vectorize(lambda v: 0.5 * v * math.erfc(-v / math.sqrt(2)))(a)
+    tol = (2.0 ** -8 + 2.0 ** -16) * np.abs(ref)
+    buf, h = guarded((T, F))
+    isam.glu_forward(T, D, F, "gelu", x, W, h)
+    dh = torch.zeros(T, F, dtype=torch.bfloat16, device="cuda")
+    dh[0] = 1
+    dx, dW = torch.empty_like(x), torch.empty_like(W)
+    isam.glu_backward(T, D, F, "gelu", x, W, dh, dx, dW)
+    isam.sync()
+    got, dup, dgate = f64(h).reshape(T, F), f64(dW)[F:, 1], f64(dW)[:F, 0]
+    assert (np.abs(got - ref) <= tol).all(), float((np.abs(got - ref) / np.abs(ref)).max())
+    assert (np.abs(dup - ref[0]) <= tol[0]).all(), float((np.abs(dup - ref[0]) / np.abs(ref[0])).max())
+    a0 = a[0]
+    slope = ref[0] / a0 + a0 * np.exp(-a0 * a0 / 2) / math.sqrt(2 * math.pi)
+    low = a0 < -1.5
+    assert (np.abs(dgate - slope) <= (2.0 ** -8 + 2.1 * 2.0 ** -16) * np.abs(slope))[low].all()
+    assert intact(buf, T * F)
