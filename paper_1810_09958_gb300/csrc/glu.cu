@@ -1030,7 +1030,7 @@ constexpr int kOneThreads = 128, kOneRows = 8;
 __global__ void __launch_bounds__(kOneThreads)
     glu_outer_few_kernel(int T, int D, int64_t F2, const uint16_t *d, const uint16_t *x, uint16_t *dW) {
     const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kOneRows;
-    const int col = (blockIdx.y * kOneThreads + threadIdx.x) * 8;
+    const int col = static_cast<int>((blockIdx.z * gridDim.y + blockIdx.y) * kOneThreads + threadIdx.x) * 8;
     if (col >= D) return;
     dependent_start();
     unsigned long long sum[kOneRows][4] = {};
@@ -1163,10 +1163,12 @@ int glu_backward_launch(const GluDesc &d, DeviceState &ds, cudaStream_t s) {
         if (rc) return rc;
     }
     if (d.dW && d.T <= kOneTokens) {
-        const int cols = tiles_of(d.D, 8 * kOneThreads);
-        if (cols > 65535) return set_error(ISAM_ERR_UNSUPPORTED, "isam_glu_backward: D (%d) is too large", d.D);
-        return launch_dependent(glu_outer_few_kernel, dim3(static_cast<unsigned>(F2 / kOneRows), static_cast<unsigned>(cols)),
-                                kOneThreads, 0, s, 1, "launch glu_outer_few_kernel", d.T, d.D, F2, dg, d.x, d.dW);
+        // Columns by y and, beyond a grid's 65535, by z too: a few blocks at the end may have none.
+        const int cols = tiles_of(d.D, 8 * kOneThreads), layers = tiles_of(cols, 65535);
+        const dim3 grid(static_cast<unsigned>(F2 / kOneRows), static_cast<unsigned>(tiles_of(cols, layers)),
+                        static_cast<unsigned>(layers));
+        return launch_dependent(glu_outer_few_kernel, grid, kOneThreads, 0, s, 1, "launch glu_outer_few_kernel", d.T, d.D,
+                                F2, dg, d.x, d.dW);
     }
     if (d.dW && d.T <= kOuterTokens) {
         const int cols = tiles_of(d.D, kOuterCols);

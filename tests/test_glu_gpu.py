@@ -373,3 +373,28 @@ def test_gelu_far_below_zero(T):
     low = a0 < -1.5
     assert (np.abs(dgate - slope) <= (2.0 ** -8 + 2.1 * 2.0 ** -16) * np.abs(slope))[low].all()
     assert intact(buf, T * F)
+
+
+@pytest.mark.parametrize("T", [1, 4, 5])
+def test_backward_of_very_deep_rows(T):
+    """More columns of dW than a grid has rows of blocks (65535 of 1024): x and W
+    are integers in a few columns and zero elsewhere, so every result is exact
+    and small."""
+    import torch
+    D, F = 65536 * 1024 + 8, 8
+    at = [0, 1, 1023, D // 2, D - 9, D - 8, D - 1]
+    rng = np.random.default_rng(T)
+    xs = rng.integers(-1, 2, (T, len(at))).astype(np.float64)
+    ws = rng.integers(-1, 2, (2 * F, len(at))).astype(np.float64)
+    x, W = torch.zeros(T, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(2 * F, D, dtype=torch.bfloat16, device="cuda")
+    x[:, at], W[:, at] = torch.from_numpy(xs).bfloat16().cuda(), torch.from_numpy(ws).bfloat16().cuda()
+    dh = torch.from_numpy(rng.integers(-1, 2, (T, F)).astype(np.float64)).bfloat16().cuda()
+    dx, dW = torch.full_like(x, float("nan")), torch.full_like(W, float("nan"))
+    isam.glu_backward(T, D, F, "relu", x, W, dh, dx, dW)
+    isam.sync()
+    rx, rw, d = lm_ref.glu_backward(xs, ws, f64(dh), "relu")
+    exact = lambda v: torch.from_numpy(v).float().bfloat16().double().numpy()
+    assert np.abs(d).max() < 256
+    assert np.array_equal(f64(dx[:, at]), exact(rx)) and np.array_equal(f64(dW[:, at]), exact(rw))
+    dx[:, at], dW[:, at] = 0, 0
+    assert not dx.any() and not dW.any()
