@@ -32,11 +32,11 @@
 // The backward pass is the same scan from the last step to the first with
 // e_t = z_t (dh_t + e_{t+1}), d_t = dh_t + e_{t+1}.
 #include <algorithm>
-#include <mutex>
 #include <type_traits>
 
 #include "gemm_common.cuh"
 #include "internal.h"
+#include "known.h"
 #include "lm_common.cuh"
 #include "ptx.cuh"
 
@@ -1077,37 +1077,33 @@ int rows_tmap(CUtensorMap *out, const void *p, int type, int hidden, int64_t row
 
 // Clusters of `c` CTAs of this kernel resident at once, asked once per device,
 // kernel and shape.
-int resident_clusters(const void *fn, int c, int threads, int smem, const DeviceState &ds) {
-    struct Known {
+int resident_clusters(const void *fn, int c, int threads, int smem, const DeviceState &ds, int *n) {
+    struct Key {
         int device;
         const void *fn;
-        int c, threads, n;
+        int c, threads;
+        bool operator==(const Key &o) const {
+            return device == o.device && fn == o.fn && c == o.c && threads == o.threads;
+        }
     };
-    static std::mutex mu;
-    static Known known[512];
-    static int count = 0;
-    std::lock_guard<std::mutex> lk(mu);
-    for (int i = 0; i < count; ++i)
-        if (known[i].device == ds.device && known[i].fn == fn && known[i].c == c && known[i].threads == threads)
-            return known[i].n;
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    cfg.gridDim = dim3(static_cast<unsigned>(c * ds.num_sms));
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = c;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, fn, &cfg) != cudaSuccess) {
+    static Known<Key, 512> known;
+    return known.get(Key{ds.device, fn, c, threads}, n, [&](int *clusters) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        cfg.gridDim = dim3(static_cast<unsigned>(c * ds.num_sms));
+        cfg.blockDim = dim3(threads);
+        cfg.dynamicSmemBytes = smem;
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = c;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        const cudaError_t e = cudaOccupancyMaxActiveClusters(clusters, fn, &cfg);
+        if (e == cudaSuccess) return static_cast<int>(ISAM_OK);
         cudaGetLastError();
-        n = 0;
-    }
-    if (count < 512) known[count++] = Known{ds.device, fn, c, threads, n};
-    return n;
+        return cuda_error(e, "cudaOccupancyMaxActiveClusters(gated linear recurrence)");
+    });
 }
 
 // Fills in the launch shape: `smem` bytes a warp.  The cluster size is the one
@@ -1127,15 +1123,17 @@ int scan_shape(const void *fn, const GlrDesc &d, int smem, const DeviceState &ds
     p.groups = static_cast<uint32_t>(groups);
     const int warps = std::min(S::kWarps, (d.T + L - 1) / L);
     const int bytes = smem * warps;
-    const int rc = ensure_smem_optin(fn, smem * S::kWarps, ds.device, "cudaFuncSetAttribute(gated linear recurrence)");
+    int rc = ensure_smem_optin(fn, smem * S::kWarps, ds.device, "cudaFuncSetAttribute(gated linear recurrence)");
     if (rc) return rc;
     int64_t best = 0, grid = 0;
     for (int c = 1; c <= kMaxCluster; ++c) {
         const int64_t span = static_cast<int64_t>(c) * warps * L;
         if (c > 1 && span - warps * L >= d.T) break;  // CTAs without steps
-        const int64_t resident = resident_clusters(fn, c, 32 * warps, bytes, ds);
-        if (resident < 1) continue;
-        const int64_t ids = std::min(resident, groups);
+        int resident = 0;
+        const int failed = resident_clusters(fn, c, 32 * warps, bytes, ds, &resident);
+        if (failed) rc = failed;  // of another size, perhaps not
+        if (failed || resident < 1) continue;
+        const int64_t ids = std::min<int64_t>(resident, groups);
         const int64_t cost = (d.T + span - 1) / span * ((groups + ids - 1) / ids);
         if (grid == 0 || cost < best) {
             best = cost;
@@ -1143,6 +1141,7 @@ int scan_shape(const void *fn, const GlrDesc &d, int smem, const DeviceState &ds
             p.cluster = static_cast<uint32_t>(c);
         }
     }
+    if (grid == 0 && rc) return rc;
     if (grid == 0) return set_error(ISAM_ERR_UNSUPPORTED, "the gated linear recurrence's kernel fits no SM");
     cfg.gridDim = dim3(static_cast<unsigned>(grid));
     cfg.blockDim = dim3(32 * warps);
