@@ -413,3 +413,54 @@ def test_step_equals_a_sequence_of_one():
     isam.sync()
     tol = F32 * float(last.abs().max())
     assert (h - out[0]).abs().max() <= tol and (state - last).abs().max() <= tol
+
+
+# Rows by TMA, as lane words and as covering words (bf16 gates), and walked.
+FORMS = [(70, 3, 128), (70, 3, 66), (70, 3, 67), (9, 3, 66)]
+
+
+@pytest.mark.parametrize("gt,ht", TYPES)
+@pytest.mark.parametrize("T,B,H", FORMS)
+@pytest.mark.parametrize("lengths", [None, [70, 0, 33]])
+def test_no_gradient_of_the_states(T, B, H, lengths, gt, ht):
+    """dh_out = NULL stands for zeros: the same bits, from dh_last alone."""
+    import torch
+    g, h0, _, _, dl = make(T, B, H, gt, ht, seed=T + H)
+    g, h0, dl = g.cuda(), h0.cuda(), dl.cuda()
+    n = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    h = torch.empty(T, B, H, dtype=tdtype(ht), device="cuda")
+    isam.glr_forward(T, B, H, g, h0, n, h)
+    got = []
+    for dh in (torch.zeros_like(h), None):
+        gb, dg = guarded((T, B, 2 * H), tdtype(gt))
+        eb, dh0 = guarded((B, H), torch.float32)
+        isam.glr_backward(T, B, H, g, h0, n, h, dh, dl, dg, dh0)
+        isam.sync()
+        assert intact(gb, T * B * 2 * H) and intact(eb, B * H)
+        assert torch.isfinite(dg).all() and dg.any()
+        got.append((dg, dh0))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("gt,ht", TYPES)
+@pytest.mark.parametrize("T,B,H", FORMS + [(1536, 5, 2048), (1536, 5, 2046), (1500, 3, 1021)])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_states_in_place_give_the_same_bits(T, B, H, ragged, gt, ht):
+    """h_last = h0 and dh0 = dh_last, also where a cluster of several CTAs takes
+    several groups of channels one after another (5 x 2048)."""
+    import torch
+    g, h0, _, dh, dl = make(T, B, H, gt, ht, seed=T + H)
+    g, h0, dh, dl = g.cuda(), h0.cuda(), dh.cuda(), dl.cuda()
+    n = torch.tensor([(T * b) // (B - 1) for b in range(B)], dtype=torch.int32, device="cuda") if ragged else None
+    out = []
+    for in_place in (False, True):
+        h = torch.empty(T, B, H, dtype=tdtype(ht), device="cuda")
+        state, e = h0.clone(), dl.clone()
+        last = state if in_place else torch.empty_like(state)
+        dh0 = e if in_place else torch.empty_like(e)
+        isam.glr_forward(T, B, H, g, state, n, h, last)
+        dg = torch.empty_like(g)
+        isam.glr_backward(T, B, H, g, h0, n, h, dh, e, dg, dh0)
+        isam.sync()
+        out.append((h, last, dg, dh0))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
