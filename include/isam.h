@@ -60,7 +60,9 @@ enum {
 int isam_version(void);
 
 /* Stream for subsequent calls from any thread: a cudaStream_t passed as
- * void*, or NULL for the legacy default stream.  Returns ISAM_OK. */
+ * void*, or NULL for the legacy default stream.  Threads that use several
+ * streams keep each other out from setting it to the end of the call that is
+ * to run there.  Returns ISAM_OK. */
 int isam_set_stream(void *stream);
 
 /* Waits for the stream, then reads and clears the device error word.

@@ -58,7 +58,10 @@ constexpr int kStages = 2;  // tiles of each input in a warp's ring
 // Rows that TMA does not bring cost the warps more instructions a step, and more
 // warps hide them: 4 warps of 32 / 16 steps and 8 of 16 / 8, 7791 x 3 x 2042
 // backward 202, 121; 3104 x 1 x 1757 forward 29, 24; 4096 x 8 x 1022 backward
-// 108, 112.
+// 108, 112.  With one fp32 channel a lane forward it goes by length, and this form
+// is the one for few rounds: 4 warps, 4 CTAs an SM and 8 warps, 2 CTAs, 777 x 6 x 1001
+// 18.0, 20.9 (ragged 15.3, 17.1), but 3104 x 1 x 1757 22.7, 20.1 and 20000 x 1 x 1001
+// 87, 69.
 template <int V, bool BACK, bool TMA>
 struct Shape;
 template <>
@@ -549,10 +552,12 @@ __device__ __forceinline__ void put_edge(float *to, const Group<V> &g, const Lan
 }
 
 // Forward.  Bound by HBM where sequences are long (65536 x 1 x 2560 bf16 169 us,
-// 5.9 TB/s, 0.87 of the copy bandwidth), by the chain of one round's folds
-// through a cluster where they are short (128 x 32 x 1024, fp32 gates, 9.8 us,
-// 0.64), and without TMA by the instructions that copy and store words
-// (777 x 6 x 1001, fp32, ragged, 13.9 us, 0.33).
+// 5.9 TB/s, 0.87 of the copy bandwidth); where they are short by a launch, first
+// loads and few rounds that follow each other (128 x 32 x 1024, fp32 gates, 9.8 us,
+// 0.64: 1024 groups on 608 CTAs, two turns of two rounds, no clusters; clusters of two
+// would have four turns of one); without TMA by the instructions that copy and
+// store words (777 x 6 x 1001, fp32, 18.0 us, 0.46) and, ragged, by the longest
+// sequences, as turns are dealt out as if all had T steps (13.8 us, 0.33).
 template <typename G, typename Hy, int V, int L, Rows ROWS>
 __global__ void __launch_bounds__(32 * Shape<V, false, ROWS == kTma>::kWarps, (Shape<V, false, ROWS == kTma>::kCtas))
     glr_forward_kernel(const __grid_constant__ CUtensorMap tm_g, const __grid_constant__ CUtensorMap tm_h,
@@ -1131,7 +1136,7 @@ int scan_shape(const void *fn, const GlrDesc &d, int smem, const DeviceState &ds
         if (c > 1 && span - warps * L >= d.T) break;  // CTAs without steps
         int resident = 0;
         const int failed = resident_clusters(fn, c, 32 * warps, bytes, ds, &resident);
-        if (failed) rc = failed;  // of another size, perhaps not
+        if (failed) rc = failed;  // matters where every size fails
         if (failed || resident < 1) continue;
         const int64_t ids = std::min<int64_t>(resident, groups);
         const int64_t cost = (d.T + span - 1) / span * ((groups + ids - 1) / ids);
@@ -1210,7 +1215,7 @@ int walk_launch(void (*fn)(const GlrDesc, int64_t), const GlrDesc &d, int V, cud
 }  // namespace
 
 // V keeps a row of a warp at 128 bytes of gates, L its z and b (backward: four
-// values a step) within the registers of two CTAs an SM.
+// values a step) within the registers that Shape's CTAs an SM leave.
 int glr_forward_launch(const GlrDesc &d, DeviceState &ds, cudaStream_t s) {
     return by_types(d.g_type, d.h_type, [&](auto gt, auto ht) {
         using G = decltype(gt);

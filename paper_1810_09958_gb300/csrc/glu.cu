@@ -16,7 +16,9 @@
 // token rows.
 //
 // Up to 32 tokens are a reading of W: glu_few_kernel streams 8 gate and 8 up rows
-// at a time through m16n8k16.
+// at a time through m16n8k16, as long as x fits shared memory beside the rings: a D of
+// up to 8832 at 8 tokens, 3904 at 16, 2240 at 20, 1408 at 32.  Beyond that the pair
+// kernel runs with most of its 256 rows empty.
 #include <algorithm>
 
 #include "gemm_common.cuh"
@@ -175,10 +177,12 @@ __device__ __forceinline__ void stage32(uint8_t *tile, int lane, int half, const
 // descriptors advanced as 32-bit words: from a single diverged thread a 64-deep
 // block took 644 cycles at every width, more than its MMAs (8192 x 4096 x 8192
 // 558 us, 200 x 1760 x 4096 13.8).  Bound by the tensor cores where tiles fill the
-// GPU: 8192 x 4096 x 8192 forward 542 us, 2030 TFLOP/s, 1.03 of the measured bf16
-// burst; 4096 x 2560 x 7680 backward, three launches of this kernel and one sum,
-// 496 to 524 us (box to box), 0.93 to 0.99.  By the chain of first loads, one round
-// of blocks and the epilogue where they do not: 200 x 1760 x 4096 11.7 us, 0.39 of
+// GPU.  In short bursts 8192 x 4096 x 8192 forward 518 to 542 us, 1.03 to 1.07 of the
+// measured bf16 burst, and 4096 x 2560 x 7680 backward, three launches of this kernel
+// and one sum, 496 to 524 us (box to box), 0.93 to 0.99; in a stream of calls, under
+// the power cap, 612 us and 580 to 590, 1.03 and 0.94 to 0.95 of the measured sustained rate
+// (0.91 and 0.83 of the burst).  By the chain of first loads, one round of
+// blocks and the epilogue where they do not: 200 x 1760 x 4096 11.5 us, 0.40 of
 // reading its bytes.
 template <Role ROLE, int BN, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kThreads, 1)
