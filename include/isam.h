@@ -575,6 +575,197 @@ int isam_w4_pack(int N, int K, int group, const uint8_t *codes, const isam_bf16 
 int isam_gemv_w4(int M, int N, int K, int group, const isam_bf16 *x, const uint8_t *tiled,
                  const isam_bf16 *tiled_scales, float *y);
 
+/*
+ * Root-mean-square norm of the rows of a residual stream, with the addition
+ * before it:
+ *   r = x + res,   y = r / sqrt(mean(r^2) + eps) * w.
+ *   x        [T][D], fp32 (what isam_gemm writes) or bf16 (x_type)
+ *   res      [T][D] (r_type), or NULL: r = x
+ *   res_out  [T][D] (r_type): r rounded to its type, or NULL if not wanted; may
+ *            be res itself
+ *   w        [D] fp32
+ * and one of
+ *   y        [T][D] (y_type), or
+ *   y8, y8_scales: the operand of isam_gemm_mxfp8, E4M3 bytes [T][D] and E8M0
+ *            bytes [ceil(D/128)][T][4].  A block of 32 gets the least power of
+ *            two that leaves none of its values above 448 (2^-127 at least, so
+ *            bytes of zeros and of blocks past D are 0); each value over its scale is rounded
+ *            to the nearest E4M3, ties to even.  A block with a NaN or an
+ *            infinity gets the scale 255 (NaN) and 0x7f in every byte.
+ * The other is NULL.  y is formed from the unrounded r; sums are fp32.
+ * 1 <= D <= 32768, eps >= 0 and finite.  res_out (unless it is res) and y may
+ * overlap no input.  Pointers aligned to their element, y8_scales to 4 bytes;
+ * rows that start on 16-byte boundaries are faster.  ISAM_ERR_INVALID_ARG for
+ * sizes < 1, null pointers, unknown types, both outputs or neither, or another
+ * eps; ISAM_ERR_UNSUPPORTED for misaligned pointers or larger D.
+ * Asynchronous on the stream set by isam_set_stream; no workspace.
+ */
+int isam_rms_norm_forward(int T, int D, int x_type, const void *x, int r_type, const void *res, void *res_out,
+                          const float *w, float eps, int y_type, void *y, uint8_t *y8, uint8_t *y8_scales);
+
+/* Bytes of isam_rms_norm_backward's workspace (host arithmetic only). */
+int isam_rms_norm_backward_workspace(int T, int D, size_t *bytes);
+
+/*
+ * Its backward pass, from r as res_out holds it (x itself without a residual).
+ * With k = 1 / sqrt(mean(r^2) + eps), n = r k and d = w dy,
+ *   dx = k (d - n mean(d n)) + dres,   dw = sum over rows of dy n.
+ *   dy    [T][D] (g_type)
+ *   dres  [T][D] (g_type): the gradient that reaches r past the norm, or NULL
+ *   dx    [T][D] (g_type): the gradient of x and of res alike, or NULL if not
+ *         wanted; may be dres or dy itself
+ *   dw    [D] fp32, or NULL if not wanted
+ *   workspace: isam_rms_norm_backward_workspace bytes of device memory,
+ *         16-byte aligned, owned by the caller and free again when the call has
+ *         completed on its stream (calls on several streams need one each);
+ *         NULL is taken where dw is NULL.
+ * The forward call keeps nothing: k is computed again.  Sums are fp32 and in a
+ * fixed order.  Limits, status codes and execution as isam_rms_norm_forward.
+ */
+int isam_rms_norm_backward(int T, int D, int r_type, const void *r, const float *w, float eps, int g_type,
+                           const void *dy, const void *dres, void *workspace, void *dx, float *dw);
+
+/*
+ * Short causal convolution over time, each channel by itself:
+ *   y_t[c] = act(bias[c] + sum_{j < width} w[j][c] x_{t - width + 1 + j}[c]).
+ *   x          [T][batch] rows of C values, row t * batch + b at x + (t * batch + b) * x_stride
+ *              (the first or last C columns of a projection's rows, for one);
+ *              fp32 or bf16 (x_type)
+ *   w          [width][C] fp32,  bias [C] fp32 or NULL
+ *   silu       1: act(v) = v sigmoid(v), 0: act(v) = v
+ *   state      [batch][width - 1][C] (x_type): the inputs before the first, oldest
+ *              first, or NULL for zeros
+ *   lengths    [batch] int32 on the device, or NULL (every sequence has T
+ *              steps); clamped to [0, T].  Steps t >= lengths[b] are padding:
+ *              whatever x holds there is not used and y is zero.
+ *   y          [T][batch][C] (y_type)
+ *   new_state  [batch][width - 1][C] (x_type), or NULL: the last inputs of each
+ *              sequence, for isam_conv1d_step; may be state itself
+ * Sums are fp32.  2 <= width <= 8, x_stride >= C, at most 2^40 values of y;
+ * pointers aligned to their element.  ISAM_ERR_INVALID_ARG for sizes < 1, null
+ * pointers, unknown types, silu not 0 or 1 or x_stride < C;
+ * ISAM_ERR_UNSUPPORTED beyond the limits or for misaligned pointers.
+ * Asynchronous on the stream set by isam_set_stream; no workspace.
+ */
+int isam_conv1d_forward(int T, int batch, int C, int width, int x_type, const void *x, int64_t x_stride,
+                        const float *w, const float *bias, int silu, const void *state, const int32_t *lengths,
+                        int y_type, void *y, void *new_state);
+
+/*
+ * One token of it for `batch` sequences whose last inputs sit in a cache of
+ * `slots` entries; slot_ids, state and new_state as in isam_glr_step.
+ *   x [batch] rows of C values, x_stride apart;  y [batch][C]
+ *   state, new_state  [slots][width - 1][C] (x_type)
+ * A padding row (slot outside [0, slots)) gets y = 0 and touches no state.
+ */
+int isam_conv1d_step(int batch, int C, int width, int slots, int x_type, const void *x, int64_t x_stride,
+                     const float *w, const float *bias, int silu, const int32_t *slot_ids, const void *state,
+                     void *new_state, int y_type, void *y);
+
+/*
+ * Selective state space scan: N states a channel that decay at rates their
+ * input sets.  With delta = softplus(dt + dt_bias), for channel c, state n,
+ *   h_t = exp(delta_t[c] A[c][n]) h_{t-1} + delta_t[c] B_t[n] u_t[c],
+ *   y_t[c] = (sum_n C_t[n] h_t + D[c] u_t[c]) * z_t[c] sigmoid(z_t[c]).
+ *   u        [T][batch][C], fp32 or bf16 (u_type), as y
+ *   dt       [T][batch][C] (p_type: fp32, what isam_gemm writes, or bf16),
+ *            dt_bias [C] fp32 or NULL
+ *   A        [C][N] fp32
+ *   B, Cm    [T][batch] rows of N values (p_type), bc_stride apart (columns of
+ *            one projection's rows)
+ *   D        [C] fp32, or NULL for zeros
+ *   z        [T][batch] rows of C values (p_type), z_stride apart, or NULL: no
+ *            such factor
+ *   h0       [batch][C][N] fp32, or NULL for zeros
+ *   lengths  as in isam_conv1d_forward: padding's inputs are not used, y is
+ *            zero there and the state stays
+ *   y        [T][batch][C] (u_type)
+ *   h_last   [batch][C][N] fp32 or NULL: the states after lengths[b] steps (h0
+ *            where that is none); may be h0 itself
+ * Gates, decays, states and sums are fp32; y alone is rounded.  Results do not
+ * depend on timing.  1 <= N <= 128, strides >= their rows, at most 2^40 values
+ * of y; pointers aligned to their element.  ISAM_ERR_INVALID_ARG for sizes < 1,
+ * null pointers, unknown types or shorter strides; ISAM_ERR_UNSUPPORTED beyond
+ * the limits or for misaligned pointers.  Asynchronous on the stream set by
+ * isam_set_stream; no workspace.
+ */
+int isam_ssm_forward(int T, int batch, int C, int N, int u_type, const void *u, int p_type, const void *dt,
+                     const float *dt_bias, const float *A, const void *B, const void *Cm, int64_t bc_stride,
+                     const float *D, const void *z, int64_t z_stride, const float *h0, const int32_t *lengths,
+                     void *y, float *h_last);
+
+/*
+ * One token of it for `batch` sequences whose states sit in a cache of `slots`
+ * entries; slot_ids, state and new_state as in isam_glr_step.
+ *   u, dt, z, y [batch][C] (z rows z_stride apart), B, Cm [batch] rows of N
+ *   state, new_state  [slots][C][N] fp32
+ * A padding row gets y = 0 and touches no state.
+ */
+int isam_ssm_step(int batch, int C, int N, int slots, int u_type, const void *u, int p_type, const void *dt,
+                  const float *dt_bias, const float *A, const void *B, const void *Cm, int64_t bc_stride,
+                  const float *D, const void *z, int64_t z_stride, const int32_t *slot_ids, const float *state,
+                  float *new_state, void *y);
+
+/* Bytes of isam_beam_select's workspace (host arithmetic only). */
+int isam_beam_select_workspace(int batch, int beams, int V, int count, size_t *bytes);
+
+/*
+ * Beam search's selection: the `count` best continuations of each of `batch`
+ * sequences' `beams` beams by
+ *   scores[b][k] + log_softmax(logits[b][k])[v],
+ * best first.
+ *   logits    [batch][beams][V], fp32 (what isam_gemm and isam_gemv_w4 write) or
+ *             bf16 (l_type).  -inf forbids a token, and so does NaN.  A row
+ *             whose largest logit is +inf or -inf has no continuation.
+ *   scores    [batch][beams] fp32: each beam's sum of log-probabilities; -inf (or
+ *             NaN, or +inf) marks a beam that has no continuation
+ *   eos       the token that ends a sequence, or -1
+ *   finished  [batch][beams] bytes, or NULL: a beam that has ended (byte not 0)
+ *             has one continuation, token eos at its own score; its logits are not used
+ *   new_scores, parents, tokens  [batch][count]: score (fp32), beam and token of
+ *             each.  Places that no continuation fills get -inf, 0 and 0.
+ *   new_finished [batch][count] bytes, or NULL: 1 where the beam has ended, by
+ *             this token or before
+ * Scores are formed in 64 bits from sums of fp32 exponentials and compared there;
+ * equal ones go to the lower beam, and within a beam to the larger logit, then
+ * to the lower token.  new_scores may be scores and new_finished finished where
+ * count = beams; otherwise outputs overlap no input.
+ *   workspace: isam_beam_select_workspace bytes of device memory, 16-byte
+ *             aligned, owned by the caller and free again when the call has
+ *             completed on its stream (calls on several streams need one each).
+ * 1 <= beams, count <= 64, batch * beams <= 2^20, V <= 2^28; pointers
+ * aligned to their element.  ISAM_ERR_INVALID_ARG for sizes < 1, null pointers,
+ * an unknown type, eos outside [-1, V), or finished without eos;
+ * ISAM_ERR_UNSUPPORTED beyond the limits or for misaligned pointers.
+ * Asynchronous on the stream set by isam_set_stream.
+ */
+int isam_beam_select(int batch, int beams, int V, int count, int l_type, const void *logits, const float *scores,
+                     int eos, const uint8_t *finished, void *workspace, float *new_scores, int32_t *parents,
+                     int32_t *tokens, uint8_t *new_finished);
+
+/*
+ * States follow the chosen beams: for every layer, sequence b and beam k,
+ *   new_state[layer][slot(b, k)] = state[layer][slot(b, parents[b][k])],
+ * slot(b, k) = slot_ids[b * beams + k], or b * beams + k without slot_ids.
+ *   parents   [batch][beams] int32
+ *   slot_ids  [batch][beams] int32, distinct where they are valid, or NULL
+ *             (batch * beams <= slots)
+ *   state     [layers][slots] rows of row_bytes bytes: the caches of
+ *             isam_glr_step, isam_conv1d_step or isam_ssm_step
+ *   new_state the same shape; `state` itself (rows change places) or another
+ *             buffer that does not overlap it, of which only the rows of
+ *             slot_ids are written
+ * A row is left as it is where its parent is outside [0, beams) or its own or
+ * its parent's slot outside [0, slots).
+ * 1 <= beams <= 64, batch * beams <= 2^20, layers * slots <= 2^31 - 1,
+ * row_bytes <= 2^31 - 1.  ISAM_ERR_INVALID_ARG for sizes < 1 or null pointers;
+ * ISAM_ERR_UNSUPPORTED beyond the limits or for a misaligned parents or
+ * slot_ids.  Rows that start on 16-byte boundaries are faster.
+ * Asynchronous on the stream set by isam_set_stream; no workspace.
+ */
+int isam_beam_reorder(int layers, int batch, int beams, int slots, size_t row_bytes, const int32_t *parents,
+                      const int32_t *slot_ids, const void *state, void *new_state);
+
 #ifdef __cplusplus
 }
 #endif

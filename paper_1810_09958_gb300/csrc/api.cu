@@ -743,4 +743,235 @@ int isam_gemv_w4(int M, int N, int K, int group, const isam_bf16 *x, const uint8
     return gemv_w4_launch(M, N, K, group, x, tiled, tiled_scales, y, *ds, current_stream());
 }
 
+namespace {
+
+bool type_ok(int t) { return t == ISAM_F32 || t == ISAM_BF16; }
+unsigned type_size(int t) { return t == ISAM_F32 ? 4 : 2; }
+
+int norm_validate(const char *name, int T, int D, float eps) {
+    if (T < 1 || D < 1) return set_error(ISAM_ERR_INVALID_ARG, "%s: sizes must be >= 1", name);
+    if (!(eps >= 0.0f) || eps > 3.0e38f)
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: eps must be >= 0 and finite", name);
+    if (D > 32768) return set_error(ISAM_ERR_UNSUPPORTED, "%s: D (%d) is above 32768", name, D);
+    return ISAM_OK;
+}
+
+// What the convolution's two entries check alike.
+int conv1d_validate(const char *name, const ConvDesc &p) {
+    if (p.T < 1 || p.batch < 1 || p.C < 1 || p.width < 1 || p.slots < 1)
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: sizes must be >= 1", name);
+    if (!type_ok(p.x_type) || !type_ok(p.y_type))
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: types must be ISAM_F32 or ISAM_BF16", name);
+    if (p.silu != 0 && p.silu != 1) return set_error(ISAM_ERR_INVALID_ARG, "%s: silu must be 0 or 1", name);
+    if (!p.x || !p.w || !p.y) return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
+    if (p.x_stride < p.C) return set_error(ISAM_ERR_INVALID_ARG, "%s: x_stride below C", name);
+    if (p.width < 2 || p.width > 8)
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: width (%d) must be 2 to 8", name, p.width);
+    if (static_cast<int64_t>(p.batch) * p.C > (int64_t{1} << 40) / p.T || p.x_stride > (int64_t{1} << 40) / p.T / p.batch)
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: more than 2^40 values", name);
+    if (!aligned(p.x, type_size(p.x_type)) || !aligned(p.state, type_size(p.x_type)) ||
+        !aligned(p.new_state, type_size(p.x_type)) || !aligned(p.y, type_size(p.y_type)) || !aligned(p.w, 4) ||
+        !aligned(p.bias, 4) || !aligned(p.lengths, 4) || !aligned(p.slot_ids, 4))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: a pointer is not aligned to its element", name);
+    return ISAM_OK;
+}
+
+// What the scan's two entries check alike.
+int ssm_validate(const char *name, const SsmDesc &p) {
+    if (p.T < 1 || p.batch < 1 || p.C < 1 || p.N < 1 || p.slots < 1)
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: sizes must be >= 1", name);
+    if (!type_ok(p.u_type) || !type_ok(p.p_type))
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: types must be ISAM_F32 or ISAM_BF16", name);
+    if (!p.u || !p.dt || !p.A || !p.B || !p.Cm || !p.y) return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
+    if (p.bc_stride < p.N || (p.z && p.z_stride < p.C))
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: a stride is below its row", name);
+    if (p.N > 128) return set_error(ISAM_ERR_UNSUPPORTED, "%s: N (%d) is above 128", name, p.N);
+    const int64_t most = (int64_t{1} << 40) / p.T / p.batch;
+    if (p.C > most || p.bc_stride > most || (p.z && p.z_stride > most))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: more than 2^40 values", name);
+    const unsigned ps = type_size(p.p_type), us = type_size(p.u_type);
+    if (!aligned(p.u, us) || !aligned(p.y, us) || !aligned(p.dt, ps) || !aligned(p.B, ps) || !aligned(p.Cm, ps) ||
+        !aligned(p.z, ps) || !aligned(p.dt_bias, 4) || !aligned(p.A, 4) || !aligned(p.D, 4) || !aligned(p.lengths, 4) ||
+        !aligned(p.slot_ids, 4) || !aligned(p.state, 4) || !aligned(p.new_state, 4))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: a pointer is not aligned to its element", name);
+    return ISAM_OK;
+}
+
+int cache_validate(const char *name, int batch, int slots, const int32_t *slot_ids, const void *state,
+                   const void *new_state) {
+    if (!state || !new_state) return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
+    if (!slot_ids && batch > slots)
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: batch (%d) above slots (%d) without slot_ids", name, batch, slots);
+    return ISAM_OK;
+}
+
+int beam_validate(const char *name, int batch, int beams, int V, int count) {
+    if (batch < 1 || beams < 1 || V < 1 || count < 1)
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: sizes must be >= 1", name);
+    if (beams > 64 || count > 64 || static_cast<int64_t>(batch) * beams > (1 << 20) || V > (1 << 28))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: beams or count above 64, batch * beams above 2^20 or V above 2^28",
+                         name);
+    return ISAM_OK;
+}
+
+}  // namespace
+
+int isam_rms_norm_forward(int T, int D, int x_type, const void *x, int r_type, const void *res, void *res_out,
+                          const float *w, float eps, int y_type, void *y, uint8_t *y8, uint8_t *y8_scales) {
+    const char *name = "isam_rms_norm_forward";
+    int rc = norm_validate(name, T, D, eps);
+    if (rc) return rc;
+    if (!type_ok(x_type) || !type_ok(r_type) || !type_ok(y_type))
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: types must be ISAM_F32 or ISAM_BF16", name);
+    if (!x || !w) return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
+    if ((y != nullptr) == (y8 != nullptr) || (y8 != nullptr) != (y8_scales != nullptr))
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: either y or y8 and y8_scales", name);
+    if (!aligned(x, type_size(x_type)) || !aligned(res, type_size(r_type)) || !aligned(res_out, type_size(r_type)) ||
+        !aligned(w, 4) || !aligned(y, type_size(y_type)) || !aligned(y8_scales, 4))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: a pointer is not aligned to its element", name);
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    NormDesc p{};
+    p.T = T, p.D = D, p.x_type = x_type, p.r_type = r_type, p.y_type = y ? y_type : -1;
+    p.x = x, p.res = res, p.res_out = res_out, p.w = w, p.eps = eps, p.y = y, p.y8 = y8, p.y8_scales = y8_scales;
+    return norm_forward_launch(p, *ds, current_stream());
+}
+
+int isam_rms_norm_backward_workspace(int T, int D, size_t *bytes) {
+    if (T < 1 || D < 1 || !bytes)
+        return set_error(ISAM_ERR_INVALID_ARG, "isam_rms_norm_backward_workspace: sizes must be >= 1, bytes non-null");
+    *bytes = norm_backward_workspace(T, D);
+    return ISAM_OK;
+}
+
+int isam_rms_norm_backward(int T, int D, int r_type, const void *r, const float *w, float eps, int g_type,
+                           const void *dy, const void *dres, void *workspace, void *dx, float *dw) {
+    const char *name = "isam_rms_norm_backward";
+    int rc = norm_validate(name, T, D, eps);
+    if (rc) return rc;
+    if (!type_ok(r_type) || !type_ok(g_type))
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: types must be ISAM_F32 or ISAM_BF16", name);
+    if (!r || !w || !dy || (dw && !workspace)) return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
+    if (!aligned(r, type_size(r_type)) || !aligned(w, 4) || !aligned(dy, type_size(g_type)) ||
+        !aligned(dres, type_size(g_type)) || !aligned(dx, type_size(g_type)) || !aligned(dw, 4) ||
+        !aligned(workspace, 16))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: a misaligned pointer", name);
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    NormBackDesc p{};
+    p.T = T, p.D = D, p.r_type = r_type, p.g_type = g_type, p.r = r, p.w = w, p.eps = eps, p.dy = dy, p.dres = dres;
+    p.workspace = static_cast<float *>(workspace), p.dx = dx, p.dw = dw;
+    return norm_backward_launch(p, *ds, current_stream());
+}
+
+int isam_conv1d_forward(int T, int batch, int C, int width, int x_type, const void *x, int64_t x_stride,
+                        const float *w, const float *bias, int silu, const void *state, const int32_t *lengths,
+                        int y_type, void *y, void *new_state) {
+    ConvDesc p{};
+    p.T = T, p.batch = batch, p.C = C, p.width = width, p.slots = 1, p.x_type = x_type, p.y_type = y_type;
+    p.silu = silu, p.x = x, p.x_stride = x_stride, p.w = w, p.bias = bias, p.state = state, p.lengths = lengths;
+    p.y = y, p.new_state = new_state;
+    int rc = conv1d_validate("isam_conv1d_forward", p);
+    if (rc) return rc;
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    return conv1d_forward_launch(p, *ds, current_stream());
+}
+
+int isam_conv1d_step(int batch, int C, int width, int slots, int x_type, const void *x, int64_t x_stride,
+                     const float *w, const float *bias, int silu, const int32_t *slot_ids, const void *state,
+                     void *new_state, int y_type, void *y) {
+    ConvDesc p{};
+    p.T = 1, p.batch = batch, p.C = C, p.width = width, p.slots = slots, p.x_type = x_type, p.y_type = y_type;
+    p.silu = silu, p.x = x, p.x_stride = x_stride, p.w = w, p.bias = bias, p.state = state, p.slot_ids = slot_ids;
+    p.y = y, p.new_state = new_state;
+    int rc = conv1d_validate("isam_conv1d_step", p);
+    if (!rc) rc = cache_validate("isam_conv1d_step", batch, slots, slot_ids, state, new_state);
+    if (rc) return rc;
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    return conv1d_step_launch(p, current_stream());
+}
+
+int isam_ssm_forward(int T, int batch, int C, int N, int u_type, const void *u, int p_type, const void *dt,
+                     const float *dt_bias, const float *A, const void *B, const void *Cm, int64_t bc_stride,
+                     const float *D, const void *z, int64_t z_stride, const float *h0, const int32_t *lengths,
+                     void *y, float *h_last) {
+    SsmDesc p{};
+    p.T = T, p.batch = batch, p.C = C, p.N = N, p.slots = 1, p.u_type = u_type, p.p_type = p_type, p.u = u, p.dt = dt;
+    p.dt_bias = dt_bias, p.A = A, p.B = B, p.Cm = Cm, p.bc_stride = bc_stride, p.D = D, p.z = z;
+    p.z_stride = z_stride, p.lengths = lengths, p.state = h0, p.new_state = h_last, p.y = y;
+    int rc = ssm_validate("isam_ssm_forward", p);
+    if (rc) return rc;
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    return ssm_forward_launch(p, *ds, current_stream());
+}
+
+int isam_ssm_step(int batch, int C, int N, int slots, int u_type, const void *u, int p_type, const void *dt,
+                  const float *dt_bias, const float *A, const void *B, const void *Cm, int64_t bc_stride,
+                  const float *D, const void *z, int64_t z_stride, const int32_t *slot_ids, const float *state,
+                  float *new_state, void *y) {
+    SsmDesc p{};
+    p.T = 1, p.batch = batch, p.C = C, p.N = N, p.slots = slots, p.u_type = u_type, p.p_type = p_type, p.u = u;
+    p.dt = dt, p.dt_bias = dt_bias, p.A = A, p.B = B, p.Cm = Cm, p.bc_stride = bc_stride, p.D = D, p.z = z;
+    p.z_stride = z_stride, p.slot_ids = slot_ids, p.state = state, p.new_state = new_state, p.y = y;
+    int rc = ssm_validate("isam_ssm_step", p);
+    if (!rc) rc = cache_validate("isam_ssm_step", batch, slots, slot_ids, state, new_state);
+    if (rc) return rc;
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    return ssm_step_launch(p, current_stream());
+}
+
+int isam_beam_select_workspace(int batch, int beams, int V, int count, size_t *bytes) {
+    int rc = beam_validate("isam_beam_select_workspace", batch, beams, V, count);
+    if (rc) return rc;
+    if (!bytes) return set_error(ISAM_ERR_INVALID_ARG, "isam_beam_select_workspace: null pointer");
+    *bytes = beam_select_workspace(batch, beams, V, count);
+    return ISAM_OK;
+}
+
+int isam_beam_select(int batch, int beams, int V, int count, int l_type, const void *logits, const float *scores,
+                     int eos, const uint8_t *finished, void *workspace, float *new_scores, int32_t *parents,
+                     int32_t *tokens, uint8_t *new_finished) {
+    const char *name = "isam_beam_select";
+    int rc = beam_validate(name, batch, beams, V, count);
+    if (rc) return rc;
+    if (!type_ok(l_type)) return set_error(ISAM_ERR_INVALID_ARG, "%s: l_type must be ISAM_F32 or ISAM_BF16", name);
+    if (!logits || !scores || !workspace || !new_scores || !parents || !tokens)
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
+    if (eos < -1 || eos >= V) return set_error(ISAM_ERR_INVALID_ARG, "%s: eos (%d) outside [-1, V)", name, eos);
+    if (finished && eos < 0) return set_error(ISAM_ERR_INVALID_ARG, "%s: finished beams need eos", name);
+    if (!aligned(logits, type_size(l_type)) || !aligned(scores, 4) || !aligned(workspace, 16) ||
+        !aligned(new_scores, 4) || !aligned(parents, 4) || !aligned(tokens, 4))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: a misaligned pointer", name);
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    BeamDesc p{};
+    p.batch = batch, p.beams = beams, p.V = V, p.count = count, p.l_type = l_type, p.eos = eos, p.logits = logits;
+    p.scores = scores, p.finished = finished, p.workspace = workspace, p.new_scores = new_scores;
+    p.parents = parents, p.tokens = tokens, p.new_finished = new_finished;
+    return beam_select_launch(p, current_stream());
+}
+
+int isam_beam_reorder(int layers, int batch, int beams, int slots, size_t row_bytes, const int32_t *parents,
+                      const int32_t *slot_ids, const void *state, void *new_state) {
+    const char *name = "isam_beam_reorder";
+    if (layers < 1 || batch < 1 || beams < 1 || slots < 1 || row_bytes < 1)
+        return set_error(ISAM_ERR_INVALID_ARG, "%s: sizes must be >= 1", name);
+    if (!parents) return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
+    if (beams > 64 || static_cast<int64_t>(batch) * beams > (1 << 20) ||
+        static_cast<int64_t>(layers) * slots > 0x7fffffffLL || row_bytes > 0x7fffffffu)
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: beams above 64 or sizes beyond the limits", name);
+    int rc = cache_validate(name, batch * beams, slots, slot_ids, state, new_state);
+    if (rc) return rc;
+    if (!aligned(parents, 4) || !aligned(slot_ids, 4))
+        return set_error(ISAM_ERR_UNSUPPORTED, "%s: a misaligned pointer", name);
+    DeviceState *ds = device_state(&rc);
+    if (!ds) return rc;
+    return beam_reorder_launch(layers, batch, beams, slots, row_bytes, parents, slot_ids, state, new_state,
+                               current_stream());
+}
+
 }  // extern "C"

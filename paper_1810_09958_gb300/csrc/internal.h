@@ -201,4 +201,89 @@ int w4_pack_launch(int N, int K, int group, const uint8_t *codes, const uint16_t
 int gemv_w4_launch(int M, int N, int K, int group, const uint16_t *x, const uint8_t *tiled, const uint16_t *scales,
                    float *y, DeviceState &ds, cudaStream_t s);
 
+// Root-mean-square norm (y_type -1: y8 and y8_scales).
+struct NormDesc {
+    int T, D;
+    int x_type, r_type, y_type;
+    const void *x;
+    const void *res;
+    void *res_out;
+    const float *w;
+    float eps;
+    void *y;
+    uint8_t *y8;
+    uint8_t *y8_scales;
+};
+int norm_forward_launch(const NormDesc &p, DeviceState &ds, cudaStream_t s);
+struct NormBackDesc {
+    int T, D;
+    int r_type, g_type;
+    const void *r;
+    const float *w;
+    float eps;
+    const void *dy;
+    const void *dres;
+    float *workspace;
+    void *dx;
+    float *dw;
+};
+size_t norm_backward_workspace(int T, int D);
+int norm_backward_launch(const NormBackDesc &p, DeviceState &ds, cudaStream_t s);
+
+// Causal convolution (forward: lengths; one token: slots and slot_ids).
+struct ConvDesc {
+    int T, batch, C, width, slots;
+    int x_type, y_type, silu;
+    const void *x;
+    int64_t x_stride;
+    const float *w;
+    const float *bias;
+    const void *state;
+    const int32_t *lengths;
+    const int32_t *slot_ids;
+    void *y;
+    void *new_state;
+};
+int conv1d_forward_launch(const ConvDesc &p, DeviceState &ds, cudaStream_t s);
+int conv1d_step_launch(const ConvDesc &p, cudaStream_t s);
+
+// Selective scan (forward: state is h0, new_state h_last; one token: slots and slot_ids).
+struct SsmDesc {
+    int T, batch, C, N, slots;
+    int u_type, p_type;
+    const void *u;
+    const void *dt;
+    const float *dt_bias;
+    const float *A;
+    const void *B;
+    const void *Cm;
+    int64_t bc_stride;
+    const float *D;
+    const void *z;
+    int64_t z_stride;
+    const int32_t *lengths;
+    const int32_t *slot_ids;
+    const float *state;
+    float *new_state;
+    void *y;
+};
+int ssm_forward_launch(const SsmDesc &p, DeviceState &ds, cudaStream_t s);
+int ssm_step_launch(const SsmDesc &p, cudaStream_t s);
+
+struct BeamDesc {
+    int batch, beams, V, count, l_type, eos;
+    const void *logits;
+    const float *scores;
+    const uint8_t *finished;
+    void *workspace;
+    float *new_scores;
+    int32_t *parents;
+    int32_t *tokens;
+    uint8_t *new_finished;
+};
+size_t beam_select_workspace(int batch, int beams, int V, int count);
+int beam_select_launch(const BeamDesc &p, cudaStream_t s);
+int beam_reorder_launch(int layers, int batch, int beams, int slots, size_t row_bytes, const int32_t *parents,
+                        const int32_t *slot_ids, const void *state, void *new_state, cudaStream_t s);
+
 }  // namespace isam

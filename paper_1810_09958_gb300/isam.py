@@ -80,6 +80,17 @@ def load():
         lib.isam_glu_backward.argtypes = [i, i, i, i, P, P, P, P, P, P]
         lib.isam_w4_pack.argtypes = [i, i, i, P, P, P, P]
         lib.isam_gemv_w4.argtypes = [i, i, i, i, P, P, P, P]
+        z, q = ctypes.c_size_t, ctypes.c_int64
+        lib.isam_rms_norm_forward.argtypes = [i, i, i, P, i, P, P, P, f, i, P, P, P]
+        lib.isam_rms_norm_backward_workspace.argtypes = [i, i, P]
+        lib.isam_rms_norm_backward.argtypes = [i, i, i, P, P, f, i, P, P, P, P, P]
+        lib.isam_conv1d_forward.argtypes = [i, i, i, i, i, P, q, P, P, i, P, P, i, P, P]
+        lib.isam_conv1d_step.argtypes = [i, i, i, i, i, P, q, P, P, i, P, P, P, i, P]
+        lib.isam_ssm_forward.argtypes = [i, i, i, i, i, P, i, P, P, P, P, P, q, P, P, q, P, P, P, P]
+        lib.isam_ssm_step.argtypes = [i, i, i, i, i, P, i, P, P, P, P, P, q, P, P, q, P, P, P, P]
+        lib.isam_beam_select_workspace.argtypes = [i, i, i, i, P]
+        lib.isam_beam_select.argtypes = [i, i, i, i, i, P, P, i, P, P, P, P, P, P]
+        lib.isam_beam_reorder.argtypes = [i, i, i, i, z, P, P, P, P]
         for name in ("isam_version", "isam_set_stream", "isam_sync", "isam_shutdown", "isam_gemm",
                      "isam_gemm_plan_info", "isam_gemm_plan_info2", "isam_gemm_grouped", "isam_gemm_fp8", "isam_gemm_grouped_fp8",
                      "isam_gemm_mxfp8", "isam_gemm_grouped_mxfp8",
@@ -89,7 +100,9 @@ def load():
                      "isam_gru_plan_info", "isam_gru_plan_for", "isam_gemm_plan_for",
                      "isam_glr_forward", "isam_glr_backward", "isam_glr_step",
                      "isam_glu_forward", "isam_glu_backward_workspace", "isam_glu_backward",
-                     "isam_w4_pack", "isam_gemv_w4"):
+                     "isam_w4_pack", "isam_gemv_w4", "isam_rms_norm_forward", "isam_rms_norm_backward_workspace",
+                     "isam_rms_norm_backward", "isam_conv1d_forward", "isam_conv1d_step", "isam_ssm_forward",
+                     "isam_ssm_step", "isam_beam_select_workspace", "isam_beam_select", "isam_beam_reorder"):
             getattr(lib, name).restype = ctypes.c_int
         _lib = lib
         return lib
@@ -417,6 +430,33 @@ class _Call:
     def opt(self, t, dtype, numel, name):
         return None if t is None else self.ptr(t, dtype, numel, name)
 
+    def rows(self, t, dtype, count, width, name):
+        """The address of `count` rows of `width` elements and the distance between
+        them: a contiguous tensor, or the columns of one ([..., a:b])."""
+        if t.is_contiguous():
+            return self.ptr(t, dtype, count * width, name), width
+        shape, strides = t.shape, t.stride()
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor")
+        if t.dtype is not dtype:
+            raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} is not on the current device")
+        if t.numel() != count * width or shape[-1] != width:
+            raise ValueError(f"{name} has shape {tuple(shape)}, expected {count} rows of {width}")
+        step = over = 0
+        for n, s in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+            if n == 1:
+                continue
+            if not step:
+                step = over = s
+            elif s != over:
+                step = -1
+            over = s * n
+        if step < width and count > 1 or (width > 1 and strides[-1] != 1):
+            raise ValueError(f"{name} must be rows of {width} neighbouring elements, a fixed distance apart")
+        return t.data_ptr(), step if count > 1 else width
+
     def kind(self, t, name):
         """ISAM_F32 or ISAM_BF16 of a tensor."""
         code = _kinds.get(t.dtype)
@@ -590,3 +630,165 @@ def gemv_w4(M, N, K, group, x, tiled, tiled_scales, y) -> None:
           c.ptr(tiled, c.torch.uint8, w4_tiled_bytes(N, K), "tiled"),
           c.ptr(tiled_scales, bf16, w4_tiled_scales(N, K, group), "tiled_scales"),
           c.ptr(y, c.torch.float32, M * N, "y"))
+
+
+def rms_norm_forward(T, D, x, res, res_out, w, eps, y, y8=None, y8_scales=None) -> None:
+    """isam_rms_norm_forward: r = x + res, y = r / sqrt(mean(r^2) + eps) * w over
+    rows of D (x, res, res_out [T,D] fp32 or bf16, res and res_out of one type, either
+    may be None, res_out may be res; w [D] fp32), into y [T,D] fp32 or bf16, or
+    with y None into y8 [T,D] E4M3 bytes and y8_scales [ceil(D/128),T,4] E8M0 bytes (uint8)
+    for gemm_mxfp8."""
+    c = _Call()
+    u8, n = c.torch.uint8, T * D
+    kept = res if res is not None else res_out
+    r_type = x.dtype if kept is None else kept.dtype
+    rt = c.kind(x, "x") if kept is None else c.kind(kept, "res")
+    if y8 is not None and y8.dtype is not u8:
+        _e4m3_dev(y8, n, "y8")
+        y8 = y8.view(u8)
+    c.run(c.lib.isam_rms_norm_forward, T, D, c.kind(x, "x"), c.ptr(x, x.dtype, n, "x"), rt, c.opt(res, r_type, n, "res"),
+          c.opt(res_out, r_type, n, "res_out"), c.ptr(w, c.torch.float32, D, "w"), float(eps),
+          0 if y is None else c.kind(y, "y"), None if y is None else c.ptr(y, y.dtype, n, "y"), c.opt(y8, u8, n, "y8"),
+          c.opt(y8_scales, u8, mx_scale_bytes(T, D), "y8_scales"))
+
+
+def rms_norm_backward_workspace(T, D) -> int:
+    """isam_rms_norm_backward_workspace: bytes of rms_norm_backward's workspace."""
+    out = ctypes.c_size_t()
+    check(load().isam_rms_norm_backward_workspace(T, D, ctypes.byref(out)))
+    return out.value
+
+
+def rms_norm_backward(T, D, r, w, eps, dy, dres, dx, dw, workspace=None) -> None:
+    """isam_rms_norm_backward: dx [T,D] (dy's type; the gradient of x and res alike)
+    and dw [D] fp32 (either may be None) from r = rms_norm_forward's res_out (or x),
+    dy [T,D] fp32 or bf16, and dres [T,D] (dy's type) or None, which is added to dx;
+    workspace a uint8 tensor of rms_norm_backward_workspace bytes, or None to
+    take one from torch's allocator on the current stream."""
+    c = _Call()
+    f32, n = c.torch.float32, T * D
+    head = (T, D, c.kind(r, "r"), c.ptr(r, r.dtype, n, "r"), c.ptr(w, f32, D, "w"), float(eps), c.kind(dy, "dy"),
+            c.ptr(dy, dy.dtype, n, "dy"), c.opt(dres, dy.dtype, n, "dres"))
+    tail = (c.opt(dx, dy.dtype, n, "dx"), c.opt(dw, f32, D, "dw"))
+    _run_with(c, c.lib.isam_rms_norm_backward, head, tail, workspace,
+              0 if dw is None else rms_norm_backward_workspace(T, D))
+
+
+def _run_with(c, fn, head, tail, workspace, need):
+    """fn(*head, workspace, *tail) with `need` bytes of the caller's or of torch's allocator."""
+    if workspace is not None:
+        ws = c.ptr(workspace, c.torch.uint8, workspace.numel(), "workspace")
+        if workspace.numel() < need:
+            raise ValueError(f"workspace has {workspace.numel()} bytes, {need} are needed")
+        c.run(fn, *head, ws, *tail)
+    elif need:
+        _with_workspace(c.device, need, lambda ws: c.run(fn, *head, ws, *tail))
+    else:
+        c.run(fn, *head, None, *tail)
+
+
+def conv1d_forward(T, batch, C, width, x, w, bias, silu, state, lengths, y, new_state=None) -> None:
+    """isam_conv1d_forward: y_t = act(bias + sum_j w[j] x_{t-width+1+j}), act SiLU
+    where silu (x [T,batch,C] fp32 or bf16, contiguous or columns of wider rows;
+    w [width,C], bias [C] or None fp32; state, new_state [batch,width-1,C] of x's type, or
+    None; lengths [batch] int32 or None; y [T,batch,C] fp32 or bf16)."""
+    c = _Call()
+    f32, edge = c.torch.float32, batch * (width - 1) * C
+    at, stride = c.rows(x, x.dtype, T * batch, C, "x")
+    c.run(c.lib.isam_conv1d_forward, T, batch, C, width, c.kind(x, "x"), at, stride, c.ptr(w, f32, width * C, "w"),
+          c.opt(bias, f32, C, "bias"), 1 if silu else 0, c.opt(state, x.dtype, edge, "state"),
+          c.opt(lengths, c.torch.int32, batch, "lengths"), c.kind(y, "y"), c.ptr(y, y.dtype, T * batch * C, "y"),
+          c.opt(new_state, x.dtype, edge, "new_state"))
+
+
+def conv1d_step(batch, C, width, slots, x, w, bias, silu, slot_ids, state, new_state, y) -> None:
+    """isam_conv1d_step: one token of conv1d_forward for `batch` sequences whose
+    last inputs are entries slot_ids (int32, or None for entry b) of state
+    [slots,width-1,C] (x's type); new_state may be state; x, y [batch,C]."""
+    c = _Call()
+    f32, edge = c.torch.float32, slots * (width - 1) * C
+    at, stride = c.rows(x, x.dtype, batch, C, "x")
+    c.run(c.lib.isam_conv1d_step, batch, C, width, slots, c.kind(x, "x"), at, stride, c.ptr(w, f32, width * C, "w"),
+          c.opt(bias, f32, C, "bias"), 1 if silu else 0, c.opt(slot_ids, c.torch.int32, batch, "slot_ids"),
+          c.ptr(state, x.dtype, edge, "state"), c.ptr(new_state, x.dtype, edge, "new_state"), c.kind(y, "y"),
+          c.ptr(y, y.dtype, batch * C, "y"))
+
+
+def _ssm_operands(c, rows, C, N, u, dt, dt_bias, A, B, Cm, D, z):
+    """What the scan's two entries take alike, from u to z_stride."""
+    f32 = c.torch.float32
+    b_at, b_stride = c.rows(B, dt.dtype, rows, N, "B")
+    c_at, c_stride = c.rows(Cm, dt.dtype, rows, N, "Cm")
+    if b_stride != c_stride:
+        raise ValueError(f"the rows of B and Cm must be equally far apart, got {b_stride} and {c_stride}")
+    z_at, z_stride = (None, C) if z is None else c.rows(z, dt.dtype, rows, C, "z")
+    return (c.kind(u, "u"), c.ptr(u, u.dtype, rows * C, "u"), c.kind(dt, "dt"), c.ptr(dt, dt.dtype, rows * C, "dt"),
+            c.opt(dt_bias, f32, C, "dt_bias"), c.ptr(A, f32, C * N, "A"), b_at, c_at, b_stride, c.opt(D, f32, C, "D"),
+            z_at, z_stride)
+
+
+def ssm_forward(T, batch, C, N, u, dt, dt_bias, A, B, Cm, D, z, h0, lengths, y, h_last=None) -> None:
+    """isam_ssm_forward: h_t = exp(delta A) h_{t-1} + delta B_t u_t with delta =
+    softplus(dt + dt_bias), y_t = (C_t h_t + D u_t) silu(z_t) (u, y [T,batch,C] fp32
+    or bf16; dt [T,batch,C], B, Cm [T,batch,N], z [T,batch,C] or None of one type, fp32 or
+    bf16, B, Cm and z contiguous or columns of wider rows; dt_bias, D [C] or None,
+    A [C,N], h0, h_last [batch,C,N] or None, all fp32; lengths [batch] int32 or None)."""
+    c = _Call()
+    f32, edge = c.torch.float32, batch * C * N
+    c.run(c.lib.isam_ssm_forward, T, batch, C, N, *_ssm_operands(c, T * batch, C, N, u, dt, dt_bias, A, B, Cm, D, z),
+          c.opt(h0, f32, edge, "h0"), c.opt(lengths, c.torch.int32, batch, "lengths"),
+          c.ptr(y, u.dtype, T * batch * C, "y"), c.opt(h_last, f32, edge, "h_last"))
+
+
+def ssm_step(batch, C, N, slots, u, dt, dt_bias, A, B, Cm, D, z, slot_ids, state, new_state, y) -> None:
+    """isam_ssm_step: one token of ssm_forward for `batch` sequences whose fp32
+    states are entries slot_ids (int32, or None for entry b) of state [slots,C,N];
+    new_state may be state; the operands are rows of one step."""
+    c = _Call()
+    f32, edge = c.torch.float32, slots * C * N
+    c.run(c.lib.isam_ssm_step, batch, C, N, slots, *_ssm_operands(c, batch, C, N, u, dt, dt_bias, A, B, Cm, D, z),
+          c.opt(slot_ids, c.torch.int32, batch, "slot_ids"), c.ptr(state, f32, edge, "state"),
+          c.ptr(new_state, f32, edge, "new_state"), c.ptr(y, u.dtype, batch * C, "y"))
+
+
+def beam_select_workspace(batch, beams, V, count) -> int:
+    """isam_beam_select_workspace: bytes of beam_select's workspace."""
+    out = ctypes.c_size_t()
+    check(load().isam_beam_select_workspace(batch, beams, V, count, ctypes.byref(out)))
+    return out.value
+
+
+def beam_select(batch, beams, V, count, logits, scores, eos, finished, new_scores, parents, tokens, new_finished=None,
+                workspace=None) -> None:
+    """isam_beam_select: the `count` best continuations of each sequence's beams by
+    scores + log_softmax(logits), best first (logits [batch,beams,V] fp32 or bf16;
+    scores [batch,beams] fp32; eos a token or -1; finished [batch,beams], new_finished
+    [batch,count] bool or uint8, or None; new_scores fp32, parents and tokens
+    int32 [batch,count]); workspace a uint8 tensor of beam_select_workspace bytes,
+    or None to take one from torch's allocator on the current stream."""
+    c = _Call()
+    torch, n = c.torch, batch * count
+    for t, name in ((finished, "finished"), (new_finished, "new_finished")):
+        if t is not None and t.dtype not in (torch.bool, torch.uint8):
+            raise ValueError(f"{name} must be torch.bool or torch.uint8, got {t.dtype}")
+    head = (batch, beams, V, count, c.kind(logits, "logits"), c.ptr(logits, logits.dtype, batch * beams * V, "logits"),
+            c.ptr(scores, torch.float32, batch * beams, "scores"), eos,
+            None if finished is None else c.ptr(finished, finished.dtype, batch * beams, "finished"))
+    tail = (c.ptr(new_scores, torch.float32, n, "new_scores"), c.ptr(parents, torch.int32, n, "parents"),
+            c.ptr(tokens, torch.int32, n, "tokens"),
+            None if new_finished is None else c.ptr(new_finished, new_finished.dtype, n, "new_finished"))
+    _run_with(c, c.lib.isam_beam_select, head, tail, workspace, beam_select_workspace(batch, beams, V, count))
+
+
+def beam_reorder(layers, batch, beams, slots, parents, slot_ids, state, new_state) -> None:
+    """isam_beam_reorder: in each layer of state [layers,slots,...] (any type), the
+    row of beam k of sequence b becomes its parent parents[b,k]'s; slot_ids
+    [batch,beams] int32, or None for row b * beams + k; new_state may be state."""
+    c = _Call()
+    n = state.numel()
+    if n == 0 or n % (layers * slots):
+        raise ValueError(f"state has {n} elements, which are not {layers} x {slots} rows")
+    c.run(c.lib.isam_beam_reorder, layers, batch, beams, slots, n // (layers * slots) * state.element_size(),
+          c.ptr(parents, c.torch.int32, batch * beams, "parents"),
+          c.opt(slot_ids, c.torch.int32, batch * beams, "slot_ids"), c.ptr(state, state.dtype, n, "state"),
+          c.ptr(new_state, state.dtype, n, "new_state"))
