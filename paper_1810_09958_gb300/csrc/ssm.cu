@@ -3,6 +3,9 @@
 //   h_t[c][n] = exp(delta A[c][n]) h_{t-1}[c][n] + delta B_t[n] u_t[c],
 //   y_t[c] = (sum_n C_t[n] h_t[c][n] + D[c] u_t[c]) silu(z_t[c]),
 // over a sequence, and one token on a cache of states.
+#include <algorithm>
+#include <cmath>
+
 #include "lm_common.cuh"
 
 namespace isam {
@@ -11,86 +14,436 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// log(1 + exp(x)) to a few units in its own last place: with e = exp(-|x|) it is
-// max(x, 0) + log(1 + e), and log(1 + e) = 2 atanh(e / (2 + e)), whose series in
-// s = e / (2 + e) <= 1/3 ends after eight terms (s^17 / 17 < 1e-8 of the sum).
-__device__ __forceinline__ float softplus(float x) {
-    const float e = __expf(-fabsf(x));
-    const float s = __fdividef(e, 2.0f + e);
-    const float q = s * s;
-    float p = 1.0f / 15.0f;
-    p = fmaf(p, q, 1.0f / 13.0f);
-    p = fmaf(p, q, 1.0f / 11.0f);
-    p = fmaf(p, q, 1.0f / 9.0f);
-    p = fmaf(p, q, 1.0f / 7.0f);
-    p = fmaf(p, q, 1.0f / 5.0f);
-    p = fmaf(p, q, 1.0f / 3.0f);
-    p = fmaf(p, q, 1.0f);
-    return fmaf(2.0f * s, p, fmaxf(x, 0.0f));
-}
-
-__device__ __forceinline__ float silu(float v) {
-    const Gate s = gate(v);
-    return v * s.keep;
-}
-
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
+// log(1 + exp(x)) to a few units in its own last place: with e = exp(-|x|) it is
+// max(x, 0) + log(1 + e), and log(1 + e) = 2 atanh(s) with s = e / (2 + e) <= 1/3.
+// atanh(s) / s is a polynomial of degree 4 in s^2, fitted for the least relative
+// error (least squares, reweighted; 8e-9 with these coefficients).
+__device__ __forceinline__ float softplus(float x) {
+    const float e = exp2_fast(-kLog2e * fabsf(x));
+    const float s = __fdividef(e, 2.0f + e);
+    const float q = s * s;
+    float p = 0.14089167f;
+    p = fmaf(p, q, 0.139803f);
+    p = fmaf(p, q, 0.20012455f);
+    p = fmaf(p, q, 0.33333158f);
+    p = fmaf(p, q, 1.0f);
+    return fmaf(2.0f * s, p, fmaxf(x, 0.0f));
+}
+
+// v / (1 + exp(-v)) (exp(-v) = inf gives 0).
+__device__ __forceinline__ float silu(float v) { return v * __fdividef(1.0f, 1.0f + exp2_fast(-kLog2e * v)); }
+
 constexpr int kThreads = 128;
 
-// G lanes a channel, S states a lane (n = lane's part * S + i).
-template <typename U, typename P, int S, int G>
-__global__ void __launch_bounds__(kThreads)
-    ssm_forward_kernel(int T, int batch, int C, int N, const U *u, const P *dt, const float *dt_bias, const float *A,
-                       const P *B, const P *Cm, int64_t bc_stride, const float *D, const P *z, int64_t z_stride,
-                       const float *h0, const int32_t *lengths, U *y, float *h_last) {
-    dependent_start();
-    const int b = blockIdx.y;
-    const int c0 = (blockIdx.x * kThreads + threadIdx.x) / G, part = threadIdx.x % G;
-    const bool on = c0 < C;
-    const int c = on ? c0 : C - 1;
-    const int len = lengths ? min(max(lengths[b], 0), T) : T;
-    float a[S], h[S];
+// ---------------------------------------------------------------- a sequence
+// Two fp32 values in one 64-bit register pair.
+struct Two {
+    uint64_t x;
+};
+__device__ __forceinline__ Two two(float lo, float hi) {
+    Two d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d.x) : "f"(lo), "f"(hi));
+    return d;
+}
+__device__ __forceinline__ float2 apart(Two a) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(a.x));
+    return f;
+}
+__device__ __forceinline__ Two mul(Two a, Two b) {
+    Two d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.x) : "l"(a.x), "l"(b.x));
+    return d;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c) {
+    Two d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.x) : "l"(a.x), "l"(b.x), "l"(c.x));
+    return d;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+    Two d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.x) : "l"(a.x), "l"(b.x));
+    return d;
+}
+__device__ __forceinline__ Two exp2_fast(Two a) {
+    const float2 f = apart(a);
+    return two(exp2_fast(f.x), exp2_fast(f.y));
+}
+
+struct Scan {
+    int T, batch, C, N;
+    const void *u, *dt, *B, *Cm, *z;
+    const float *dt_bias, *A, *D, *h0;
+    const int32_t *lengths;
+    int64_t bc_stride, z_stride;
+    void *y;
+    float *h_last;
+    int groups;      // of channels a sequence
+    int time_warps;  // warps of a CTA that share a group's time
+    int time_ctas;   // CTAs of a cluster that do
+    int dt_grain, u_grain, z_grain, bc_grain;  // bytes that their rows are aligned to: 16, 4 or 2
+    bool fast;       // 16 for all, and no states to fill up
+};
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void *dst, const void *src, bool on) {
+    // (src-size 0: the bytes become zeros and nothing is read)
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(on ? 16 : 0) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(on ? 4 : 0) : "memory");
+}
+
+// ROWS rows of WIDTH elements, `pitch` elements apart, to shared memory; rows from
+// `left` on and elements from `live` on become zeros.  g: bytes that rows are aligned to (16, 4 or 2).
+template <int ROWS, int WIDTH, int SPACE, typename T>
+__device__ __forceinline__ void bring(T *dst, const T *src, int64_t pitch, int left, int live, int g, int lane) {
+    const auto by = [&](auto word) {
+        constexpr int BYTES = sizeof(word), E = BYTES / sizeof(T);
+        if constexpr (E > 0 && WIDTH % (E > 0 ? E : 1) == 0) {
+            constexpr int PER = WIDTH / E, ALL = ROWS * PER;
 #pragma unroll
-    for (int i = 0; i < S; ++i) {
-        const int n = part * S + i;
-        const int64_t at = static_cast<int64_t>(c) * N + n;
-        a[i] = n < N ? A[at] * kLog2e : 0.0f;
-        h[i] = n < N && h0 ? h0[static_cast<int64_t>(b) * C * N + at] : 0.0f;
-    }
-    const float bias = dt_bias ? dt_bias[c] : 0.0f, skip = D ? D[c] : 0.0f;
-    for (int t = 0; t < len; ++t) {
-        const int64_t row = static_cast<int64_t>(t) * batch + b;
-        const float uv = to_f32(u[row * C + c]);
-        const float delta = softplus(to_f32(dt[row * C + c]) + bias);
-        const float in = delta * uv;
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const int n = part * S + i;
-            if (n < N) {
-                h[i] = fmaf(exp2_fast(delta * a[i]), h[i], in * to_f32(B[row * bc_stride + n]));
-                sum = fmaf(to_f32(Cm[row * bc_stride + n]), h[i], sum);
+            for (int i = 0; i < (ALL + 31) / 32; ++i) {
+                const int f = lane + 32 * i, t = f / PER, e = f % PER * E;
+                if (ALL % 32 != 0 && f >= ALL) continue;
+                const bool on = t < left && e < live;
+                const T *from = on ? src + t * pitch + e : src;
+                if constexpr (BYTES >= 4) copy_async<BYTES>(dst + t * SPACE + e, from, on);
+                else dst[t * SPACE + e] = on ? *from : from_f32<T>(0.0f);
             }
         }
-#pragma unroll
-        for (int d = 1; d < G; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
-        sum = fmaf(skip, uv, sum);
-        if (z) sum *= silu(to_f32(z[row * z_stride + c]));
-        if (on && part == 0) y[row * C + c] = from_f32<U>(sum);
-    }
-    if (on && part == 0)
-        for (int t = len; t < T; ++t) y[(static_cast<int64_t>(t) * batch + b) * C + c] = from_f32<U>(0.0f);
-    if (h_last && on)
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const int n = part * S + i;
-            if (n < N) h_last[(static_cast<int64_t>(b) * C + c) * N + n] = h[i];
+    };
+    constexpr bool wide = WIDTH * sizeof(T) % 16 == 0;
+    if (wide && g == 16) by(uint4());
+    else if (g >= 4 || sizeof(T) == 4) by(uint32_t());
+    else by(uint16_t());
+}
+
+// The same where rows are on 16-byte boundaries and a block is whole: the lane's
+// place in it does not change, so `at` (of the lane's first piece) only moves on.
+template <int ROWS, int WIDTH, int SPACE, typename T>
+struct Lane16 {
+    static constexpr int E = 16 / sizeof(T), PER = WIDTH / E, ALL = ROWS * PER;
+    static constexpr bool ok = WIDTH * sizeof(T) % 16 == 0 && (PER > 0 && 32 % (PER > 0 ? PER : 1) == 0);
+    const char *at;
+    __device__ __forceinline__ void start(const T *src, int64_t pitch, int live, int lane) {
+        if constexpr (ok) {
+            const int e = lane % PER * E;
+            at = reinterpret_cast<const char *>(src + lane / PER * pitch + (e < live ? e : 0));
         }
+    }
+    // (lanes past `live` elements bring others, which no one uses)
+    __device__ __forceinline__ void bring(T *dst, int64_t pitch_bytes, int lane) {
+        if constexpr (ok) {
+            T *to = dst + lane / PER * SPACE + lane % PER * E;
+#pragma unroll
+            for (int i = 0; i < (ALL + 31) / 32; ++i)
+                if (ALL % 32 == 0 || lane + 32 * i < ALL)
+                    copy_async<16>(to + i * (32 / PER) * SPACE, at + i * (32 / PER) * pitch_bytes, true);
+            at += ROWS * pitch_bytes;
+        }
+    }
+};
+
+// A warp has 32 / G channels, S states of one in each lane: lane = part * (32 / G) + channel.
+// Its operands come by asynchronous copies into a ring of blocks of TB steps.
+template <typename U, typename P, int S, int G>
+struct Walk {
+    static constexpr int CH = 32 / G, NP = S * G;
+    static constexpr int TB = 8;                   // steps a block
+    static constexpr int PAIRS = TB / G;           // steps of a block whose gates a lane forms
+    static constexpr int kStages = 4;
+    static constexpr bool kWiden = sizeof(P) == 2;  // B and C are widened once a block
+    // Bytes of a stage: dt, z, u, and B and C; behind the stages B and C in fp32, and (delta, delta u).
+    static constexpr int kDt = TB * CH * sizeof(P), kU = TB * CH * sizeof(U), kBc = TB * 2 * NP * sizeof(P);
+    static constexpr int up16(int n) { return (n + 15) / 16 * 16; }
+    static constexpr int kStage = up16(kDt) * 2 + up16(kU) + up16(kBc);
+    static constexpr int kWide = kWiden ? TB * 2 * NP * 4 : 0;
+    static constexpr int kGates = G > 1 ? TB * CH * 8 : 0;
+    static constexpr int kBytes = kStages * kStage + kWide + kGates;
+
+    using DtLane = Lane16<TB, CH, CH, P>;
+    using ULane = Lane16<TB, CH, CH, U>;
+    using BcLane = Lane16<TB, NP, 2 * NP, P>;
+    static constexpr bool kFast = DtLane::ok && ULane::ok && BcLane::ok;
+
+    const Scan &p;
+    const int b, lane, part, first;  // first: the warp's first channel
+    char *smem;
+    float bias, skip;
+    Two a[S / 2], h[S / 2];
+    DtLane ldt, lz;
+    ULane lu;
+    BcLane lb, lc;
+
+    __device__ __forceinline__ P *dt_of(int st) const { return reinterpret_cast<P *>(smem + st * kStage); }
+    __device__ __forceinline__ P *z_of(int st) const { return reinterpret_cast<P *>(smem + st * kStage + up16(kDt)); }
+    __device__ __forceinline__ U *u_of(int st) const { return reinterpret_cast<U *>(smem + st * kStage + 2 * up16(kDt)); }
+    __device__ __forceinline__ P *bc_of(int st) const {
+        return reinterpret_cast<P *>(smem + st * kStage + 2 * up16(kDt) + up16(kU));
+    }
+
+    template <bool FOLD>
+    __device__ __forceinline__ void bring_block(int64_t t, int64_t t1, int st) {
+        const int64_t across = static_cast<int64_t>(p.batch) * p.C;
+        if (kFast && p.fast && t + TB <= t1) {
+            ldt.bring(dt_of(st), across * sizeof(P), lane);
+            lu.bring(u_of(st), across * sizeof(U), lane);
+            if (!FOLD && p.z) lz.bring(z_of(st), p.batch * p.z_stride * sizeof(P), lane);
+            lb.bring(bc_of(st), p.batch * p.bc_stride * sizeof(P), lane);
+            if (!FOLD) lc.bring(bc_of(st) + NP, p.batch * p.bc_stride * sizeof(P), lane);
+        } else if (t < t1) {
+            const int left = static_cast<int>(min(t1 - t, static_cast<int64_t>(TB))), live = p.C - first;
+            const int64_t r = t * p.batch + b;
+            bring<TB, CH, CH>(dt_of(st), static_cast<const P *>(p.dt) + r * p.C + first, across, left, live, p.dt_grain, lane);
+            bring<TB, CH, CH>(u_of(st), static_cast<const U *>(p.u) + r * p.C + first, across, left, live, p.u_grain, lane);
+            if (!FOLD && p.z)
+                bring<TB, CH, CH>(z_of(st), static_cast<const P *>(p.z) + r * p.z_stride + first, p.batch * p.z_stride, left,
+                                  live, p.z_grain, lane);
+            bring<TB, NP, 2 * NP>(bc_of(st), static_cast<const P *>(p.B) + r * p.bc_stride, p.batch * p.bc_stride, left, p.N,
+                                  p.bc_grain, lane);
+            if (!FOLD)
+                bring<TB, NP, 2 * NP>(bc_of(st) + NP, static_cast<const P *>(p.Cm) + r * p.bc_stride,
+                                      p.batch * p.bc_stride, left, p.N, p.bc_grain, lane);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+
+    // A step's decays.
+    __device__ __forceinline__ void decays(float delta, Two (&e)[S / 2]) const {
+        const Two dd = two(delta, delta);
+#pragma unroll
+        for (int k = 0; k < S / 2; ++k) e[k] = exp2_fast(mul(a[k], dd));
+    }
+
+    // One step of the states; FOLD: without the sum over them.
+    template <bool FOLD>
+    __device__ __forceinline__ float step(const Two (&e)[S / 2], float in, const float *at) {
+        const Two ii = two(in, in);
+        Two sum[2];
+#pragma unroll
+        for (int k = 0; k < S / 2; k += 2) {
+            const ulonglong2 B = *reinterpret_cast<const ulonglong2 *>(at + 2 * k);
+            h[k] = fma(e[k], h[k], mul(ii, Two{B.x}));
+            h[k + 1] = fma(e[k + 1], h[k + 1], mul(ii, Two{B.y}));
+            if (!FOLD) {
+                const ulonglong2 Cv = *reinterpret_cast<const ulonglong2 *>(at + NP + 2 * k);
+                sum[0] = k ? fma(Two{Cv.x}, h[k], sum[0]) : mul(Two{Cv.x}, h[k]);
+                sum[1] = k ? fma(Two{Cv.y}, h[k + 1], sum[1]) : mul(Two{Cv.y}, h[k + 1]);
+            }
+        }
+        if (FOLD) return 0.0f;
+        const float2 x = apart(add2(sum[0], sum[1]));
+        return x.x + x.y;
+    }
+
+    // The steps of one block: gates, states, outputs.
+    template <bool FOLD, bool FULL>
+    __device__ __forceinline__ float block(int st, const float *bc, float2 *gates, int left, U *py, int64_t py_step) {
+        const int mine = lane % CH;
+        const P *dt = dt_of(st) + mine, *z = z_of(st) + mine;
+        const U *u = u_of(st) + mine;
+        float delta[PAIRS], in[PAIRS], uv[PAIRS], total = 0.0f;
+#pragma unroll
+        for (int j = 0; j < PAIRS; ++j) {
+            const int i = j * G + part;
+            uv[j] = to_f32(u[i * CH]);
+            delta[j] = softplus(to_f32(dt[i * CH]) + bias);
+            if (!FULL && i >= left) delta[j] = 0.0f;  // (a step past the end keeps the state)
+            in[j] = delta[j] * uv[j];
+            total += delta[j];
+            if (G > 1) gates[i * CH + mine] = make_float2(delta[j], in[j]);
+        }
+        if (G > 1 || kWiden) __syncwarp();
+        float sums[PAIRS];
+        const auto gate_of = [&](int i) {  // (delta, delta u) of step i
+            return G > 1 ? gates[i * CH + mine] : make_float2(delta[i / G], in[i / G]);
+        };
+        // The next step's decays are formed beside a step's products.
+        float2 g = gate_of(0);
+        Two e[2][S / 2];
+        decays(g.x, e[0]);
+#pragma unroll
+        for (int j = 0; j < PAIRS; ++j) {
+            float v[G];
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const int at = j * G + i;
+                const float now = g.y;
+                if (at + 1 < TB) {
+                    g = gate_of(at + 1);
+                    decays(g.x, e[(at + 1) & 1]);
+                }
+                v[i] = step<FOLD>(e[at & 1], now, bc + at * 2 * NP);
+            }
+            // Sums over the parts: each lane ends with that of the step it formed the gates of.
+            if (!FOLD)
+#pragma unroll
+                for (int d = G / 2; d > 0; d >>= 1) {
+                    const bool up = part & d;
+#pragma unroll
+                    for (int i = 0; i < d; ++i) {
+                        const float send = up ? v[i] : v[i + d], keep = up ? v[i + d] : v[i];
+                        v[i] = keep + __shfl_xor_sync(~0u, send, d * CH);
+                    }
+                }
+            sums[j] = v[0];
+        }
+        if (!FOLD) {
+            const bool c_on = first + mine < p.C;
+#pragma unroll
+            for (int j = 0; j < PAIRS; ++j) {
+                const int i = j * G + part;
+                sums[j] = fmaf(skip, uv[j], sums[j]);
+                if (p.z) sums[j] *= silu(to_f32(z[i * CH]));
+            }
+#pragma unroll
+            for (int j = 0; j < PAIRS; ++j)
+                if (c_on && (FULL || j * G + part < left)) py[j * py_step] = from_f32<U>(sums[j]);
+        }
+        return total;
+    }
+
+    // Steps t0 to t1.  FOLD: states alone; returns the lane's sum of delta.
+    template <bool FOLD>
+    __device__ __forceinline__ float run(int64_t t0, int64_t t1) {
+        float total = 0.0f;
+        if (t0 >= t1) return total;
+        float *wide = reinterpret_cast<float *>(smem + kStages * kStage);
+        float2 *gates = reinterpret_cast<float2 *>(smem + kStages * kStage + kWide);
+        const int64_t r = t0 * p.batch + b, across = static_cast<int64_t>(p.batch) * p.C;
+        if (kFast && p.fast) {
+            ldt.start(static_cast<const P *>(p.dt) + r * p.C + first, across, p.C - first, lane);
+            lu.start(static_cast<const U *>(p.u) + r * p.C + first, across, p.C - first, lane);
+            if (!FOLD && p.z) lz.start(static_cast<const P *>(p.z) + r * p.z_stride + first, p.batch * p.z_stride, p.C - first, lane);
+            lb.start(static_cast<const P *>(p.B) + r * p.bc_stride, p.batch * p.bc_stride, p.N, lane);
+            if (!FOLD) lc.start(static_cast<const P *>(p.Cm) + r * p.bc_stride, p.batch * p.bc_stride, p.N, lane);
+        }
+        U *py = static_cast<U *>(p.y) + (r + part * p.batch) * p.C + first + lane % CH;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) bring_block<FOLD>(t0 + i * TB, t1, i);
+        int st = 0;
+        for (int64_t t = t0; t < t1; t += TB) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+            __syncwarp();
+            bring_block<FOLD>(t + (kStages - 1) * TB, t1, st == 0 ? kStages - 1 : st - 1);
+            const float *bc;
+            if constexpr (kWiden) {
+                constexpr int ALL = TB * 2 * NP / 4;
+                bc = wide;
+#pragma unroll
+                for (int i = 0; i < (ALL + 31) / 32; ++i) {
+                    const int f = lane + 32 * i;
+                    if (ALL % 32 != 0 && f >= ALL) continue;
+                    const uint2 q = reinterpret_cast<const uint2 *>(bc_of(st))[f];
+                    reinterpret_cast<float4 *>(wide)[f] =
+                        make_float4(__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xffff0000u),
+                                    __uint_as_float(q.y << 16), __uint_as_float(q.y & 0xffff0000u));
+                }
+            } else {
+                bc = reinterpret_cast<const float *>(bc_of(st));
+            }
+            bc += part * S;
+            if (t + TB <= t1) total += block<FOLD, true>(st, bc, gates, TB, py, G * across);
+            else total += block<FOLD, false>(st, bc, gates, static_cast<int>(t1 - t), py, G * across);
+            py += TB * across;
+            st = st + 1 == kStages ? 0 : st + 1;
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        return total;
+    }
+};
+
+template <typename U, typename P, int S, int G>
+__global__ void __launch_bounds__(384)
+    ssm_forward_kernel(const __grid_constant__ Scan p) {
+    using W = Walk<U, P, S, G>;
+    constexpr int CH = W::CH;
+    extern __shared__ float4 raw[];
+    griddep_wait();
+    const int warp = threadIdx.x / 32, warps = blockDim.x / 32, lane = threadIdx.x % 32;
+    const int rank = p.time_ctas > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+    const int across = warps / p.time_warps;  // groups a CTA
+    const int chunk = rank * p.time_warps + warp % p.time_warps, chunks = p.time_ctas * p.time_warps;
+    const int mine = warp / p.time_warps;
+    const int64_t group = static_cast<int64_t>(blockIdx.x / p.time_ctas) * across + mine;
+    const int b = blockIdx.y;
+    const int64_t c_wanted = group * CH + lane % CH;
+    const bool c_on = c_wanted < p.C;
+    const int c = c_on ? static_cast<int>(c_wanted) : p.C - 1;
+    W w{p, b, lane, lane / CH, static_cast<int>(group * CH)};
+    w.smem = reinterpret_cast<char *>(raw) + warp * W::kBytes;
+    w.bias = p.dt_bias ? p.dt_bias[c] : 0.0f;
+    w.skip = p.D ? p.D[c] : 0.0f;
+    const int len = group >= p.groups ? 0 : p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
+    const int64_t first = (static_cast<int64_t>(b) * p.C + c) * p.N + w.part * S;  // this lane's states
+    const auto state = [&](int i) { return w.part * S + i < p.N && p.h0 ? p.h0[first + i] : 0.0f; };
+#pragma unroll
+    for (int k = 0; k < S / 2; ++k) {
+        const auto rate = [&](int i) {
+            return w.part * S + i < p.N ? p.A[static_cast<int64_t>(c) * p.N + w.part * S + i] * kLog2e : 0.0f;
+        };
+        w.a[k] = two(rate(2 * k), rate(2 * k + 1));
+    }
+    const int64_t each = (len + static_cast<int64_t>(chunks) - 1) / chunks;
+    const int64_t per = (each + W::TB - 1) / W::TB * W::TB;
+    const int64_t t0 = min(chunk * per, static_cast<int64_t>(len)), t1 = min(t0 + per, static_cast<int64_t>(len));
+    if (chunks > 1) {
+        // Folds: a chunk's states from zero, and its sum of delta (a decay over it is one exponential).
+        char *folds = reinterpret_cast<char *>(raw) + warps * W::kBytes;  // [warp][S / 2 + 1][32] pairs
+        Two *own = reinterpret_cast<Two *>(folds) + warp * (S / 2 + 1) * 32;
+#pragma unroll
+        for (int k = 0; k < S / 2; ++k) w.h[k] = two(0.0f, 0.0f);
+        float total = chunk + 1 < chunks ? w.template run<true>(t0, t1) : 0.0f;
+#pragma unroll
+        for (int d = CH; d < 32; d <<= 1) total += __shfl_xor_sync(~0u, total, d);
+#pragma unroll
+        for (int k = 0; k < S / 2; ++k) own[k * 32 + lane] = w.h[k];
+        own[S / 2 * 32 + lane] = two(total, total);
+        if (p.time_ctas > 1) cluster_sync_all();
+        else __syncthreads();
+#pragma unroll
+        for (int k = 0; k < S / 2; ++k) w.h[k] = two(state(2 * k), state(2 * k + 1));
+        for (int j = 0; j < chunk; ++j) {
+            const int from = mine * p.time_warps + j % p.time_warps;
+            const Two *there = reinterpret_cast<const Two *>(folds) + from * (S / 2 + 1) * 32 + lane;
+            const uint32_t addr = p.time_ctas > 1 ? mapa_shared(smem_u32(there), j / p.time_warps) : smem_u32(there);
+            const auto get = [&](int k) {
+                Two v;
+                asm volatile("ld.shared::cluster.b64 %0, [%1];" : "=l"(v.x) : "r"(addr + k * 256) : "memory");
+                return v;
+            };
+            const Two sum = get(S / 2);
+#pragma unroll
+            for (int k = 0; k < S / 2; ++k) w.h[k] = fma(exp2_fast(mul(w.a[k], sum)), w.h[k], get(k));
+        }
+        // Behind this all starts are known: folds may go, and h_last may be h0.
+        if (p.time_ctas > 1) cluster_sync_all();
+        else __syncthreads();
+    } else {
+#pragma unroll
+        for (int k = 0; k < S / 2; ++k) w.h[k] = two(state(2 * k), state(2 * k + 1));
+    }
+    w.template run<false>(t0, t1);
+    // (earlier, the next kernel's CTAs would fill some SMs' free places and leave others idle)
+    griddep_launch_dependents();
+    if (!c_on) return;
+    if (p.h_last && chunk == chunks - 1)
+#pragma unroll
+        for (int k = 0; k < S / 2; ++k) {
+            const float2 v = apart(w.h[k]);
+            if (w.part * S + 2 * k < p.N) p.h_last[first + 2 * k] = v.x;
+            if (w.part * S + 2 * k + 1 < p.N) p.h_last[first + 2 * k + 1] = v.y;
+        }
+    for (int64_t t = len + chunk * G + w.part; t < p.T; t += chunks * G)
+        static_cast<U *>(p.y)[(t * p.batch + b) * p.C + c] = from_f32<U>(0.0f);
 }
 
 // One token: G lanes a channel, S words of V states a lane, neighbouring lanes on neighbouring words.
@@ -158,14 +511,37 @@ int by_type(int type, F &&f) {
 }
 
 template <typename U, typename P, int S, int G>
-int forward(const SsmDesc &p, cudaStream_t s) {
-    const unsigned across = static_cast<unsigned>((static_cast<int64_t>(p.C) * G + kThreads - 1) / kThreads);
+int forward(const SsmDesc &p, int time_warps, int time_ctas, const DeviceState &ds, cudaStream_t s) {
+    using W = Walk<U, P, S, G>;
     if (p.batch > 65535) return set_error(ISAM_ERR_UNSUPPORTED, "isam_ssm_forward: batch (%d) above 65535", p.batch);
-    return launch_dependent(ssm_forward_kernel<U, P, S, G>, dim3(across, p.batch), kThreads, 0, s, 1,
-                            "launch ssm_forward_kernel", p.T, p.batch, p.C, p.N, static_cast<const U *>(p.u),
-                            static_cast<const P *>(p.dt), p.dt_bias, p.A, static_cast<const P *>(p.B),
-                            static_cast<const P *>(p.Cm), p.bc_stride, p.D, static_cast<const P *>(p.z), p.z_stride,
-                            p.state, p.lengths, static_cast<U *>(p.y), p.new_state);
+    Scan a{};
+    a.T = p.T, a.batch = p.batch, a.C = p.C, a.N = p.N, a.u = p.u, a.dt = p.dt, a.B = p.B, a.Cm = p.Cm, a.z = p.z;
+    a.dt_bias = p.dt_bias, a.A = p.A, a.D = p.D, a.h0 = p.state, a.lengths = p.lengths, a.bc_stride = p.bc_stride;
+    a.z_stride = p.z_stride, a.y = p.y, a.h_last = p.new_state;
+    a.groups = (p.C + W::CH - 1) / W::CH;
+    a.time_warps = time_warps, a.time_ctas = time_ctas;
+    const auto grain = [](const void *at, int64_t pitch, int size) {
+        const uintptr_t odd = reinterpret_cast<uintptr_t>(at) | static_cast<uintptr_t>(pitch * size);
+        return odd % 16 == 0 ? 16 : odd % 4 == 0 ? 4 : 2;
+    };
+    // (16 bytes also means that what lies within a row's end does so in whole words)
+    a.dt_grain = grain(p.dt, p.C, sizeof(P));
+    a.u_grain = grain(p.u, p.C, sizeof(U));
+    a.z_grain = std::min(grain(p.z, p.z_stride, sizeof(P)), grain(nullptr, p.C, sizeof(P)));
+    a.bc_grain = std::min({grain(p.B, p.bc_stride, sizeof(P)), grain(p.Cm, p.bc_stride, sizeof(P)),
+                           grain(nullptr, p.N, sizeof(P))});
+    a.fast = a.dt_grain == 16 && a.u_grain == 16 && (a.z_grain == 16 || !p.z) && a.bc_grain == 16 && p.N == W::NP;
+    const int warps = time_warps > 4 ? time_warps : 4;
+    const int across = warps / time_warps;
+    const unsigned blocks = static_cast<unsigned>((a.groups + across - 1) / across) * time_ctas;
+    const size_t smem = static_cast<size_t>(warps) * (W::kBytes + (time_warps * time_ctas > 1 ? (S / 2 + 1) * 256 : 0));
+    const auto fn = ssm_forward_kernel<U, P, S, G>;
+    if (smem > 48 * 1024)
+        if (const int rc = ensure_smem_optin(reinterpret_cast<const void *>(fn), static_cast<int>(smem), ds.device,
+                                             "cudaFuncSetAttribute(ssm_forward_kernel)"))
+            return rc;
+    return launch_dependent(fn, dim3(blocks, p.batch), warps * 32, smem, s, static_cast<unsigned>(time_ctas),
+                            "launch ssm_forward_kernel", a);
 }
 
 template <typename U, typename P, int V, int S, int G>
@@ -180,18 +556,71 @@ int step(const SsmDesc &p, cudaStream_t s) {
                             p.slot_ids, p.state, p.new_state, static_cast<U *>(p.y));
 }
 
+// How a sequence is cut: states a lane, warps and CTAs that share a group's time.
+// Few channels leave SMs idle; fewer states a lane use more of them, at more
+// instructions a state, and cuts in time as well, at a second reading (the folds).
+struct Cut {
+    int S, time_warps, time_ctas;
+};
+
+// The least time by these figures (clocks a step, measured): alone on a scheduler a
+// warp takes `alone`, among others `among`, and with folds 1.75 times as much; a
+// wave of CTAs takes 1.5 us to start, more for folds and their exchange in clusters.
+Cut choose(int64_t T, int64_t batch, int64_t C, int N, const DeviceState &ds) {
+    struct Kind {
+        int S, alone, among, regs;
+    };
+    const Kind kinds[] = {{16, 300, 187, 168}, {8, 260, 98, 112}, {4, 170, 61, 108}};
+    Cut best{};
+    double least = 0.0;
+    for (const Kind &k : kinds) {
+        const int G = N <= k.S ? 1 : N <= 2 * k.S ? 2 : N <= 4 * k.S ? 4 : 8;
+        if (k.S * G < N || (k.S == 16 && N <= 8) || (k.S == 8 && N <= 4) || (k.S == 4 && N > 16)) continue;
+        const int64_t groups = (C * G + 31) / 32;
+        const int most = k.S * G > 32 ? 4 : 8;
+        for (int tw = 1; tw <= most; tw *= 2)
+            for (int tc = 1; tc <= (tw == most ? 8 : 1); tc *= 2) {
+                const int warps = tw > 4 ? tw : 4, across = warps / tw;
+                const double ctas = static_cast<double>((groups + across - 1) / across) * tc * batch;
+                const int resident = std::min(65536 / (k.regs * warps * 32), 227 * 1024 / (warps * 128 * (96 / G + 2 * k.S * G)));
+                const double room = static_cast<double>(ds.num_sms) * resident;
+                const double waves = ctas <= room ? 1.0 : 0.5 + ctas / room;
+                const double on_one = std::ceil(std::min(ctas, room) / ds.num_sms) * warps / 4;
+                const int64_t steps = ((T + tw * tc - 1) / (tw * tc) + 7) / 8 * 8;
+                double t = steps * std::max<double>(k.alone, on_one * k.among) * (tw * tc > 1 ? 1.75 : 1.0) + 3000;
+                if (tw * tc > 1) t += 1500 + 60 * tw * tc;
+                if (tc > 1) t += tc == 2 ? 2500 : tc == 4 ? 12500 : 32500;
+                t *= waves;
+                if (least == 0.0 || t < least) least = t, best = Cut{k.S, tw, tc};
+            }
+    }
+    return best;
+}
+
 }  // namespace
 
-int ssm_forward_launch(const SsmDesc &p, DeviceState &, cudaStream_t s) {
+int ssm_forward_launch(const SsmDesc &p, DeviceState &ds, cudaStream_t s) {
+    const Cut c = choose(p.T, p.batch, p.C, p.N, ds);
     return by_type(p.u_type, [&](auto u) {
         return by_type(p.p_type, [&](auto q) {
             using U = decltype(u);
             using P = decltype(q);
-            if (p.N <= 8) return forward<U, P, 8, 1>(p, s);
-            if (p.N <= 16) return forward<U, P, 16, 1>(p, s);
-            if (p.N <= 32) return forward<U, P, 16, 2>(p, s);
-            if (p.N <= 64) return forward<U, P, 16, 4>(p, s);
-            return forward<U, P, 16, 8>(p, s);
+            const int tw = c.time_warps, tc = c.time_ctas;
+            if (c.S == 4) {
+                if (p.N <= 4) return forward<U, P, 4, 1>(p, tw, tc, ds, s);
+                if (p.N <= 8) return forward<U, P, 4, 2>(p, tw, tc, ds, s);
+                return forward<U, P, 4, 4>(p, tw, tc, ds, s);
+            }
+            if (c.S == 8) {
+                if (p.N <= 8) return forward<U, P, 8, 1>(p, tw, tc, ds, s);
+                if (p.N <= 16) return forward<U, P, 8, 2>(p, tw, tc, ds, s);
+                if (p.N <= 32) return forward<U, P, 8, 4>(p, tw, tc, ds, s);
+                return forward<U, P, 8, 8>(p, tw, tc, ds, s);
+            }
+            if (p.N <= 16) return forward<U, P, 16, 1>(p, tw, tc, ds, s);
+            if (p.N <= 32) return forward<U, P, 16, 2>(p, tw, tc, ds, s);
+            if (p.N <= 64) return forward<U, P, 16, 4>(p, tw, tc, ds, s);
+            return forward<U, P, 16, 8>(p, tw, tc, ds, s);
         });
     });
 }
