@@ -952,7 +952,7 @@ int isam_beam_select(int batch, int beams, int V, int count, int l_type, const v
     p.batch = batch, p.beams = beams, p.V = V, p.count = count, p.l_type = l_type, p.eos = eos, p.logits = logits;
     p.scores = scores, p.finished = finished, p.workspace = workspace, p.new_scores = new_scores;
     p.parents = parents, p.tokens = tokens, p.new_finished = new_finished;
-    return beam_select_launch(p, current_stream());
+    return beam_select_launch(p, *ds, current_stream());
 }
 
 int isam_beam_reorder(int layers, int batch, int beams, int slots, size_t row_bytes, const int32_t *parents,

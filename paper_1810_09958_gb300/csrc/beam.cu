@@ -14,7 +14,12 @@
 // order entries were found in.
 #include <math_constants.h>
 
+#include <algorithm>
+#include <cfloat>
+#include <limits>
+
 #include "lm_common.cuh"
+#include "two.cuh"
 
 namespace isam {
 
@@ -23,7 +28,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPer = 16;                       // logits a thread and tile
 constexpr int kTile = kThreads * kPer;
-constexpr int kList = kTile + 1024;            // entries a CTA holds
+constexpr int kStages = 3;                     // tiles in shared memory: one looked at, two on their way
+constexpr int kFull = 512;                     // entries from which a careful reading cuts its list down
+constexpr int kList = kFull + 8 * kThreads;    // (it looks at up to 8 a thread at a time)
+constexpr float kNone = -std::numeric_limits<float>::infinity();
 
 using Key = unsigned long long;
 
@@ -34,9 +42,62 @@ __device__ __forceinline__ uint32_t ordered(float v) {
 __device__ __forceinline__ float unordered(uint32_t o) {
     return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
+__device__ __forceinline__ Key ordered(double v) {
+    const Key u = static_cast<Key>(__double_as_longlong(v));
+    return u ^ (static_cast<Key>(static_cast<long long>(u) >> 63) | 0x8000000000000000ull);
+}
 
-// The best min(n, count) of list[0, n), best first, into best[]; all threads of
-// the CTA call it, and list may be written again after it.
+// Sums of exponentials are kept relative to 2^r, r = ceil(top log2(e)) a whole
+// number: sums of different parts differ by exact powers of two, and with log2(e) in
+// two parts fma(x, lo, fma(x, hi, -r)) is log2(exp(x) / 2^r) but for the rounding of a
+// small number.  Where top is so large that r would not do (a row whose logits
+// are all the type's lowest value), they are relative to exp(top).
+constexpr float kLog2eHi = 1.44269502f, kLog2eLo = 1.92596303e-8f;
+constexpr float kHuge = 1.2676506e30f;  // 2^100
+struct Piece {
+    float top;  // largest logit (-inf: none)
+    float sum;
+};
+__device__ __forceinline__ bool huge(float top) { return !(fabsf(top) <= kHuge); }
+__device__ __forceinline__ float power_of(float top) { return ceilf(top * kLog2eHi); }
+__device__ __forceinline__ float term(float x, float r) { return exp2_fast(fmaf(x, kLog2eLo, fmaf(x, kLog2eHi, -r))); }
+// A part's sum relative to what belongs to `top`, the larger one.
+__device__ __forceinline__ float lift(Piece p, float top) {
+    if (p.top == top) return p.sum;
+    if (huge(top)) return p.sum * exp2_fast((p.top - top) * kLog2eHi);
+    return huge(p.top) ? 0.0f : p.sum * exp2_fast(power_of(p.top) - power_of(top));
+}
+__device__ __forceinline__ Piece join(Piece a, Piece b) {
+    const float m = fmaxf(a.top, b.top);
+    if (m == kNone) return Piece{m, 0.0f};
+    return Piece{m, lift(a, m) + lift(b, m)};
+}
+
+// log(x) of a positive finite x to 1e-11: x = m 2^e with m in [0.7, 1.42), and
+// log(m) = 2 atanh(q), q = (m - 1) / (m + 1), by its series (q^17 / 17 < 1e-14).
+// (The library's 64-bit functions cost this kernel 3 us.)
+__device__ double log_of(float x) {
+    int e = static_cast<int>(__float_as_uint(x) >> 23) - 127;
+    float mf = __uint_as_float((__float_as_uint(x) & 0x7fffffu) | 0x3f800000u);
+    if (mf > 1.41421356f) mf *= 0.5f, ++e;
+    const double m = mf, d = m + 1.0;
+    double inv = __fdividef(1.0f, mf + 1.0f);
+    inv = inv * (2.0 - d * inv);
+    inv = inv * (2.0 - d * inv);
+    const double q = (m - 1.0) * inv, q2 = q * q;
+    double p = 1.0 / 15;
+    p = p * q2 + 1.0 / 13;
+    p = p * q2 + 1.0 / 11;
+    p = p * q2 + 1.0 / 9;
+    p = p * q2 + 1.0 / 7;
+    p = p * q2 + 1.0 / 5;
+    p = p * q2 + 1.0 / 3;
+    p = p * q2 + 1.0;
+    return e * 0.69314718055994531 + 2.0 * q * p;
+}
+
+// The best of list[0, n), best first, in best[0, min(n, count)); all threads of the
+// CTA call it, and it may leave the list in any state.
 __device__ void take_best(Key *list, int n, int count, Key *best, Key *warp_best) {
     if (n <= 2 * kThreads) {
         // Each entry's place is the number of those above it.
@@ -65,15 +126,19 @@ __device__ void take_best(Key *list, int n, int count, Key *best, Key *warp_best
     }
 }
 
-struct Piece {
-    float top;  // largest logit (-inf: none)
-    float sum;  // sum of exp(logit - top)
-};
-
+// A CTA reads one piece of a row.  `floor` is a value that at least `count` entries
+// read so far reach: the threads are `groups` >= count groups, and it is the
+// lowest of the groups' largest values (a few times `count` entries reach it, and of
+// a later tile ever fewer; it is raised behind tiles 0, 1, 2, 4, 8, ...).  Entries at or above it are
+// listed, and at the end the best of the list picked.  A list that overflows (rows in ascending order)
+// is filled again by a second reading that knows the last floor, and, where too
+// many entries are equal, cuts the list down to its exact best tile by tile.
 template <typename L>
-__global__ void __launch_bounds__(kThreads)
-    beam_rows_kernel(int V, int count, int pieces, int piece, const L *logits, const float *scores,
+__global__ void __launch_bounds__(kThreads, 3)
+    beam_rows_kernel(int V, int count, int groups, int pieces, int piece, const L *logits, const float *scores,
                      const uint8_t *finished, Piece *out, Key *out_best) {
+    constexpr int E = 16 / sizeof(L), kVectors = kPer / E;
+    extern __shared__ uint4 ring[];  // [kStages][kVectors][kThreads]: a thread reads what it brought itself
     __shared__ Key list[kList];
     __shared__ Key best[64];
     __shared__ Key warp_best[kThreads / 32];
@@ -82,265 +147,490 @@ __global__ void __launch_bounds__(kThreads)
     __shared__ Piece warp_piece[kThreads / 32];
     dependent_start();
     const int row = blockIdx.x / pieces, part = blockIdx.x % pieces;
-    Key *row_best = out_best + static_cast<int64_t>(blockIdx.x) * count;
     const float score = scores[row];
     if ((finished && finished[row]) || !(fabsf(score) < CUDART_INF_F)) return;  // the merge does not look at it
-    const int lo = part * piece, hi = min(V, lo + piece);
     const L *l = logits + static_cast<int64_t>(row) * V;
-    const int groups = count <= 8 ? 8 : count <= 16 ? 16 : count <= 32 ? 32 : 64, lanes = kThreads / groups;
-    float top = -CUDART_INF_F, sum = 0.0f, floor = -CUDART_INF_F;
+    // Whole 16-byte words from the row's first boundary; what lies before belongs to the first piece, what is behind to the last.
+    const int skew = min(V, static_cast<int>((16 - reinterpret_cast<uintptr_t>(l) % 16) % 16 / sizeof(L)));
+    const int words = (V - skew) / E;
+    const int lo = min(words, part * piece), hi = min(words, lo + piece);
+    const uint4 *w = reinterpret_cast<const uint4 *>(l + skew);
+    const int lanes = kThreads / groups;
     if (threadIdx.x == 0) listed = 0;
-    __syncthreads();
-    for (int at = lo; at < hi; at += kTile) {
-        float v[kPer], m = -CUDART_INF_F;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int t = at + i * kThreads + threadIdx.x;
-            // (the larger of NaN and -inf is -inf; -0 becomes 0)
-            v[i] = t < hi ? fmaxf(to_f32(l[t]), -CUDART_INF_F) + 0.0f : -CUDART_INF_F;
-            m = fmaxf(m, v[i]);
-        }
-        if (m > top) {
-            sum *= exp2f((top - m) * 1.4426950408889634f);
-            top = m;
-        }
-        if (top > -CUDART_INF_F)
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) sum += exp2f((v[i] - top) * 1.4426950408889634f);
-        if (at == lo) {
-            // At least `count` entries are no lower than the lowest of `count` groups' largest.
-            float g = m;
-            for (int d = 1; d < lanes; d <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, d));
-            if (threadIdx.x % lanes == 0) group_top[threadIdx.x / lanes] = g;
-            __syncthreads();
-            floor = group_top[0];
-            for (int i = 1; i < groups; ++i) floor = fminf(floor, group_top[i]);
-        }
-        if (m >= floor && m > -CUDART_INF_F)
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (v[i] >= floor && v[i] > -CUDART_INF_F)
-                    list[atomicAdd(&listed, 1)] =
-                        static_cast<Key>(ordered(v[i])) << 32 | static_cast<uint32_t>(~(at + i * kThreads + threadIdx.x));
+    float top = kNone, sum = 0.0f, r = 0.0f;
+    float floor = -FLT_MAX, keep = -FLT_MAX;  // (-inf is never listed)
+    bool over = false;
+
+    // The floor from what every thread has read.
+    const auto raise = [&] {
+        float g = top;
+        for (int d = 1; d < lanes; d <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, d));
+        __syncthreads();
+        if (threadIdx.x % lanes == 0) group_top[threadIdx.x / lanes] = g;
+        __syncthreads();
+        g = group_top[threadIdx.x % groups];
+        if (groups == 64) g = fminf(g, group_top[threadIdx.x % 64 ^ 32]);
+        for (int d = 1; d < groups && d < 32; d <<= 1) g = fminf(g, __shfl_xor_sync(~0u, g, d));
+        floor = fmaxf(floor, g);
+        keep = fmaxf(keep, g);
+    };
+    const auto push = [&](float v, int token) {
+        const int at = atomicAdd(&listed, 1);
+        if (at < kList) list[at] = static_cast<Key>(ordered(v)) << 32 | static_cast<uint32_t>(~token);
+        over = at >= kFull;
+    };
+    // Where there are more than `most`, those below `keep` go.
+    const auto cut = [&](int most) {
         __syncthreads();
         const int n = listed;
-        if (n > kList - kTile) {
-            take_best(list, n, count, best, warp_best);
-            if (threadIdx.x < count) list[threadIdx.x] = best[threadIdx.x];
-            floor = unordered(static_cast<uint32_t>(best[count - 1] >> 32));
-            if (threadIdx.x == 0) listed = count;
-        }
-        __syncthreads();
-    }
-    const int n = listed;
-    take_best(list, n, count, best, warp_best);
-    if (threadIdx.x < count) row_best[threadIdx.x] = threadIdx.x < n ? best[threadIdx.x] : 0;
+        if (n <= most) return n;
+        const Key least = static_cast<Key>(ordered(keep)) << 32;
+        int kept = 0;
+        for (int from = 0; from < n; from += 8 * kThreads) {
+            // (what is kept lands in places that have been read)
+            Key mine[8];
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        const float t2 = __shfl_xor_sync(~0u, top, d), s2 = __shfl_xor_sync(~0u, sum, d);
-        const float m = fmaxf(top, t2);
-        if (m > -CUDART_INF_F)
-            sum = sum * exp2f((top - m) * 1.4426950408889634f) + s2 * exp2f((t2 - m) * 1.4426950408889634f);
-        top = m;
+            for (int i = 0; i < 8; ++i) {
+                const int at = from + i * kThreads + threadIdx.x;
+                mine[i] = at < n ? list[at] : 0;
+            }
+            __syncthreads();
+            if (threadIdx.x == 0) listed = kept;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (mine[i] >= least && mine[i] != 0) list[atomicAdd(&listed, 1)] = mine[i];
+            __syncthreads();
+            kept = listed;
+            __syncthreads();
+        }
+        return kept;
+    };
+
+    const auto fetch = [&](int at, int stage) {
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) {
+            const int t = at + i * kThreads + threadIdx.x;
+            const uint32_t to = smem_u32(&ring[(stage * kVectors + i) * kThreads + threadIdx.x]);
+            if (t < hi) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(w + t) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int pass = 0, tile = 0;
+    // One word a thread at a time, the list cut down when it is long.
+    const auto careful = [&](uint32_t which, int at) {
+        for (int i = 0; i < kVectors; ++i) {
+            for (int k = 0; k < E; ++k) {
+                const int token = skew + (at + i * kThreads + threadIdx.x) * E + k;
+                if (which >> (i * E + k) & 1) {
+                    const float v = to_f32(l[token]) + 0.0f;
+                    if (v >= floor) push(v, token);
+                }
+            }
+            if (!__syncthreads_or(over)) continue;
+            over = false;
+            const int n = cut(kFull / 2);
+            if (n > kFull / 2) {
+                take_best(list, n, count, best, warp_best);
+                if (threadIdx.x < count) list[threadIdx.x] = best[threadIdx.x];
+                // Later tokens lose to equal values: from here on only larger ones are listed.
+                const uint32_t last = static_cast<uint32_t>(best[count - 1] >> 32);
+                keep = fmaxf(keep, unordered(last));
+                floor = fmaxf(floor, unordered(last + 1));
+                if (threadIdx.x == 0) listed = count;
+                __syncthreads();
+            }
+        }
+    };
+    const auto look = [&](int at, int stage) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+        uint4 brought[kVectors];
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) brought[i] = ring[(stage * kVectors + i) * kThreads + threadIdx.x];
+        fetch(at + (kStages - 1) * kThreads * kVectors, stage == 0 ? kStages - 1 : stage - 1);
+        float v[kPer];
+        const bool whole = at + kThreads * kVectors <= hi;
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) {
+            const uint32_t word[4] = {brought[i].x, brought[i].y, brought[i].z, brought[i].w};
+#pragma unroll
+            for (int k = 0; k < E; ++k) {
+                if constexpr (E == 4) v[i * E + k] = __uint_as_float(word[k]);
+                else v[i * E + k] = __uint_as_float(k % 2 ? word[k / 2] & 0xffff0000u : word[k / 2] << 16);
+            }
+        }
+        if (!whole)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (at + i / E * kThreads + threadIdx.x >= hi) v[i] = kNone;
+        float m = fmaxf(v[0], kNone);  // (the larger of NaN and -inf is -inf)
+#pragma unroll
+        for (int i = 1; i < kPer; ++i) m = fmaxf(m, v[i]);
+        if (pass == 0) {
+            if (m > top) {
+                sum = lift(Piece{top, sum}, m);
+                top = m;
+                r = power_of(m);
+            }
+            Two sums[2] = {two(0.0f, 0.0f), two(0.0f, 0.0f)};
+            const Two minus = two(-r, -r), hi2 = two(kLog2eHi, kLog2eHi), lo2 = two(kLog2eLo, kLog2eLo);
+#pragma unroll
+            for (int i = 0; i < kPer; i += 2) {
+                const Two x = two(v[i], v[i + 1]);
+                sums[i / 2 % 2] = add2(sums[i / 2 % 2], exp2_fast(fma(x, lo2, fma(x, hi2, minus))));
+            }
+            const float2 ends = apart(add2(sums[0], sums[1]));
+            float part_sum = ends.x + ends.y;
+            if (!(part_sum <= kTile) || huge(top)) {
+                // A NaN among the logits, nothing above -inf so far, or logits beyond 2^100.
+                part_sum = 0.0f;
+                if (top > kNone)
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) {
+                        const float x = fmaxf(v[i], kNone);
+                        part_sum += huge(top) ? exp2_fast((x - top) * kLog2eHi) : term(x, r);
+                    }
+            }
+            sum += part_sum;
+            if ((tile & (tile - 1)) == 0) raise();
+        }
+        uint32_t again = 0;
+        if (m >= floor) {
+            uint32_t which = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) which |= v[i] >= floor ? 1u << i : 0;
+            const auto list_those = [&](uint32_t some) {
+                for (; some != 0; some &= some - 1) {
+                    // (from shared memory: a register cannot be picked by number)
+                    const int i = __ffs(some) - 1;
+                    const L *word = reinterpret_cast<const L *>(&ring[(stage * kVectors + i / E) * kThreads + threadIdx.x]);
+                    push(to_f32(word[i % E]) + 0.0f, skew + (at + i / E * kThreads + threadIdx.x) * E + i % E);  // (-0 becomes 0)
+                }
+            };
+            if (pass == 0) list_those(which);
+            else again = which;
+        }
+        if (pass == 1) careful(again, at);
+        ++tile;
+    };
+    // What lies before the first boundary and behind the last, one value a thread.
+    const int behind = V - skew - words * E;
+    const auto edge = [&](int n, int first) {
+        const float v = threadIdx.x < n ? fmaxf(to_f32(l[first + threadIdx.x]), kNone) + 0.0f : kNone;
+        if (v > kNone) {
+            if (pass == 0) {
+                const Piece p = join(Piece{top, sum}, Piece{v, huge(v) ? 1.0f : term(v, power_of(v))});
+                top = p.top, sum = p.sum, r = power_of(top);
+            }
+            if (v >= floor) push(v, first + threadIdx.x);
+        }
+    };
+    __syncthreads();
+    for (; pass < 2; ++pass) {
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) fetch(lo + i * kThreads * kVectors, i);
+        if (part == 0) edge(skew, 0);
+        int stage = 0;
+        for (int at = lo; at < hi; at += kThreads * kVectors) {
+            look(at, stage);
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        if (part == pieces - 1) edge(behind, V - behind);
+        if (pass == 1) break;
+        __syncthreads();
+        const bool whole = listed <= kList;
+        __syncthreads();
+        if (whole) break;
+        if (threadIdx.x == 0) listed = 0;
+        over = false;
+        raise();  // (and every thread sees the empty list)
     }
-    if (threadIdx.x % 32 == 0) warp_piece[threadIdx.x / 32] = Piece{top, sum};
+    const int n = cut(128);
+    take_best(list, n, count, best, warp_best);
+    Key *row_best = out_best + static_cast<int64_t>(blockIdx.x) * count;
+    if (threadIdx.x < count) row_best[threadIdx.x] = threadIdx.x < n ? best[threadIdx.x] : 0;
+    Piece p{top, sum};
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1)
+        p = join(p, Piece{__shfl_xor_sync(~0u, p.top, d), __shfl_xor_sync(~0u, p.sum, d)});
+    if (threadIdx.x % 32 == 0) warp_piece[threadIdx.x / 32] = p;
     __syncthreads();
     if (threadIdx.x == 0) {
-        Piece p = warp_piece[0];
-        for (int i = 1; i < kThreads / 32; ++i) {
-            const Piece q = warp_piece[i];
-            const float m = fmaxf(p.top, q.top);
-            if (m > -CUDART_INF_F)
-                p.sum = p.sum * exp2f((p.top - m) * 1.4426950408889634f) + q.sum * exp2f((q.top - m) * 1.4426950408889634f);
-            p.top = m;
-        }
+        for (int i = 1; i < kThreads / 32; ++i) p = join(p, warp_piece[i]);
         out[blockIdx.x] = p;
     }
 }
 
-// A candidate of the merge: by score, then by its place (beam, logit, token).
+constexpr int kHeld = 4;                    // candidates a thread brings at a time
+constexpr int kMost = kHeld * kThreads + 64;  // candidates that the merge holds
+
 __global__ void __launch_bounds__(kThreads)
-    beam_merge_kernel(int beams, int count, int pieces, const float *scores, int eos, const uint8_t *finished,
+    beam_merge_kernel(int beams, int count, int groups, int pieces, const float *scores, int eos, const uint8_t *finished,
                       const Piece *part, const Key *part_best, float *new_scores, int32_t *parents, int32_t *tokens,
                       uint8_t *new_finished) {
     __shared__ double base[64];  // score - log-sum-exp
     __shared__ int kind[64];     // 0 none, 1 open, 2 ended
-    __shared__ double best_score[kThreads / 32];
-    __shared__ long long best_place[kThreads / 32];
+    __shared__ Piece held_part[kThreads];
+    __shared__ float terms[kThreads];
+    __shared__ Key group_top[64], warp_full[kThreads / 32];
+    // Candidates: their scores' bits in order (0: none), and what tells equal ones apart.
+    __shared__ Key score_of[kMost], entry_of[kMost];
+    __shared__ uint8_t beam_of[kMost];
+    __shared__ Key best_score[64], best_entry[64];
+    __shared__ uint8_t best_beam[64];
+    __shared__ int listed;
     dependent_start();
     const int64_t seq = blockIdx.x, first = seq * beams;
-    if (threadIdx.x < beams) {
-        const int64_t row = first + threadIdx.x;
-        const double score = scores[row];
-        int what = 0;
-        double at = 0.0;
-        if (fabs(score) < CUDART_INF) {
-            if (finished && finished[row]) {
-                what = 2;
-                at = score;
-            } else {
-                float top = -CUDART_INF_F;
-                for (int i = 0; i < pieces; ++i) top = fmaxf(top, part[row * pieces + i].top);
-                if (fabsf(top) < CUDART_INF_F) {
-                    double sum = 0.0;
-                    for (int i = 0; i < pieces; ++i) {
-                        const Piece p = part[row * pieces + i];
-                        if (p.top > -CUDART_INF_F)
-                            sum += p.sum * exp(static_cast<double>(p.top) - static_cast<double>(top));
-                    }
-                    what = 1;
-                    at = score - (static_cast<double>(top) + log(sum));
-                }
-            }
-        }
-        base[threadIdx.x] = at;
-        kind[threadIdx.x] = what;
-    }
-    __syncthreads();
-    // Round r takes the best candidate below round r - 1's.  Place: beam, then the key from the largest down.
-    const int each = pieces * count;
-    double last_score = CUDART_INF;
-    int last_beam = -1;
-    Key last_key = ~0ull;
-    for (int r = 0; r < count; ++r) {
-        double s = -CUDART_INF;
-        int beam = 64;
-        Key key = 0;
-        for (int i = threadIdx.x; i < beams * each; i += kThreads) {
-            const int k = i / each;
-            if (kind[k] == 0 || (kind[k] == 2 && i % each != 0)) continue;
-            Key e = 1;
-            double v = base[k];
-            if (kind[k] == 1) {
-                e = part_best[(first + k) * each + i % each];
-                if (e == 0) continue;
-                v += unordered(static_cast<uint32_t>(e >> 32));
-            }
-            const bool left = v < last_score || (v == last_score && (k > last_beam || (k == last_beam && e < last_key)));
-            if (left && (v > s || (v == s && (k < beam || (k == beam && e > key))))) s = v, beam = k, key = e;
-        }
+    const int each = pieces * count, all = beams * each;
+    // Entries of rows that the rows kernel did not look at are undefined; `kind` tells.
+    Key entry[kHeld];
+    const auto bring = [&](int from) {
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            const double s2 = __shfl_xor_sync(~0u, s, d);
-            const int b2 = __shfl_xor_sync(~0u, beam, d);
-            const Key k2 = __shfl_xor_sync(~0u, key, d);
-            if (s2 > s || (s2 == s && (b2 < beam || (b2 == beam && k2 > key)))) s = s2, beam = b2, key = k2;
+        for (int h = 0; h < kHeld; ++h) {
+            const int i = from + h * kThreads + threadIdx.x;
+            entry[h] = i < all ? part_best[first * each + i] : 0;
         }
-        __shared__ Key best_key[kThreads / 32];
-        if (threadIdx.x % 32 == 0) {
-            best_score[threadIdx.x / 32] = s;
-            best_place[threadIdx.x / 32] = beam;
-            best_key[threadIdx.x / 32] = key;
+    };
+    bring(0);
+    // Sums of exponentials: a thread a piece, kThreads / pieces beams at a time.
+    const int at_once = kThreads / pieces;
+    for (int from = 0; from < beams; from += at_once) {
+        const int k = from + threadIdx.x / pieces, i = threadIdx.x % pieces;
+        const bool on = threadIdx.x / pieces < at_once && k < beams;
+        double score = 0.0;
+        int what = 0;
+        Piece p{kNone, 0.0f};
+        if (on) {
+            p = part[(first + k) * pieces + i];
+            score = scores[first + k];
+            const bool ended = finished && finished[first + k];
+            if (fabs(score) < CUDART_INF) what = ended ? 2 : 1;
+            if (what != 1) p = Piece{kNone, 0.0f};
+        }
+        held_part[threadIdx.x] = p;
+        __syncthreads();
+        float top = p.top;
+        if (on) {
+#pragma unroll 4
+            for (int j = 0; j < pieces; ++j) top = fmaxf(top, held_part[threadIdx.x - i + j].top);
+        }
+        terms[threadIdx.x] = top > kNone ? lift(p, top) : 0.0f;
+        __syncthreads();
+        if (on && i == 0) {
+            float sum = 0.0f;
+#pragma unroll 4
+            for (int j = 0; j < pieces; ++j) sum += terms[threadIdx.x + j];
+            if (what == 1 && !(fabsf(top) < CUDART_INF_F)) what = 0;
+            const double zero = huge(top) ? static_cast<double>(top) : power_of(top) * 0.69314718055994531;
+            base[k] = what == 1 ? score - (zero + log_of(sum)) : score;
+            kind[k] = what;
         }
         __syncthreads();
-        for (int i = 0; i < kThreads / 32; ++i) {
-            const double s2 = best_score[i];
-            const int b2 = static_cast<int>(best_place[i]);
-            const Key k2 = best_key[i];
-            if (s2 > s || (s2 == s && (b2 < beam || (b2 == beam && k2 > key)))) s = s2, beam = b2, key = k2;
+    }
+    Key top = 0, full = 1;  // best of the thread; of the last entries of full lists
+    int held = 0;           // best of what was listed before
+    const int lanes = kThreads / groups;
+    for (int from = 0; from < all; from += kHeld * kThreads) {
+        if (from > 0) bring(from);
+        Key s[kHeld];
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) {
+            const int i = from + h * kThreads + threadIdx.x;
+            s[h] = 0;
+            if (i < all) {
+                const int beam = i / each, what = kind[beam];
+                if (what == 2 && i == beam * each) s[h] = ordered(base[beam]), entry[h] = 0;
+                if (what == 1 && entry[h] != 0)
+                    s[h] = ordered(base[beam] + unordered(static_cast<uint32_t>(entry[h] >> 32)));
+                if (i % count == count - 1) full = max(full, s[h]);
+            }
+            top = max(top, s[h]);
+        }
+        // A score that `count` candidates reach: the lowest of the largest of `groups` groups, as in the rows kernel,
+        // or the last of a full list of one piece.
+        Key g = top, f = full;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const Key o = __shfl_xor_sync(~0u, g, d);
+            if (d < lanes) g = max(g, o);
+            f = max(f, __shfl_xor_sync(~0u, f, d));
+        }
+        if (threadIdx.x % lanes == 0) group_top[threadIdx.x / lanes] = g;
+        if (threadIdx.x % 32 == 0) warp_full[threadIdx.x / 32] = f;
+        if (threadIdx.x == 0) listed = held;
+        if (threadIdx.x < held) {
+            score_of[threadIdx.x] = best_score[threadIdx.x];
+            entry_of[threadIdx.x] = best_entry[threadIdx.x];
+            beam_of[threadIdx.x] = best_beam[threadIdx.x];
         }
         __syncthreads();
-        if (threadIdx.x == 0) {
-            const bool found = beam < 64;
-            const int token = !found ? 0 : kind[beam] == 2 ? eos : static_cast<int>(~static_cast<uint32_t>(key));
-            const int64_t at = seq * count + r;
-            new_scores[at] = found ? static_cast<float>(s) : -CUDART_INF_F;
-            parents[at] = found ? beam : 0;
-            tokens[at] = token;
-            if (new_finished) new_finished[at] = found && (kind[beam] == 2 || token == eos);
+        g = group_top[threadIdx.x % groups];
+        if (groups == 64) g = min(g, group_top[threadIdx.x % 64 ^ 32]);
+        f = warp_full[threadIdx.x % (kThreads / 32)];
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const Key o = __shfl_xor_sync(~0u, g, d);
+            if (d < groups) g = min(g, o);
+            if (d < kThreads / 32) f = max(f, __shfl_xor_sync(~0u, f, d));
         }
-        last_score = s;
-        last_beam = beam;
-        last_key = key;
+        const Key floor = max(g, f);
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h)
+            if (s[h] >= floor) {
+                const int at = atomicAdd(&listed, 1);
+                score_of[at] = s[h];
+                entry_of[at] = entry[h];
+                beam_of[at] = static_cast<uint8_t>((from + h * kThreads + threadIdx.x) / each);
+            }
+        __syncthreads();
+        const int n = listed;
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            const Key mine = score_of[i];
+            int above = 0;
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) {
+                const Key o = score_of[j];
+                above += o > mine;
+                if (o == mine && j != i)
+                    above += beam_of[j] < beam_of[i] || (beam_of[j] == beam_of[i] && entry_of[j] > entry_of[i]);
+            }
+            if (above < count) {
+                best_score[above] = mine;
+                best_entry[above] = entry_of[i];
+                best_beam[above] = beam_of[i];
+            }
+        }
+        held = min(n, count);
+        __syncthreads();
+    }
+    if (threadIdx.x < count) {
+        const int64_t at = seq * count + threadIdx.x;
+        float score = kNone;
+        int beam = 0, token = 0, end = 0;
+        if (threadIdx.x < held) {
+            beam = best_beam[threadIdx.x];
+            const Key e = best_entry[threadIdx.x];
+            const bool ended = kind[beam] == 2;
+            token = ended ? eos : static_cast<int>(~static_cast<uint32_t>(e));
+            score = static_cast<float>(ended ? base[beam] : base[beam] + unordered(static_cast<uint32_t>(e >> 32)));
+            end = ended || token == eos;
+        }
+        new_scores[at] = score;
+        parents[at] = beam;
+        tokens[at] = token;
+        if (new_finished) new_finished[at] = static_cast<uint8_t>(end);
     }
 }
 
-constexpr int kChunk = 512;  // bytes of a row a CTA moves
-
-// A CTA moves one chunk of the rows of one layer's sequence: all of its beams'
-// chunks into shared memory, then each from its parent's.
-template <typename W>
+// Reordering.  A CTA moves kThreads words of the rows of one layer's sequence; a
+// thread reads its word of up to HELD beams' parents before it writes any, so rows
+// may change places (a call in place has HELD >= beams).
+template <typename W, int HELD>
 __global__ void __launch_bounds__(kThreads)
     beam_reorder_kernel(int batch, int beams, int slots, size_t row_bytes, int chunks, const int32_t *parents,
                         const int32_t *slot_ids, const char *state, char *new_state) {
-    extern __shared__ uint4 raw[];
-    W *held = reinterpret_cast<W *>(raw);
+    __shared__ int to[64], from[64];  // slots; to = -1: the row is left as it is
     dependent_start();
-    constexpr int words = kChunk / sizeof(W);
     const int chunk = blockIdx.x % chunks;
     const int64_t group = blockIdx.x / chunks;
     const int b = static_cast<int>(group % batch);
     const int64_t layer = group / batch;
-    const size_t at = static_cast<size_t>(chunk) * kChunk;
-    const int live = static_cast<int>((min(row_bytes - at, static_cast<size_t>(kChunk))) / sizeof(W));
-    const auto slot = [&](int k) { return slot_ids ? slot_ids[b * beams + k] : b * beams + k; };
-    for (int i = threadIdx.x; i < beams * words; i += kThreads) {
-        const int k = i / words, j = i % words, sl = slot(k);
-        if (j < live && sl >= 0 && sl < slots)
-            held[i] = reinterpret_cast<const W *>(state + (layer * slots + sl) * row_bytes + at)[j];
+    if (threadIdx.x < beams) {
+        const auto slot = [&](int k) { return slot_ids ? slot_ids[b * beams + k] : b * beams + k; };
+        const int parent = parents[b * beams + threadIdx.x];
+        int t = slot(threadIdx.x), f = parent >= 0 && parent < beams ? slot(parent) : -1;
+        if (t < 0 || t >= slots || f < 0 || f >= slots || (state == new_state && t == f)) t = f = -1;
+        to[threadIdx.x] = t;
+        from[threadIdx.x] = f;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < beams * words; i += kThreads) {
-        const int k = i / words, j = i % words, sl = slot(k), from = parents[b * beams + k];
-        if (j >= live || sl < 0 || sl >= slots || from < 0 || from >= beams) continue;
-        const int fs = slot(from);
-        if (fs < 0 || fs >= slots) continue;
-        reinterpret_cast<W *>(new_state + (layer * slots + sl) * row_bytes + at)[j] = held[from * words + j];
+    const size_t at = (static_cast<size_t>(chunk) * kThreads + threadIdx.x) * sizeof(W);
+    if (at >= row_bytes) return;
+    const char *src = state + layer * slots * row_bytes + at;
+    char *dst = new_state + layer * slots * row_bytes + at;
+    for (int k0 = 0; k0 < beams; k0 += HELD) {
+        W held[HELD];
+#pragma unroll
+        for (int k = 0; k < HELD; ++k)
+            if (k0 + k < beams && to[k0 + k] >= 0) held[k] = *reinterpret_cast<const W *>(src + from[k0 + k] * row_bytes);
+#pragma unroll
+        for (int k = 0; k < HELD; ++k)
+            if (k0 + k < beams && to[k0 + k] >= 0) *reinterpret_cast<W *>(dst + to[k0 + k] * row_bytes) = held[k];
     }
 }
 
-// Pieces a row is cut into, and their length: enough CTAs to fill the GPU, no more
-// than 64 pieces, and none shorter than a tile.
-void cut(int rows, int V, int *pieces, int *piece) {
-    int n = (152 * 4 + rows - 1) / rows;
-    const int most = (V + kTile - 1) / kTile;
-    n = n > most ? most : n;
-    n = n > 64 ? 64 : n;
-    *piece = (V + n - 1) / n;
-    *pieces = (V + *piece - 1) / *piece;
+template <typename W>
+int reorder(int layers, int batch, int beams, int slots, size_t row_bytes, const int32_t *parents, const int32_t *slot_ids,
+            const void *state, void *new_state, cudaStream_t s) {
+    const int64_t chunks = static_cast<int64_t>((row_bytes + sizeof(W) * kThreads - 1) / (sizeof(W) * kThreads));
+    const int64_t blocks = chunks * layers * batch;
+    if (blocks > 0x7fffffff) return set_error(ISAM_ERR_UNSUPPORTED, "isam_beam_reorder: too many bytes");
+    const bool in_place = state == new_state;
+    auto fn = beam_reorder_kernel<W, 8>;
+    if (in_place && beams > 8) fn = beam_reorder_kernel<W, 16>;
+    if constexpr (sizeof(W) <= 4)
+        if (in_place && beams > 16) fn = beam_reorder_kernel<W, 64>;
+    return launch_dependent(fn, dim3(static_cast<unsigned>(blocks)), kThreads, 0, s, 1, "launch beam_reorder_kernel",
+                            batch, beams, slots, row_bytes, static_cast<int>(chunks), parents, slot_ids,
+                            static_cast<const char *>(state), static_cast<char *>(new_state));
+}
+
+// Pieces a row is cut into, and 16-byte words of one: enough CTAs to fill the GPU
+// three CTAs deep, no more than 32 pieces, and none shorter than a word a thread.
+void cut(int rows, int V, int l_type, int *pieces, int *piece) {
+    const int E = l_type == ISAM_F32 ? 4 : 8, words = (V + E - 1) / E;
+    int n = (152 * 3 + rows - 1) / rows;
+    n = std::min(n, std::min(32, (words + kThreads - 1) / kThreads));
+    *piece = (words + n - 1) / n;
+    *pieces = (words + *piece - 1) / *piece;
+}
+
+int groups_of(int count) { return count <= 8 ? 8 : count <= 16 ? 16 : count <= 32 ? 32 : 64; }
+
+template <typename L>
+int rows_launch(const BeamDesc &p, int pieces, int piece, Piece *part, Key *best, const DeviceState &ds, cudaStream_t s) {
+    constexpr int smem = kStages * kTile * sizeof(L);
+    const auto fn = beam_rows_kernel<L>;
+    const int rc = ensure_smem_optin(reinterpret_cast<const void *>(fn), smem, ds.device, "cudaFuncSetAttribute(beam_rows_kernel)");
+    if (rc) return rc;
+    return launch_dependent(fn, dim3(static_cast<unsigned>(p.batch) * p.beams * pieces), kThreads, smem, s, 1,
+                            "launch beam_rows_kernel", p.V, p.count, groups_of(p.count), pieces, piece,
+                            static_cast<const L *>(p.logits), p.scores, p.finished, part, best);
 }
 
 }  // namespace
 
 size_t beam_select_workspace(int batch, int beams, int V, int count) {
+    // (fp32 logits have the larger number of pieces)
     int pieces, piece;
-    cut(batch * beams, V, &pieces, &piece);
+    cut(batch * beams, V, ISAM_F32, &pieces, &piece);
     return static_cast<size_t>(batch) * beams * pieces * (count * sizeof(Key) + sizeof(Piece));
 }
 
-int beam_select_launch(const BeamDesc &p, cudaStream_t s) {
+int beam_select_launch(const BeamDesc &p, DeviceState &ds, cudaStream_t s) {
     int pieces, piece;
     const int rows = p.batch * p.beams;
-    cut(rows, p.V, &pieces, &piece);
+    cut(rows, p.V, p.l_type, &pieces, &piece);
     Key *best = static_cast<Key *>(p.workspace);
     Piece *part = reinterpret_cast<Piece *>(best + static_cast<size_t>(rows) * pieces * p.count);
-    const dim3 grid(static_cast<unsigned>(rows) * pieces);
-    int rc;
-    if (p.l_type == ISAM_F32)
-        rc = launch_dependent(beam_rows_kernel<float>, grid, kThreads, 0, s, 1, "launch beam_rows_kernel", p.V, p.count,
-                              pieces, piece, static_cast<const float *>(p.logits), p.scores, p.finished, part, best);
-    else
-        rc = launch_dependent(beam_rows_kernel<bf16>, grid, kThreads, 0, s, 1, "launch beam_rows_kernel", p.V, p.count,
-                              pieces, piece, static_cast<const bf16 *>(p.logits), p.scores, p.finished, part, best);
+    const int rc = p.l_type == ISAM_F32 ? rows_launch<float>(p, pieces, piece, part, best, ds, s)
+                                        : rows_launch<bf16>(p, pieces, piece, part, best, ds, s);
     if (rc) return rc;
     return launch_dependent(beam_merge_kernel, dim3(p.batch), kThreads, 0, s, 1, "launch beam_merge_kernel", p.beams,
-                            p.count, pieces, p.scores, p.eos, p.finished, part, best, p.new_scores, p.parents, p.tokens,
-                            p.new_finished);
+                            p.count, groups_of(p.count), pieces, p.scores, p.eos, p.finished, part, best, p.new_scores,
+                            p.parents, p.tokens, p.new_finished);
 }
 
 int beam_reorder_launch(int layers, int batch, int beams, int slots, size_t row_bytes, const int32_t *parents,
                         const int32_t *slot_ids, const void *state, void *new_state, cudaStream_t s) {
-    const int64_t chunks = static_cast<int64_t>((row_bytes + kChunk - 1) / kChunk);
-    const int64_t blocks = chunks * layers * batch;
-    if (blocks > 0x7fffffff) return set_error(ISAM_ERR_UNSUPPORTED, "isam_beam_reorder: too many bytes");
     const uintptr_t odd = reinterpret_cast<uintptr_t>(state) | reinterpret_cast<uintptr_t>(new_state) | row_bytes;
-    const auto fn = odd % 16 == 0  ? beam_reorder_kernel<uint4>
-                    : odd % 4 == 0 ? beam_reorder_kernel<uint32_t>
-                    : odd % 2 == 0 ? beam_reorder_kernel<uint16_t>
-                                   : beam_reorder_kernel<uint8_t>;
-    return launch_dependent(fn, dim3(static_cast<unsigned>(blocks)), kThreads, static_cast<size_t>(beams) * kChunk, s, 1,
-                            "launch beam_reorder_kernel", batch, beams, slots, row_bytes, static_cast<int>(chunks),
-                            parents, slot_ids, static_cast<const char *>(state), static_cast<char *>(new_state));
+    const bool few = state != new_state || beams <= 16;  // else 64 words are held, of 4 bytes at most
+    if (odd % 16 == 0 && few)
+        return reorder<uint4>(layers, batch, beams, slots, row_bytes, parents, slot_ids, state, new_state, s);
+    if (odd % 4 == 0) return reorder<uint32_t>(layers, batch, beams, slots, row_bytes, parents, slot_ids, state, new_state, s);
+    if (odd % 2 == 0) return reorder<uint16_t>(layers, batch, beams, slots, row_bytes, parents, slot_ids, state, new_state, s);
+    return reorder<uint8_t>(layers, batch, beams, slots, row_bytes, parents, slot_ids, state, new_state, s);
 }
 
 }  // namespace isam

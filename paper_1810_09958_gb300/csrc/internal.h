@@ -282,7 +282,7 @@ struct BeamDesc {
     uint8_t *new_finished;
 };
 size_t beam_select_workspace(int batch, int beams, int V, int count);
-int beam_select_launch(const BeamDesc &p, cudaStream_t s);
+int beam_select_launch(const BeamDesc &p, DeviceState &ds, cudaStream_t s);
 int beam_reorder_launch(int layers, int batch, int beams, int slots, size_t row_bytes, const int32_t *parents,
                         const int32_t *slot_ids, const void *state, void *new_state, cudaStream_t s);
 

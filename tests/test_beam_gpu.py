@@ -83,6 +83,31 @@ def test_masks_ends_and_dead_beams(V, kind):
     check(l, s, count, -1, None)
 
 
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [37, 5003, 70001])
+def test_masks_of_the_lowest_value(V, kind):
+    """Tokens masked with the type's lowest value, rows that hold nothing else, rows of very large logits."""
+    rng = np.random.default_rng(V)
+    low = torch.finfo(TYPES[kind]).min
+    l = logits_of(rng, (4, 3, V), kind)
+    l[0, :, 1::2] = low
+    l[1, 0] = low                       # uniform
+    l[1, 1] = low
+    l[1, 1, V // 3] = low / 2           # one token stands out
+    l[2] = l[2] * 1e32                  # differences of 1e32: one token takes all
+    l[3, :, ::5] = -1e35
+    s = scores_of(rng, (4, 3))
+    s[2] *= 1e33                        # (the sums of such rows are as large)
+    check(l[:2], s[:2], 6)
+    check(l[3:], s[3:], 6)
+    got = run(l[2:3], s[2:3], 3)
+    best = l[2].double().max(1)
+    for k in range(3):                  # each beam's own best token costs nothing, and all others 1e30 or more
+        at = [i for i in range(3) if got[1][0, i] == k]
+        assert all(got[0][0, i] <= s[2, k].item() for i in at)
+    assert got[2][0, 0] == best.indices[got[1][0, 0]].item()
+
+
 def test_ties_go_to_the_lower_beam_and_token():
     V, beams = 5000, 4
     l = torch.zeros(1, beams, V, device="cuda")
