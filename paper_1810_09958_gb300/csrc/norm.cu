@@ -9,6 +9,8 @@
 // as many warps as its row needs with NV vectors of V elements a thread; rows
 // that start on 16-byte boundaries take V = 8, others V = 1, neighbouring
 // threads on neighbouring elements either way.
+#include <algorithm>
+
 #include "lm_common.cuh"
 
 namespace isam {
@@ -22,12 +24,45 @@ struct alignas(V == 8 ? 16 : sizeof(T)) Vec {
     T v[V];
 };
 
+// V elements as they are loaded: whole words, taken apart where they are used (16-bit
+// elements in registers of their own would be waited for where they arrive).
+template <typename T, int V>
+struct Raw;
+template <int V>
+struct Raw<float, V> {
+    Vec<float, V> w;
+    __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const Vec<float, V> *>(p); }
+    __device__ __forceinline__ void word(int i, float4 q) { w.v[4 * i] = q.x, w.v[4 * i + 1] = q.y, w.v[4 * i + 2] = q.z, w.v[4 * i + 3] = q.w; }
+    __device__ __forceinline__ float operator[](int i) const { return w.v[i]; }
+};
+template <>
+struct Raw<bf16, 8> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const bf16 *p) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(p);
+        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+    }
+    __device__ __forceinline__ void word(int, float4 q) {
+        w[0] = __float_as_uint(q.x), w[1] = __float_as_uint(q.y), w[2] = __float_as_uint(q.z), w[3] = __float_as_uint(q.w);
+    }
+    __device__ __forceinline__ float operator[](int i) const {
+        return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+};
+template <>
+struct Raw<bf16, 1> {
+    uint32_t w;
+    __device__ __forceinline__ void load(const bf16 *p) { w = *reinterpret_cast<const uint16_t *>(p); }
+    __device__ __forceinline__ float operator[](int) const { return __uint_as_float(w << 16); }
+};
+
 // V elements at p as fp32.
 template <int V, typename T>
 __device__ __forceinline__ void load(const T *p, float (&f)[V]) {
-    const Vec<T, V> a = *reinterpret_cast<const Vec<T, V> *>(p);
+    Raw<T, V> a;
+    a.load(p);
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = to_f32(a.v[i]);
+    for (int i = 0; i < V; ++i) f[i] = a[i];
 }
 
 template <int V, typename T>
@@ -162,75 +197,130 @@ __global__ void __launch_bounds__(kMaxThreads)
     }
 }
 
-// Rows are walked by persistent CTAs, whose threads keep their columns' sums of
-// dw; the CTA's sum goes to a row of `part` in the workspace.  KEEP: r and dy
-// stay in registers between the sums and dx; else they are read again (wide rows).
-template <typename R, typename G, int V, int NV, bool KEEP>
-__global__ void __launch_bounds__(kMaxThreads)
-    norm_backward_kernel(int T, int D, int team_warps, int teams, const R *r, const float *w, float eps, const G *dy,
-                         const G *dres, G *dx, float *part) {
-    extern __shared__ float smem[];  // [teams - 1][D] behind the loop
+// How a backward pass has its operands: through a ring in shared memory, filled by
+// asynchronous copies some rows ahead (each thread reads back what it asked for
+// itself, so nothing waits for other threads); straight into registers (rows off 16-byte
+// boundaries); or, for wide rows, read twice, the second time from L2.
+enum { kRing, kKeep, kTwice };
+
+// Rows are walked by persistent CTAs, whose threads keep their columns' w and sums
+// of dw.  The CTA's sums go to a row of `part` in the workspace.
+template <typename R, typename G, int V, int NV, int MODE>
+__global__ void __launch_bounds__(MODE == kTwice ? 1024 : 512, MODE == kTwice || NV * V > 8 ? 1 : 2)
+    norm_backward_kernel(int T, int D, int team_warps, int teams, int stages, const R *r, const float *w, float eps,
+                         const G *dy, const G *dres, G *dx, float *part) {
+    extern __shared__ float4 smem_raw[];  // the ring; behind the loop the teams' sums, [teams - 1][D]
+    float *smem = reinterpret_cast<float *>(smem_raw);
     __shared__ float2 sums[2][32];
     dependent_start();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int team = warp / team_warps, tid = (warp - team * team_warps) * 32 + lane;
     const int step = team_warps * 32 * V;
-    float acc[NV][V];
+    constexpr bool HOLD = MODE != kTwice;
+    constexpr int HELD = HOLD ? NV : 1;
+    // 16-byte words of a thread and row: r, dy, dres.
+    constexpr int RW = V * sizeof(R) / 16, GW = V * sizeof(G) / 16, WORDS = NV * (RW + 2 * GW);
+    float acc[NV][V], ww[HELD][V];
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[j][i] = 0.0f;
+    if constexpr (HOLD)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = j * step + tid * V;
+            if (c < D) load<V>(w + c, ww[j]);
+        }
+    const bool with_res = dx && dres;
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * teams, first = static_cast<int64_t>(blockIdx.x) * teams;
+    const auto place = [&](int stage, int word) { return smem_raw + (stage * WORDS + word) * blockDim.x + threadIdx.x; };
+    const auto fetch = [&](int64_t row, int stage) {
+        if (row < T) {
+            const auto copy = [&](int word, const void *from) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(place(stage, word))), "l"(from)
+                             : "memory");
+            };
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int c = j * step + tid * V;
+                if (c >= D) continue;
+                const char *rp = reinterpret_cast<const char *>(r + row * D + c);
+                const char *gp = reinterpret_cast<const char *>(dy + row * D + c);
+                const char *dp = reinterpret_cast<const char *>(dres + row * D + c);
+#pragma unroll
+                for (int i = 0; i < RW; ++i) copy(j * (RW + 2 * GW) + i, rp + 16 * i);
+#pragma unroll
+                for (int i = 0; i < GW; ++i) copy(j * (RW + 2 * GW) + RW + i, gp + 16 * i);
+                if (with_res)
+#pragma unroll
+                    for (int i = 0; i < GW; ++i) copy(j * (RW + 2 * GW) + RW + GW + i, dp + 16 * i);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if constexpr (MODE == kRing)
+        for (int i = 0; i < stages - 1; ++i) fetch(first + team + i * stride, i);
 
-    int turn = 0;
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * teams; first < T;
-         first += static_cast<int64_t>(gridDim.x) * teams, turn ^= 1) {
-        const int64_t row = first + team;
+    int turn = 0, stage = 0;
+    for (int64_t row0 = first; row0 < T; row0 += stride) {
+        const int64_t row = row0 + team, base = row * D;
         const bool on = row < T;
-        const int64_t base = row * D;
-        Vec<R, V> rv[KEEP ? NV : 1];
-        Vec<G, V> gv[KEEP ? NV : 1];
-        float s2 = 0.0f, sd = 0.0f;
-        if constexpr (KEEP) {
+        Raw<R, V> rv[HELD];
+        Raw<G, V> gv[HELD];
+        if constexpr (MODE == kRing) {
+            if (stages == 2) asm volatile("cp.async.wait_group 0;" ::: "memory");
+            else asm volatile("cp.async.wait_group 1;" ::: "memory");
+            fetch(row + (stages - 1) * stride, stage == 0 ? stages - 1 : stage - 1);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int i = 0; i < RW; ++i) rv[j].word(i, *place(stage, j * (RW + 2 * GW) + i));
+#pragma unroll
+                for (int i = 0; i < GW; ++i) gv[j].word(i, *place(stage, j * (RW + 2 * GW) + RW + i));
+            }
+        } else if constexpr (MODE == kKeep) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int c = j * step + tid * V;
                 if (on && c < D) {
-                    rv[j] = *reinterpret_cast<const Vec<R, V> *>(r + base + c);
-                    gv[j] = *reinterpret_cast<const Vec<G, V> *>(dy + base + c);
+                    rv[j].load(r + base + c);
+                    gv[j].load(dy + base + c);
                 }
             }
         }
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
+        const auto operands = [&](int j, float (&a)[V], float (&g)[V], float (&wv)[V]) {
             const int c = j * step + tid * V;
-            if (on && c < D) {
-                float a[V], g[V], ww[V];
-                if constexpr (KEEP) {
+            if constexpr (HOLD) {
 #pragma unroll
-                    for (int i = 0; i < V; ++i) a[i] = to_f32(rv[j].v[i]), g[i] = to_f32(gv[j].v[i]);
-                } else {
-                    load<V>(r + base + c, a);
-                    load<V>(dy + base + c, g);
-                }
-                load<V>(w + c, ww);
+                for (int i = 0; i < V; ++i) a[i] = rv[j][i], g[i] = gv[j][i], wv[i] = ww[j][i];
+            } else {
+                load<V>(r + base + c, a);
+                load<V>(dy + base + c, g);
+                load<V>(w + c, wv);
+            }
+        };
+        float s2 = 0.0f, sd = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (on && j * step + tid * V < D) {
+                float a[V], g[V], wv[V];
+                operands(j, a, g, wv);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     s2 = fmaf(a[i], a[i], s2);
-                    sd = fmaf(a[i] * ww[i], g[i], sd);
+                    sd = fmaf(a[i] * wv[i], g[i], sd);
                 }
             }
-        }
         s2 = warp_sum(s2);
         sd = warp_sum(sd);
         if (team_warps > 1) {
             if (lane == 0) sums[turn][warp] = make_float2(s2, sd);
             __syncthreads();
-            s2 = sd = 0.0f;
-            for (int i = 0; i < team_warps; ++i) {
-                const float2 p = sums[turn][team * team_warps + i];
-                s2 += p.x;
-                sd += p.y;
-            }
+            // (each warp folds the team's words, lane by lane)
+            const float2 p = lane < team_warps ? sums[turn][team * team_warps + lane] : make_float2(0.0f, 0.0f);
+            s2 = warp_sum(p.x);
+            sd = warp_sum(p.y);
+            turn ^= 1;
         }
         const float k = rsqrtf(s2 / static_cast<float>(D) + eps);
         const float m = sd * k / static_cast<float>(D);  // mean(d n)
@@ -238,28 +328,34 @@ __global__ void __launch_bounds__(kMaxThreads)
         for (int j = 0; j < NV; ++j) {
             const int c = j * step + tid * V;
             if (on && c < D) {
-                float a[V], g[V], ww[V], o[V];
-                if constexpr (KEEP) {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) a[i] = to_f32(rv[j].v[i]), g[i] = to_f32(gv[j].v[i]);
-                } else {
-                    load<V>(r + base + c, a);
-                    load<V>(dy + base + c, g);
-                }
-                load<V>(w + c, ww);
+                float a[V], g[V], wv[V], o[V];
+                operands(j, a, g, wv);
 #pragma unroll
                 for (int i = 0; i < V; ++i) o[i] = 0.0f;
-                if (dx && dres) load<V>(dres + base + c, o);
+                if (with_res) {
+                    if constexpr (MODE == kRing) {
+                        Raw<G, V> d;
+#pragma unroll
+                        for (int i = 0; i < GW; ++i) d.word(i, *place(stage, j * (RW + 2 * GW) + RW + GW + i));
+#pragma unroll
+                        for (int i = 0; i < V; ++i) o[i] = d[i];
+                    } else {
+                        load<V>(dres + base + c, o);
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     const float n = a[i] * k;
                     acc[j][i] = fmaf(g[i], n, acc[j][i]);
-                    o[i] = fmaf(k, fmaf(-n, m, ww[i] * g[i]), o[i]);
+                    o[i] = fmaf(k, fmaf(-n, m, wv[i] * g[i]), o[i]);
                 }
                 if (dx) store<V>(dx + base + c, o);
             }
         }
+        stage = stage + 1 == stages ? 0 : stage + 1;
     }
+    if constexpr (MODE == kRing) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
     if (!part) return;
     // The teams' sums, in the teams' order.
     if (team > 0)
@@ -325,18 +421,29 @@ int forward(const NormDesc &p, cudaStream_t s) {
                             static_cast<Y *>(p.y), p.y8, p.y8_scales);
 }
 
-constexpr int kBackCtas = 152;  // the workspace has a row for each
+// CTAs of the backward pass at most; the workspace has a row for each.
+int back_ctas(int D) { return 152 * (D <= 2048 ? 6 : D <= 8192 ? 4 : 1); }
 
-template <typename R, typename G, int V, int NV, bool KEEP>
-int backward(const NormBackDesc &p, cudaStream_t s) {
+template <typename R, typename G, int V, int NV, int MODE>
+int backward(const NormBackDesc &p, const DeviceState &ds, cudaStream_t s) {
     const int tw = team_warps(p.D, V, NV);
-    const int teams = tw >= 16 ? 1 : 16 / tw;
+    const int teams = tw >= 8 ? 1 : 8 / tw, threads = teams * tw * 32;
+    size_t smem = static_cast<size_t>(teams - 1) * p.D * 4;
+    int stages = 1;
+    const auto fn = norm_backward_kernel<R, G, V, NV, MODE>;
+    if (MODE == kRing) {
+        const size_t stage = static_cast<size_t>(threads) * NV * V * (sizeof(R) + 2 * sizeof(G));
+        stages = stage > 36 * 1024 ? 2 : 3;
+        smem = std::max(smem, stages * stage);
+        const int rc = ensure_smem_optin(reinterpret_cast<const void *>(fn), static_cast<int>(smem), ds.device,
+                                         "cudaFuncSetAttribute(norm_backward_kernel)");
+        if (rc) return rc;
+    }
     const int64_t most = (p.T + static_cast<int64_t>(teams) - 1) / teams;
-    const int blocks = static_cast<int>(most < kBackCtas ? most : kBackCtas);
-    const size_t smem = static_cast<size_t>(teams - 1) * p.D * 4;
-    const auto fn = norm_backward_kernel<R, G, V, NV, KEEP>;
-    int rc = launch_dependent(fn, dim3(blocks), teams * tw * 32, smem, s, 1, "launch norm_backward_kernel", p.T, p.D,
-                              tw, teams, static_cast<const R *>(p.r), p.w, p.eps, static_cast<const G *>(p.dy),
+    const int room = ds.num_sms * std::max(1, std::min(static_cast<int>(220 * 1024 / (smem + 2048)), 1024 / threads));
+    const int blocks = static_cast<int>(std::min<int64_t>({most, back_ctas(p.D), room}));
+    int rc = launch_dependent(fn, dim3(blocks), threads, smem, s, 1, "launch norm_backward_kernel", p.T, p.D, tw, teams,
+                              stages, static_cast<const R *>(p.r), p.w, p.eps, static_cast<const G *>(p.dy),
                               static_cast<const G *>(p.dres), static_cast<G *>(p.dx), p.dw ? p.workspace : nullptr);
     if (rc || !p.dw) return rc;
     return launch_dependent(norm_sum_kernel, dim3((p.D + 31) / 32), 32 * kSumRows, 0, s, 1, "launch norm_sum_kernel",
@@ -345,7 +452,7 @@ int backward(const NormBackDesc &p, cudaStream_t s) {
 
 }  // namespace
 
-int norm_forward_launch(const NormDesc &p, DeviceState &, cudaStream_t s) {
+int norm_forward_launch(const NormDesc &p, DeviceState &ds, cudaStream_t s) {
     const bool wide = rows16(p.D, p.x_type, p.x) && rows16(p.D, p.r_type, p.res) && rows16(p.D, p.r_type, p.res_out) &&
                       reinterpret_cast<uintptr_t>(p.w) % 16 == 0 && p.D % 8 == 0 &&
                       (p.y ? rows16(p.D, p.y_type, p.y) : reinterpret_cast<uintptr_t>(p.y8) % 8 == 0);
@@ -356,7 +463,10 @@ int norm_forward_launch(const NormDesc &p, DeviceState &, cudaStream_t s) {
             const auto as = [&](auto y) {
                 using Y = decltype(y);
                 if (!wide) return p.D <= 8192 ? forward<X, R, Y, 1, 8>(p, s) : forward<X, R, Y, 1, 32>(p, s);
-                if (p.D <= 8192) return forward<X, R, Y, 8, 1>(p, s);
+                // Teams of up to 320 threads where there are rows enough (8192 x 4096, fp32 to E4M3: 512 threads 68 us, 256
+                // threads 57); a vector a thread where a row's latency counts.
+                if (p.D <= 2560 || (p.D <= 8192 && p.T <= 2 * ds.num_sms)) return forward<X, R, Y, 8, 1>(p, s);
+                if (p.D <= 5120) return forward<X, R, Y, 8, 2>(p, s);
                 return forward<X, R, Y, 8, 4>(p, s);
             };
             return p.y_type < 0 ? as(Mx()) : by_type(p.y_type, as);
@@ -364,9 +474,9 @@ int norm_forward_launch(const NormDesc &p, DeviceState &, cudaStream_t s) {
     });
 }
 
-size_t norm_backward_workspace(int, int D) { return static_cast<size_t>(kBackCtas) * D * 4; }
+size_t norm_backward_workspace(int, int D) { return static_cast<size_t>(back_ctas(D)) * D * 4; }
 
-int norm_backward_launch(const NormBackDesc &p, DeviceState &, cudaStream_t s) {
+int norm_backward_launch(const NormBackDesc &p, DeviceState &ds, cudaStream_t s) {
     if (!p.dx && !p.dw) return ISAM_OK;
     const bool wide = rows16(p.D, p.r_type, p.r) && rows16(p.D, p.g_type, p.dy) && rows16(p.D, p.g_type, p.dres) &&
                       rows16(p.D, p.g_type, p.dx) && reinterpret_cast<uintptr_t>(p.w) % 16 == 0 && p.D % 8 == 0;
@@ -374,9 +484,12 @@ int norm_backward_launch(const NormBackDesc &p, DeviceState &, cudaStream_t s) {
         return by_type(p.g_type, [&](auto g) {
             using R = decltype(r);
             using G = decltype(g);
-            if (!wide) return p.D <= 8192 ? backward<R, G, 1, 8, true>(p, s) : backward<R, G, 1, 32, false>(p, s);
-            if (p.D <= 8192) return backward<R, G, 8, 1, true>(p, s);
-            return backward<R, G, 8, 4, false>(p, s);
+            if (!wide) {
+                if (p.D <= 4096) return backward<R, G, 1, 8, kKeep>(p, ds, s);
+                return p.D <= 8192 ? backward<R, G, 1, 16, kKeep>(p, ds, s) : backward<R, G, 1, 32, kTwice>(p, ds, s);
+            }
+            if (p.D <= 4096) return backward<R, G, 8, 1, kRing>(p, ds, s);
+            return p.D <= 8192 ? backward<R, G, 8, 2, kRing>(p, ds, s) : backward<R, G, 8, 4, kTwice>(p, ds, s);
         });
     });
 }
