@@ -7,8 +7,8 @@
 // A row is held in the registers of one team of warps from its only reading to
 // its only writing, so the bound is HBM: every operand moves once.  A team has
 // as many warps as its row needs with NV vectors of V elements a thread; rows
-// that start on 16-byte boundaries take V = 8, others V = 1, neighbouring
-// threads on neighbouring elements either way.
+// that start on 16-byte boundaries take V = 8, or 4 where all are fp32 (a load
+// of 16 bytes a lane, without gaps between lanes), others V = 1.
 #include <algorithm>
 
 #include "lm_common.cuh"
@@ -20,7 +20,7 @@ namespace {
 constexpr int kMaxThreads = 1024;
 
 template <typename T, int V>
-struct alignas(V == 8 ? 16 : sizeof(T)) Vec {
+struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Vec {
     T v[V];
 };
 
@@ -47,6 +47,15 @@ struct Raw<bf16, 8> {
     }
     __device__ __forceinline__ float operator[](int i) const {
         return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+};
+template <>
+struct Raw<bf16, 4> {
+    uint2 w;
+    __device__ __forceinline__ void load(const bf16 *p) { w = *reinterpret_cast<const uint2 *>(p); }
+    __device__ __forceinline__ float operator[](int i) const {
+        const uint32_t u = i < 2 ? w.x : w.y;
+        return __uint_as_float(i % 2 ? u & 0xffff0000u : u << 16);
     }
 };
 template <>
@@ -114,6 +123,45 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
     return r;
 }
 
+// V outputs at column c of a row (all lanes of a warp call it: neighbouring vectors
+// of one row, their values 0 behind its end).
+template <typename Y, int V>
+__device__ __forceinline__ void put(const float (&o)[V], bool on, int64_t row, int c, int T, int D, Y *y, uint8_t *y8,
+                                    uint8_t *y8_scales) {
+    const int64_t at = row * D + c;
+    if constexpr (!std::is_same<Y, Mx>::value) {
+        if (on && c < D) store<V>(y + at, o);
+    } else {
+        // A block of 32 is 32 / V lanes; infinities and NaN have the largest bits.
+        const int lane = threadIdx.x % 32;
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(o[i]) & 0x7fffffffu);
+#pragma unroll
+        for (int d = 1; d < 32 / V; d <<= 1) top = max(top, __shfl_xor_sync(~0u, top, d));
+        float inv;
+        uint32_t scale = mx_scale(top, inv);
+        const int atom = c / 128, atoms = (D + 127) / 128;
+        if constexpr (V > 1) {
+            Vec<uint32_t, V / 4> q;
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i)
+                q.v[i] = e4m3x2(o[4 * i] * inv, o[4 * i + 1] * inv) | e4m3x2(o[4 * i + 2] * inv, o[4 * i + 3] * inv) << 16;
+            if (on && c < D) *reinterpret_cast<Vec<uint32_t, V / 4> *>(y8 + at) = q;
+            // The four blocks of an atom lie in 128 / V lanes: one word.
+            scale |= __shfl_down_sync(~0u, scale, 32 / V) << 8;
+            scale |= __shfl_down_sync(~0u, scale, 64 / V) << 16;
+            if (on && lane % (128 / V) == 0 && atom < atoms)
+                *reinterpret_cast<uint32_t *>(y8_scales + (static_cast<int64_t>(atom) * T + row) * 4) = scale;
+        } else {
+            if (on && c < D) y8[at] = static_cast<uint8_t>(e4m3x2(o[0] * inv, 0.0f));
+            if (on && lane == 0 && atom < atoms)
+                y8_scales[(static_cast<int64_t>(atom) * T + row) * 4 + c / 32 % 4] = static_cast<uint8_t>(scale);
+        }
+    }
+}
+
+// One row a team.
 template <typename X, typename R, typename Y, int V, int NV>
 __global__ void __launch_bounds__(kMaxThreads)
     norm_forward_kernel(int T, int D, int team_warps, int teams, const X *x, const R *res, R *res_out, const float *w,
@@ -166,34 +214,7 @@ __global__ void __launch_bounds__(kMaxThreads)
 #pragma unroll
             for (int i = 0; i < V; ++i) o[i] *= r[j][i] * k;
         }
-        if constexpr (!std::is_same<Y, Mx>::value) {
-            if (on && c < D) store<V>(y + base + c, o);
-        } else {
-            // A block of 32 is 4 lanes of 8 elements, or 32 lanes of one; infinities and NaN have the largest bits.
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(o[i]) & 0x7fffffffu);
-#pragma unroll
-            for (int d = 1; d < 32 / V; d <<= 1) top = max(top, __shfl_xor_sync(~0u, top, d));
-            float inv;
-            uint32_t scale = mx_scale(top, inv);
-            const int atom = c / 128, atoms = (D + 127) / 128;
-            if constexpr (V == 8) {
-                uint2 q;
-                q.x = e4m3x2(o[0] * inv, o[1] * inv) | e4m3x2(o[2] * inv, o[3] * inv) << 16;
-                q.y = e4m3x2(o[4] * inv, o[5] * inv) | e4m3x2(o[6] * inv, o[7] * inv) << 16;
-                if (on && c < D) *reinterpret_cast<uint2 *>(y8 + base + c) = q;
-                // The four blocks of an atom lie in 16 lanes: one word.
-                scale |= __shfl_down_sync(~0u, scale, 4) << 8;
-                scale |= __shfl_down_sync(~0u, scale, 8) << 16;
-                if (on && lane % 16 == 0 && atom < atoms)
-                    *reinterpret_cast<uint32_t *>(y8_scales + (static_cast<int64_t>(atom) * T + row) * 4) = scale;
-            } else {
-                if (on && c < D) y8[base + c] = static_cast<uint8_t>(e4m3x2(o[0] * inv, 0.0f));
-                if (on && lane == 0 && atom < atoms)
-                    y8_scales[(static_cast<int64_t>(atom) * T + row) * 4 + c / 32 % 4] = static_cast<uint8_t>(scale);
-            }
-        }
+        put<Y, V>(o, on, row, c, T, D, y, y8, y8_scales);
     }
 }
 
@@ -455,7 +476,7 @@ int backward(const NormBackDesc &p, const DeviceState &ds, cudaStream_t s) {
 int norm_forward_launch(const NormDesc &p, DeviceState &ds, cudaStream_t s) {
     const bool wide = rows16(p.D, p.x_type, p.x) && rows16(p.D, p.r_type, p.res) && rows16(p.D, p.r_type, p.res_out) &&
                       reinterpret_cast<uintptr_t>(p.w) % 16 == 0 && p.D % 8 == 0 &&
-                      (p.y ? rows16(p.D, p.y_type, p.y) : reinterpret_cast<uintptr_t>(p.y8) % 8 == 0);
+                      (p.y ? rows16(p.D, p.y_type, p.y) : reinterpret_cast<uintptr_t>(p.y8) % 8 == 0);  // (8 elements are a whole word of each)
     return by_type(p.x_type, [&](auto x) {
         return by_type(p.r_type, [&](auto r) {
             using X = decltype(x);
@@ -464,10 +485,13 @@ int norm_forward_launch(const NormDesc &p, DeviceState &ds, cudaStream_t s) {
                 using Y = decltype(y);
                 if (!wide) return p.D <= 8192 ? forward<X, R, Y, 1, 8>(p, s) : forward<X, R, Y, 1, 32>(p, s);
                 // Teams of up to 320 threads where there are rows enough (8192 x 4096, fp32 to E4M3: 512 threads 68 us, 256
-                // threads 57); a vector a thread where a row's latency counts.
-                if (p.D <= 2560 || (p.D <= 8192 && p.T <= 2 * ds.num_sms)) return forward<X, R, Y, 8, 1>(p, s);
-                if (p.D <= 5120) return forward<X, R, Y, 8, 2>(p, s);
-                return forward<X, R, Y, 8, 4>(p, s);
+                // threads 57; persistent CTAs with a ring of rows as in the backward pass: 91); a vector or two a
+                // thread where a row's latency counts.  Four elements where x and res are fp32 (8192 x 2560: 76 us
+                // with eight, 50 with four); where one is bf16, 57 with eight and 62 with four.
+                constexpr int V = sizeof(X) == 4 && sizeof(R) == 4 ? 4 : 8, F = 8 / V;
+                if (p.D <= 2560 || (p.D <= 8192 && p.T <= 2 * ds.num_sms)) return forward<X, R, Y, V, F>(p, s);
+                if (p.D <= 5120) return forward<X, R, Y, V, 2 * F>(p, s);
+                return forward<X, R, Y, V, 4 * F>(p, s);
             };
             return p.y_type < 0 ? as(Mx()) : by_type(p.y_type, as);
         });
@@ -488,8 +512,9 @@ int norm_backward_launch(const NormBackDesc &p, DeviceState &ds, cudaStream_t s)
                 if (p.D <= 4096) return backward<R, G, 1, 8, kKeep>(p, ds, s);
                 return p.D <= 8192 ? backward<R, G, 1, 16, kKeep>(p, ds, s) : backward<R, G, 1, 32, kTwice>(p, ds, s);
             }
-            if (p.D <= 4096) return backward<R, G, 8, 1, kRing>(p, ds, s);
-            return p.D <= 8192 ? backward<R, G, 8, 2, kRing>(p, ds, s) : backward<R, G, 8, 4, kTwice>(p, ds, s);
+            constexpr int V = sizeof(R) == 4 && sizeof(G) == 4 ? 4 : 8, F = 8 / V;
+            if (p.D <= 4096) return backward<R, G, V, F, kRing>(p, ds, s);
+            return p.D <= 8192 ? backward<R, G, V, 2 * F, kRing>(p, ds, s) : backward<R, G, V, 4 * F, kTwice>(p, ds, s);
         });
     });
 }
