@@ -407,62 +407,100 @@ __global__ void __launch_bounds__(384)
         static_cast<U *>(p.y)[(t * p.batch + b) * p.C + c] = from_f32<U>(0.0f);
 }
 
-// One token: G lanes a channel, S words of V states a lane, neighbouring lanes on neighbouring words.
+// One token: G lanes a channel, S words of V states a lane, neighbouring lanes on
+// neighbouring words; a thread has its channel of kSeqs sequences, whose states are all
+// asked for before any is used.  The bound is reading and writing the states (HBM).
+constexpr int kSeqs = 2;
+
 template <typename U, typename P, int V, int S, int G>
 __global__ void __launch_bounds__(kThreads)
-    ssm_step_kernel(int64_t channels, int C, int N, int slots, const U *u, const P *dt, const float *dt_bias,
-                    const float *A, const P *B, const P *Cm, int64_t bc_stride, const float *D, const P *z,
-                    int64_t z_stride, const int32_t *slot_ids, const float *state, float *new_state, U *y) {
+    ssm_step_kernel(int batch, int C, int N, int slots, const U *u, const P *dt, const float *dt_bias, const float *A,
+                    const P *B, const P *Cm, int64_t bc_stride, const float *D, const P *z, int64_t z_stride,
+                    const int32_t *slot_ids, const float *state, float *new_state, U *y) {
     dependent_start();
-    const int64_t i0 = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / G;
+    const int64_t c0 = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / G;
     const int part = threadIdx.x % G;
-    const bool on = i0 < channels;
-    const int64_t i = on ? i0 : channels - 1;
-    const int64_t b = i / C;
-    const int c = static_cast<int>(i - b * C);
-    const int slot = slot_ids ? slot_ids[b] : static_cast<int>(b);
-    const bool used = slot >= 0 && slot < slots;
-    float sum = 0.0f, out = 0.0f;
-    if (used) {
-        const float uv = to_f32(u[i]);
-        const float delta = softplus(to_f32(dt[i]) + (dt_bias ? dt_bias[c] : 0.0f));
-        const float in = delta * uv;
-        const int64_t at = (static_cast<int64_t>(slot) * C + c) * N;
+    const bool on = c0 < C;
+    const int c = on ? static_cast<int>(c0) : C - 1;
+    float a[S][V];
 #pragma unroll
-        for (int j = 0; j < S; ++j) {
-            const int n = (j * G + part) * V;
-            if (n < N) {
-                float h[V], a[V];
-                if constexpr (V == 4) {
-                    const float4 hv = *reinterpret_cast<const float4 *>(state + at + n);
-                    const float4 av = *reinterpret_cast<const float4 *>(A + static_cast<int64_t>(c) * N + n);
-                    h[0] = hv.x, h[1] = hv.y, h[2] = hv.z, h[3] = hv.w;
-                    a[0] = av.x, a[1] = av.y, a[2] = av.z, a[3] = av.w;
-                } else {
-                    h[0] = state[at + n];
-                    a[0] = A[static_cast<int64_t>(c) * N + n];
-                }
+    for (int j = 0; j < S; ++j) {
+        const int n = (j * G + part) * V;
+        const float *at = A + static_cast<int64_t>(c) * N + n;
+        if constexpr (V == 4) {
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (n < N) v = *reinterpret_cast<const float4 *>(at);
+            a[j][0] = v.x, a[j][1] = v.y, a[j][2] = v.z, a[j][3] = v.w;
+        } else {
+            a[j][0] = n < N ? *at : 0.0f;
+        }
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    h[k] = fmaf(exp2_fast(delta * (a[k] * kLog2e)), h[k], in * to_f32(B[b * bc_stride + n + k]));
-                    sum = fmaf(to_f32(Cm[b * bc_stride + n + k]), h[k], sum);
-                }
-                if (on) {
-                    if constexpr (V == 4)
-                        *reinterpret_cast<float4 *>(new_state + at + n) = make_float4(h[0], h[1], h[2], h[3]);
-                    else
-                        new_state[at + n] = h[0];
+        for (int k = 0; k < V; ++k) a[j][k] *= kLog2e;
+    }
+    const float bias = dt_bias ? dt_bias[c] : 0.0f, skip = D ? D[c] : 0.0f;
+    for (int64_t b0 = static_cast<int64_t>(blockIdx.y) * kSeqs; b0 < batch; b0 += static_cast<int64_t>(gridDim.y) * kSeqs) {
+        float h[kSeqs][S][V], uv[kSeqs], dv[kSeqs], zv[kSeqs];
+        int64_t at[kSeqs];
+        bool used[kSeqs];
+#pragma unroll
+        for (int q = 0; q < kSeqs; ++q) {
+            const int64_t b = b0 + q;
+            const int slot = b >= batch ? -1 : slot_ids ? slot_ids[b] : static_cast<int>(b);
+            used[q] = slot >= 0 && slot < slots;
+            at[q] = (static_cast<int64_t>(slot) * C + c) * N;
+            uv[q] = dv[q] = zv[q] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < S; ++j) {
+                const int n = (j * G + part) * V;
+#pragma unroll
+                for (int k = 0; k < V; ++k) h[q][j][k] = 0.0f;
+                if (used[q] && n < N) {
+                    if constexpr (V == 4) {
+                        const float4 v = *reinterpret_cast<const float4 *>(state + at[q] + n);
+                        h[q][j][0] = v.x, h[q][j][1] = v.y, h[q][j][2] = v.z, h[q][j][3] = v.w;
+                    } else {
+                        h[q][j][0] = state[at[q] + n];
+                    }
                 }
             }
+            if (used[q]) {
+                uv[q] = to_f32(u[b * C + c]);
+                dv[q] = to_f32(dt[b * C + c]);
+                if (z) zv[q] = to_f32(z[b * z_stride + c]);
+            }
         }
-        out = fmaf(D ? D[c] : 0.0f, uv, 0.0f);
-    }
 #pragma unroll
-    for (int d = 1; d < G; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
-    if (on && part == 0) {
-        out += sum;
-        if (used && z) out *= silu(to_f32(z[b * z_stride + c]));
-        y[i] = from_f32<U>(used ? out : 0.0f);
+        for (int q = 0; q < kSeqs; ++q) {
+            const int64_t b = b0 + q;
+            const float delta = softplus(dv[q] + bias), in = delta * uv[q];
+            float sum = 0.0f;
+            if (used[q])
+#pragma unroll
+                for (int j = 0; j < S; ++j) {
+                    const int n = (j * G + part) * V;
+                    if (n >= N) continue;
+                    const P *bp = B + b * bc_stride + n, *cp = Cm + b * bc_stride + n;
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        h[q][j][k] = fmaf(exp2_fast(delta * a[j][k]), h[q][j][k], in * to_f32(bp[k]));
+                        sum = fmaf(to_f32(cp[k]), h[q][j][k], sum);
+                    }
+                    if (on) {
+                        if constexpr (V == 4)
+                            *reinterpret_cast<float4 *>(new_state + at[q] + n) =
+                                make_float4(h[q][j][0], h[q][j][1], h[q][j][2], h[q][j][3]);
+                        else
+                            new_state[at[q] + n] = h[q][j][0];
+                    }
+                }
+#pragma unroll
+            for (int d = 1; d < G; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
+            if (on && part == 0 && b < batch) {
+                float out = fmaf(skip, uv[q], sum);
+                if (z) out *= silu(zv[q]);
+                y[b * C + c] = from_f32<U>(used[q] ? out : 0.0f);
+            }
+        }
     }
 }
 
@@ -507,11 +545,10 @@ int forward(const SsmDesc &p, int time_warps, int time_ctas, const DeviceState &
 
 template <typename U, typename P, int V, int S, int G>
 int step(const SsmDesc &p, cudaStream_t s) {
-    const int64_t channels = static_cast<int64_t>(p.batch) * p.C;
-    const int64_t blocks = (channels * G + kThreads - 1) / kThreads;
-    if (blocks > 0x7fffffff) return set_error(ISAM_ERR_UNSUPPORTED, "isam_ssm_step: batch x C too large");
-    return launch_dependent(ssm_step_kernel<U, P, V, S, G>, dim3(static_cast<unsigned>(blocks)), kThreads, 0, s, 1,
-                            "launch ssm_step_kernel", channels, p.C, p.N, p.slots, static_cast<const U *>(p.u),
+    const unsigned across = static_cast<unsigned>((static_cast<int64_t>(p.C) * G + kThreads - 1) / kThreads);
+    const int down = std::min((p.batch + kSeqs - 1) / kSeqs, 65535);
+    return launch_dependent(ssm_step_kernel<U, P, V, S, G>, dim3(across, static_cast<unsigned>(down)), kThreads, 0, s, 1,
+                            "launch ssm_step_kernel", p.batch, p.C, p.N, p.slots, static_cast<const U *>(p.u),
                             static_cast<const P *>(p.dt), p.dt_bias, p.A, static_cast<const P *>(p.B),
                             static_cast<const P *>(p.Cm), p.bc_stride, p.D, static_cast<const P *>(p.z), p.z_stride,
                             p.slot_ids, p.state, p.new_state, static_cast<U *>(p.y));

@@ -435,6 +435,13 @@ class _Call:
         them: a contiguous tensor, or the columns of one ([..., a:b])."""
         if t.is_contiguous():
             return self.ptr(t, dtype, count * width, name), width
+        if t.dtype is dtype and t.get_device() == self.device and t.numel() == count * width:
+            strides = t.stride()
+            if strides[-1] == 1:  # (what usually comes, without the loop below)
+                shape = t.shape
+                if shape[-1] == width and (len(shape) == 2 or len(shape) == 3 and strides[0] == shape[1] * strides[1]):
+                    if strides[-2] >= width:
+                        return t.data_ptr(), strides[-2]
         shape, strides = t.shape, t.stride()
         if not t.is_cuda:
             raise ValueError(f"{name} must be a CUDA tensor")
