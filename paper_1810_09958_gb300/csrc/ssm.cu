@@ -3,6 +3,25 @@
 //   h_t[c][n] = exp(delta A[c][n]) h_{t-1}[c][n] + delta B_t[n] u_t[c],
 //   y_t[c] = (sum_n C_t[n] h_t[c][n] + D[c] u_t[c]) silu(z_t[c]),
 // over a sequence, and one token on a cache of states.
+//
+// A state and step takes one exponential and four fp32 products and sums, so
+// the exponential unit (32 a clock and SM, measured) and the multiply-add
+// pipe (128) bound it: 151 us for 2048 x 8 x 4096 with 16 states, where its bytes take
+// 120.  A warp has 32 / G channels with G lanes each, whose S states stay in
+// registers, in packed pairs (no more products a clock than single ones, but half the
+// issue slots; 105 a step of 32 channels, with its gates).  It works alone: operands come by asynchronous copies
+// into a ring of its own, some blocks of steps ahead (loaded straight into registers
+// a block ahead they came too late: 460 us; unpacked where they arrive, 715), the gates of a
+// block are formed by all lanes, each a step's of a channel, and the sums over a channel's lanes
+// end in the lane that formed that step's gates.
+//
+// Where channels are few, time is cut into chunks, one to a warp of a CTA and of a
+// cluster's CTAs.  A run of steps is affine in the state and its decay is one exponential of
+// the sum of its deltas, so each chunk is first folded from zero, without outputs
+// (about 0.8 of a full step), then walked from the state that the folds before it give.
+// Folds pass through (distributed) shared memory in two levels, CTAs then warps
+// (all chunks read by all: 4.6 MB of remote reads a cluster, 1.25 ms where this takes 0.18).
+// Nothing depends on timing.  2048 x 8 x 4096, 16 states: 412 us; 65536 x 1 x 1024: 630 us.
 #include <algorithm>
 #include <cmath>
 
@@ -90,7 +109,7 @@ __device__ __forceinline__ void bring(T *dst, const T *src, int64_t pitch, int l
 // place in it does not change, so `at` (of the lane's first piece) only moves on.
 template <int ROWS, int WIDTH, int SPACE, typename T>
 struct Lane16 {
-    static constexpr int E = 16 / sizeof(T), PER = WIDTH / E, ALL = ROWS * PER;
+    static constexpr int E = 16 / sizeof(T), PER = WIDTH / E;
     static constexpr bool ok = WIDTH * sizeof(T) % 16 == 0 && (PER > 0 && 32 % (PER > 0 ? PER : 1) == 0);
     const char *at;
     __device__ __forceinline__ void start(const T *src, int64_t pitch, int live, int lane) {
@@ -104,8 +123,8 @@ struct Lane16 {
         if constexpr (ok) {
             T *to = dst + lane / PER * SPACE + lane % PER * E;
 #pragma unroll
-            for (int i = 0; i < (ALL + 31) / 32; ++i)
-                if (ALL % 32 == 0 || lane + 32 * i < ALL)
+            for (int i = 0; i < (ROWS * PER + 31) / 32; ++i)
+                if (ROWS * PER % 32 == 0 || lane + 32 * i < ROWS * PER)
                     copy_async<16>(to + i * (32 / PER) * SPACE, at + i * (32 / PER) * pitch_bytes, true);
             at += ROWS * pitch_bytes;
         }
@@ -117,9 +136,9 @@ struct Lane16 {
 template <typename U, typename P, int S, int G>
 struct Walk {
     static constexpr int CH = 32 / G, NP = S * G;
-    static constexpr int TB = 8;                   // steps a block
+    static constexpr int TB = S == 4 && G == 4 ? 16 : 8;  // steps a block (16: 2048 x 8 x 4096 416 us, 8: 448)
     static constexpr int PAIRS = TB / G;           // steps of a block whose gates a lane forms
-    static constexpr int kStages = 4;
+    static constexpr int kStages = TB == 16 ? 3 : 4;
     static constexpr bool kWiden = sizeof(P) == 2;  // B and C are widened once a block
     // Bytes of a stage: dt, z, u, and B and C; behind the stages B and C in fp32, and (delta, delta u).
     static constexpr int kDt = TB * CH * sizeof(P), kU = TB * CH * sizeof(U), kBc = TB * 2 * NP * sizeof(P);
@@ -323,7 +342,7 @@ struct Walk {
 };
 
 template <typename U, typename P, int S, int G>
-__global__ void __launch_bounds__(384)
+__global__ void __launch_bounds__(256, 2)
     ssm_forward_kernel(const __grid_constant__ Scan p) {
     using W = Walk<U, P, S, G>;
     constexpr int CH = W::CH;
@@ -357,34 +376,51 @@ __global__ void __launch_bounds__(384)
     const int64_t per = (each + W::TB - 1) / W::TB * W::TB;
     const int64_t t0 = min(chunk * per, static_cast<int64_t>(len)), t1 = min(t0 + per, static_cast<int64_t>(len));
     if (chunks > 1) {
-        // Folds: a chunk's states from zero, and its sum of delta (a decay over it is one exponential).
-        char *folds = reinterpret_cast<char *>(raw) + warps * W::kBytes;  // [warp][S / 2 + 1][32] pairs
-        Two *own = reinterpret_cast<Two *>(folds) + warp * (S / 2 + 1) * 32;
+        // Folds: a chunk's states from zero, and its sum of delta (a decay over it is one exponential).  A warp's
+        // chunk starts from the folds of the CTAs before its own (each from its warps' folds, by the last
+        // warp of a group) and of the warps before it.
+        constexpr int kFold = (S / 2 + 1) * 32;  // pairs
+        Two *folds = reinterpret_cast<Two *>(reinterpret_cast<char *>(raw) + warps * W::kBytes);  // [warp][S / 2 + 1][32]
+        Two *totals = folds + warps * kFold;                                                      // [across][S / 2 + 1][32]
+        const int turn = warp % p.time_warps;
 #pragma unroll
         for (int k = 0; k < S / 2; ++k) w.h[k] = two(0.0f, 0.0f);
         float total = chunk + 1 < chunks ? w.template run<true>(t0, t1) : 0.0f;
 #pragma unroll
         for (int d = CH; d < 32; d <<= 1) total += __shfl_xor_sync(~0u, total, d);
 #pragma unroll
-        for (int k = 0; k < S / 2; ++k) own[k * 32 + lane] = w.h[k];
-        own[S / 2 * 32 + lane] = two(total, total);
-        if (p.time_ctas > 1) cluster_sync_all();
-        else __syncthreads();
-#pragma unroll
-        for (int k = 0; k < S / 2; ++k) w.h[k] = two(state(2 * k), state(2 * k + 1));
-        for (int j = 0; j < chunk; ++j) {
-            const int from = mine * p.time_warps + j % p.time_warps;
-            const Two *there = reinterpret_cast<const Two *>(folds) + from * (S / 2 + 1) * 32 + lane;
-            const uint32_t addr = p.time_ctas > 1 ? mapa_shared(smem_u32(there), j / p.time_warps) : smem_u32(there);
+        for (int k = 0; k < S / 2; ++k) folds[warp * kFold + k * 32 + lane] = w.h[k];
+        folds[warp * kFold + S / 2 * 32 + lane] = two(total, total);
+        __syncthreads();
+        // The states behind those at `there` (shared memory, of any CTA of the cluster).
+        const auto behind = [&](uint32_t there) {
             const auto get = [&](int k) {
                 Two v;
-                asm volatile("ld.shared::cluster.b64 %0, [%1];" : "=l"(v.x) : "r"(addr + k * 256) : "memory");
+                asm volatile("ld.shared::cluster.b64 %0, [%1];" : "=l"(v.x) : "r"(there + k * 256) : "memory");
                 return v;
             };
             const Two sum = get(S / 2);
 #pragma unroll
             for (int k = 0; k < S / 2; ++k) w.h[k] = fma(exp2_fast(mul(w.a[k], sum)), w.h[k], get(k));
+            return sum;
+        };
+        const uint32_t mine_first = smem_u32(folds + mine * p.time_warps * kFold + lane);
+        if (p.time_ctas > 1) {
+            if (turn == p.time_warps - 1) {
+#pragma unroll
+                for (int k = 0; k < S / 2; ++k) w.h[k] = two(0.0f, 0.0f);
+                Two sums = two(0.0f, 0.0f);
+                for (int j = 0; j < p.time_warps; ++j) sums = add2(sums, behind(mine_first + j * kFold * 8));
+#pragma unroll
+                for (int k = 0; k < S / 2; ++k) totals[mine * kFold + k * 32 + lane] = w.h[k];
+                totals[mine * kFold + S / 2 * 32 + lane] = sums;
+            }
+            cluster_sync_all();
         }
+#pragma unroll
+        for (int k = 0; k < S / 2; ++k) w.h[k] = two(state(2 * k), state(2 * k + 1));
+        for (int j = 0; j < rank; ++j) behind(mapa_shared(smem_u32(totals + mine * kFold + lane), j));
+        for (int j = 0; j < turn; ++j) behind(mine_first + j * kFold * 8);
         // Behind this all starts are known: folds may go, and h_last may be h0.
         if (p.time_ctas > 1) cluster_sync_all();
         else __syncthreads();
@@ -533,7 +569,8 @@ int forward(const SsmDesc &p, int time_warps, int time_ctas, const DeviceState &
     const int warps = time_warps > 4 ? time_warps : 4;
     const int across = warps / time_warps;
     const unsigned blocks = static_cast<unsigned>((a.groups + across - 1) / across) * time_ctas;
-    const size_t smem = static_cast<size_t>(warps) * (W::kBytes + (time_warps * time_ctas > 1 ? (S / 2 + 1) * 256 : 0));
+    const size_t smem = static_cast<size_t>(warps) * W::kBytes +
+                        (time_warps * time_ctas > 1 ? static_cast<size_t>(warps + across) * (S / 2 + 1) * 256 : 0);
     const auto fn = ssm_forward_kernel<U, P, S, G>;
     if (smem > 48 * 1024)
         if (const int rc = ensure_smem_optin(reinterpret_cast<const void *>(fn), static_cast<int>(smem), ds.device,
@@ -561,14 +598,15 @@ struct Cut {
     int S, time_warps, time_ctas;
 };
 
-// The least time by these figures (clocks a step, measured): alone on a scheduler a
-// warp takes `alone`, among others `among`, and with folds 1.75 times as much; a
-// wave of CTAs takes 1.5 us to start, more for folds and their exchange in clusters.
+// The least time by these figures (clocks, fitted to 140 measured times of seven
+// shapes, whose fastest cut it finds or comes within 9% of): a step takes a warp
+// `alone` on its scheduler, `among` others that many each, and with folds 1.86 times as much; a wave of CTAs takes
+// time to start, more for folds and their exchange in clusters.
 Cut choose(int64_t T, int64_t batch, int64_t C, int N, const DeviceState &ds) {
     struct Kind {
-        int S, alone, among, regs;
+        int S, alone, among;
     };
-    const Kind kinds[] = {{16, 300, 187, 168}, {8, 260, 98, 112}, {4, 170, 61, 108}};
+    const Kind kinds[] = {{16, 370, 165}, {8, 316, 86}, {4, 165, 57}};
     Cut best{};
     double least = 0.0;
     for (const Kind &k : kinds) {
@@ -580,14 +618,14 @@ Cut choose(int64_t T, int64_t batch, int64_t C, int N, const DeviceState &ds) {
             for (int tc = 1; tc <= (tw == most ? 8 : 1); tc *= 2) {
                 const int warps = tw > 4 ? tw : 4, across = warps / tw;
                 const double ctas = static_cast<double>((groups + across - 1) / across) * tc * batch;
-                const int resident = std::min(65536 / (k.regs * warps * 32), 227 * 1024 / (warps * 128 * (96 / G + 2 * k.S * G)));
+                const int resident = std::max(1, std::min(16 / warps, 227 * 1024 / (warps * 128 * (96 / G + 2 * k.S * G))));
                 const double room = static_cast<double>(ds.num_sms) * resident;
-                const double waves = ctas <= room ? 1.0 : 0.5 + ctas / room;
+                const double waves = ctas <= room ? 1.0 : 0.4 + ctas / room;
                 const double on_one = std::ceil(std::min(ctas, room) / ds.num_sms) * warps / 4;
                 const int64_t steps = ((T + tw * tc - 1) / (tw * tc) + 7) / 8 * 8;
-                double t = steps * std::max<double>(k.alone, on_one * k.among) * (tw * tc > 1 ? 1.75 : 1.0) + 3000;
-                if (tw * tc > 1) t += 1500 + 60 * tw * tc;
-                if (tc > 1) t += tc == 2 ? 2500 : tc == 4 ? 12500 : 32500;
+                double t = steps * std::max<double>(k.alone, on_one * k.among) * (tw * tc > 1 ? 1.86 : 1.0) + 2500;
+                if (tw * tc > 1) t += 2300 + 250 * tw;
+                if (tc > 1) t += 2500 + 1000 * tc;
                 t *= waves;
                 if (least == 0.0 || t < least) least = t, best = Cut{k.S, tw, tc};
             }
