@@ -602,7 +602,7 @@ struct Cut {
 // shapes, whose fastest cut it finds or comes within 9% of): a step takes a warp
 // `alone` on its scheduler, `among` others that many each, and with folds 1.86 times as much; a wave of CTAs takes
 // time to start, more for folds and their exchange in clusters.
-Cut choose(int64_t T, int64_t batch, int64_t C, int N, const DeviceState &ds) {
+Cut choose(int64_t T, int64_t batch, int64_t C, int N, int u_size, int p_size, const DeviceState &ds) {
     struct Kind {
         int S, alone, among;
     };
@@ -614,11 +614,15 @@ Cut choose(int64_t T, int64_t batch, int64_t C, int N, const DeviceState &ds) {
         if (k.S * G < N || (k.S == 16 && N <= 8) || (k.S == 8 && N <= 4) || (k.S == 4 && N > 16)) continue;
         const int64_t groups = (C * G + 31) / 32;
         const int most = k.S * G > 32 ? 4 : 8;
+        // Shared memory of a warp (as Walk counts it), and warps that find room on an SM.
+        const int CH = 32 / G, TB = k.S == 4 && G == 4 ? 16 : 8;
+        const int bytes = (TB == 16 ? 3 : 4) * TB * (CH * (2 * p_size + u_size) + 2 * k.S * G * p_size) +
+                          (p_size == 2 ? TB * 2 * k.S * G * 4 : 0) + (G > 1 ? TB * CH * 8 : 0) + (k.S / 2 + 1) * 288;
         for (int tw = 1; tw <= most; tw *= 2)
             for (int tc = 1; tc <= (tw == most ? 8 : 1); tc *= 2) {
                 const int warps = tw > 4 ? tw : 4, across = warps / tw;
                 const double ctas = static_cast<double>((groups + across - 1) / across) * tc * batch;
-                const int resident = std::max(1, std::min(16 / warps, 227 * 1024 / (warps * 128 * (96 / G + 2 * k.S * G))));
+                const int resident = std::max(1, std::min(16 / warps, 227 * 1024 / (warps * bytes)));
                 const double room = static_cast<double>(ds.num_sms) * resident;
                 const double waves = ctas <= room ? 1.0 : 0.4 + ctas / room;
                 const double on_one = std::ceil(std::min(ctas, room) / ds.num_sms) * warps / 4;
@@ -636,7 +640,7 @@ Cut choose(int64_t T, int64_t batch, int64_t C, int N, const DeviceState &ds) {
 }  // namespace
 
 int ssm_forward_launch(const SsmDesc &p, DeviceState &ds, cudaStream_t s) {
-    const Cut c = choose(p.T, p.batch, p.C, p.N, ds);
+    const Cut c = choose(p.T, p.batch, p.C, p.N, p.u_type == ISAM_F32 ? 4 : 2, p.p_type == ISAM_F32 ? 4 : 2, ds);
     return by_type(p.u_type, [&](auto u) {
         return by_type(p.p_type, [&](auto q) {
             using U = decltype(u);
