@@ -641,8 +641,9 @@ int isam_rms_norm_backward(int T, int D, int r_type, const void *r, const float 
  *   y          [T][batch][C] (y_type)
  *   new_state  [batch][width - 1][C] (x_type), or NULL: the last inputs of each
  *              sequence, for isam_conv1d_step; may be state itself
- * Sums are fp32.  2 <= width <= 8, x_stride >= C, at most 2^40 values of y;
- * pointers aligned to their element.  ISAM_ERR_INVALID_ARG for sizes < 1, null
+ * Sums are fp32.  2 <= width <= 8, batch <= 65535, x_stride >= C, at most 2^40
+ * values of y; pointers aligned to their element; but for new_state outputs overlap
+ * no input.  ISAM_ERR_INVALID_ARG for sizes < 1, null
  * pointers, unknown types, silu not 0 or 1 or x_stride < C;
  * ISAM_ERR_UNSUPPORTED beyond the limits or for misaligned pointers.
  * Asynchronous on the stream set by isam_set_stream; no workspace.
@@ -656,7 +657,8 @@ int isam_conv1d_forward(int T, int batch, int C, int width, int x_type, const vo
  * `slots` entries; slot_ids, state and new_state as in isam_glr_step.
  *   x [batch] rows of C values, x_stride apart;  y [batch][C]
  *   state, new_state  [slots][width - 1][C] (x_type)
- * A padding row (slot outside [0, slots)) gets y = 0 and touches no state.
+ * A padding row (slot outside [0, slots)) gets y = 0 and touches no state.  Any
+ * batch; other limits and status codes as isam_conv1d_forward.
  */
 int isam_conv1d_step(int batch, int C, int width, int slots, int x_type, const void *x, int64_t x_stride,
                      const float *w, const float *bias, int silu, const int32_t *slot_ids, const void *state,
@@ -683,8 +685,9 @@ int isam_conv1d_step(int batch, int C, int width, int slots, int x_type, const v
  *   h_last   [batch][C][N] fp32 or NULL: the states after lengths[b] steps (h0
  *            where that is none); may be h0 itself
  * Gates, decays, states and sums are fp32; y alone is rounded.  Results do not
- * depend on timing.  1 <= N <= 128, strides >= their rows, at most 2^40 values
- * of y; pointers aligned to their element.  ISAM_ERR_INVALID_ARG for sizes < 1,
+ * depend on timing.  1 <= N <= 128, batch <= 65535, strides >= their rows, at most
+ * 2^40 values of y; pointers aligned to their element; but for h_last outputs
+ * overlap no input.  ISAM_ERR_INVALID_ARG for sizes < 1,
  * null pointers, unknown types or shorter strides; ISAM_ERR_UNSUPPORTED beyond
  * the limits or for misaligned pointers.  Asynchronous on the stream set by
  * isam_set_stream; no workspace.
@@ -699,7 +702,8 @@ int isam_ssm_forward(int T, int batch, int C, int N, int u_type, const void *u, 
  * entries; slot_ids, state and new_state as in isam_glr_step.
  *   u, dt, z, y [batch][C] (z rows z_stride apart), B, Cm [batch] rows of N
  *   state, new_state  [slots][C][N] fp32
- * A padding row gets y = 0 and touches no state.
+ * A padding row gets y = 0 and touches no state.  Any batch; other limits and
+ * status codes as isam_ssm_forward.
  */
 int isam_ssm_step(int batch, int C, int N, int slots, int u_type, const void *u, int p_type, const void *dt,
                   const float *dt_bias, const float *A, const void *B, const void *Cm, int64_t bc_stride,
@@ -716,7 +720,8 @@ int isam_beam_select_workspace(int batch, int beams, int V, int count, size_t *b
  * best first.
  *   logits    [batch][beams][V], fp32 (what isam_gemm and isam_gemv_w4 write) or
  *             bf16 (l_type).  -inf forbids a token, and so does NaN.  A row
- *             whose largest logit is +inf or -inf has no continuation.
+ *             whose largest logit is +inf or -inf has no continuation (one
+ *             that holds only the type's lowest value has: they are equal).
  *   scores    [batch][beams] fp32: each beam's sum of log-probabilities; -inf (or
  *             NaN, or +inf) marks a beam that has no continuation
  *   eos       the token that ends a sequence, or -1

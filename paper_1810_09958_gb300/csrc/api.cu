@@ -797,6 +797,12 @@ int ssm_validate(const char *name, const SsmDesc &p) {
     return ISAM_OK;
 }
 
+int sequences_validate(const char *name, int batch) {
+    // (a grid's axis)
+    if (batch > 65535) return set_error(ISAM_ERR_UNSUPPORTED, "%s: batch (%d) is above 65535", name, batch);
+    return ISAM_OK;
+}
+
 int cache_validate(const char *name, int batch, int slots, const int32_t *slot_ids, const void *state,
                    const void *new_state) {
     if (!state || !new_state) return set_error(ISAM_ERR_INVALID_ARG, "%s: null pointer", name);
@@ -872,6 +878,7 @@ int isam_conv1d_forward(int T, int batch, int C, int width, int x_type, const vo
     p.silu = silu, p.x = x, p.x_stride = x_stride, p.w = w, p.bias = bias, p.state = state, p.lengths = lengths;
     p.y = y, p.new_state = new_state;
     int rc = conv1d_validate("isam_conv1d_forward", p);
+    if (!rc) rc = sequences_validate("isam_conv1d_forward", batch);
     if (rc) return rc;
     DeviceState *ds = device_state(&rc);
     if (!ds) return rc;
@@ -902,6 +909,7 @@ int isam_ssm_forward(int T, int batch, int C, int N, int u_type, const void *u, 
     p.dt_bias = dt_bias, p.A = A, p.B = B, p.Cm = Cm, p.bc_stride = bc_stride, p.D = D, p.z = z;
     p.z_stride = z_stride, p.lengths = lengths, p.state = h0, p.new_state = h_last, p.y = y;
     int rc = ssm_validate("isam_ssm_forward", p);
+    if (!rc) rc = sequences_validate("isam_ssm_forward", batch);
     if (rc) return rc;
     DeviceState *ds = device_state(&rc);
     if (!ds) return rc;

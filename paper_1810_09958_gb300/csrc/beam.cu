@@ -147,8 +147,6 @@ __global__ void __launch_bounds__(kThreads, 3)
     __shared__ Piece warp_piece[kThreads / 32];
     dependent_start();
     const int row = blockIdx.x / pieces, part = blockIdx.x % pieces;
-    const float score = scores[row];
-    if ((finished && finished[row]) || !(fabsf(score) < CUDART_INF_F)) return;  // the merge does not look at it
     const L *l = logits + static_cast<int64_t>(row) * V;
     // Whole 16-byte words from the row's first boundary; what lies before belongs to the first piece, what is behind to the last.
     const int skew = min(V, static_cast<int>((16 - reinterpret_cast<uintptr_t>(l) % 16) % 16 / sizeof(L)));
@@ -156,6 +154,21 @@ __global__ void __launch_bounds__(kThreads, 3)
     const int lo = min(words, part * piece), hi = min(words, lo + piece);
     const uint4 *w = reinterpret_cast<const uint4 *>(l + skew);
     const int lanes = kThreads / groups;
+    const auto fetch = [&](int at, int stage) {
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) {
+            const int t = at + i * kThreads + threadIdx.x;
+            const uint32_t to = smem_u32(&ring[(stage * kVectors + i) * kThreads + threadIdx.x]);
+            if (t < hi) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(w + t) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    fetch(lo, 0);
+    const float score = scores[row];
+    if ((finished && finished[row]) || !(fabsf(score) < CUDART_INF_F)) {  // the merge does not look at it
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        return;
+    }
     if (threadIdx.x == 0) listed = 0;
     float top = kNone, sum = 0.0f, r = 0.0f;
     float floor = -FLT_MAX, keep = -FLT_MAX;  // (-inf is never listed)
@@ -207,15 +220,6 @@ __global__ void __launch_bounds__(kThreads, 3)
         return kept;
     };
 
-    const auto fetch = [&](int at, int stage) {
-#pragma unroll
-        for (int i = 0; i < kVectors; ++i) {
-            const int t = at + i * kThreads + threadIdx.x;
-            const uint32_t to = smem_u32(&ring[(stage * kVectors + i) * kThreads + threadIdx.x]);
-            if (t < hi) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(w + t) : "memory");
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
     int pass = 0, tile = 0;
     // One word a thread at a time, the list cut down when it is long.
     const auto careful = [&](uint32_t which, int at) {
@@ -327,8 +331,9 @@ __global__ void __launch_bounds__(kThreads, 3)
     };
     __syncthreads();
     for (; pass < 2; ++pass) {
+        if (pass == 1) fetch(lo, 0);
 #pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) fetch(lo + i * kThreads * kVectors, i);
+        for (int i = 1; i < kStages - 1; ++i) fetch(lo + i * kThreads * kVectors, i);
         if (part == 0) edge(skew, 0);
         int stage = 0;
         for (int at = lo; at < hi; at += kThreads * kVectors) {
@@ -356,9 +361,12 @@ __global__ void __launch_bounds__(kThreads, 3)
         p = join(p, Piece{__shfl_xor_sync(~0u, p.top, d), __shfl_xor_sync(~0u, p.sum, d)});
     if (threadIdx.x % 32 == 0) warp_piece[threadIdx.x / 32] = p;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < kThreads / 32; ++i) p = join(p, warp_piece[i]);
-        out[blockIdx.x] = p;
+    if (threadIdx.x < 32) {
+        p = warp_piece[threadIdx.x % (kThreads / 32)];
+#pragma unroll
+        for (int d = kThreads / 64; d > 0; d >>= 1)
+            p = join(p, Piece{__shfl_xor_sync(~0u, p.top, d), __shfl_xor_sync(~0u, p.sum, d)});
+        if (threadIdx.x == 0) out[blockIdx.x] = p;
     }
 }
 

@@ -111,12 +111,11 @@ template <typename X, typename Y, int V, int W>
 __global__ void __launch_bounds__(kThreads)
     conv1d_forward_kernel(int T, int batch, int C, int run, int silu_on, const X *x, int64_t x_stride, const float *w,
                           const float *bias, const X *state, const int32_t *lengths, Y *y, X *new_state) {
-    const int c = (blockIdx.x * kThreads + threadIdx.x) * V;
-    if (c >= C) return;
+    const int64_t c_wide = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * V;
+    if (c_wide >= C) return;
     dependent_start();
-    const int b = blockIdx.z % batch;
-    const int64_t first = (static_cast<int64_t>(blockIdx.y) + static_cast<int64_t>(blockIdx.z / batch) * gridDim.y) * run;
-    if (first >= T) return;
+    const int c = static_cast<int>(c_wide), b = blockIdx.z;
+    const int64_t first = static_cast<int64_t>(blockIdx.y) * run;
     const int len = lengths ? min(max(lengths[b], 0), T) : T;
     const int64_t pitch = static_cast<int64_t>(batch) * x_stride;
     const X *xb = x + b * x_stride + c;
@@ -267,12 +266,10 @@ int conv1d_forward_launch(const ConvDesc &p, DeviceState &ds, cudaStream_t s) {
         // Runs long enough that the inputs read twice are few, short enough to fill the GPU.
         int run = 32;
         while (run > 4 && static_cast<int64_t>(across) * p.batch * ((p.T + run - 1) / run) < ds.num_sms * 8) run /= 2;
-        const int64_t runs = (p.T + static_cast<int64_t>(run) - 1) / run;
-        const unsigned gy = static_cast<unsigned>(runs < 32768 ? runs : 32768);
-        const int64_t gz = (runs + gy - 1) / gy * p.batch;
-        if (gz > 65535) return set_error(ISAM_ERR_UNSUPPORTED, "isam_conv1d_forward: batch x steps too large");
-        return launch_dependent(conv1d_forward_kernel<X, Y, V, W>, dim3(across, gy, static_cast<unsigned>(gz)), kThreads,
-                                0, s, 1, "launch conv1d_forward_kernel", p.T, p.batch, p.C, run, p.silu,
+        while ((p.T + static_cast<int64_t>(run) - 1) / run > 65535) run *= 2;
+        const unsigned runs = static_cast<unsigned>((p.T + static_cast<int64_t>(run) - 1) / run);
+        return launch_dependent(conv1d_forward_kernel<X, Y, V, W>, dim3(across, runs, p.batch), kThreads, 0, s, 1,
+                                "launch conv1d_forward_kernel", p.T, p.batch, p.C, run, p.silu,
                                 static_cast<const X *>(p.x), p.x_stride, p.w, p.bias, static_cast<const X *>(p.state),
                                 p.lengths, static_cast<Y *>(p.y), static_cast<X *>(p.new_state));
     });

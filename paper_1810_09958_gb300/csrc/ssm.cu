@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(256, 2)
             if (w.part * S + 2 * k < p.N) p.h_last[first + 2 * k] = v.x;
             if (w.part * S + 2 * k + 1 < p.N) p.h_last[first + 2 * k + 1] = v.y;
         }
-    for (int64_t t = len + chunk * G + w.part; t < p.T; t += chunks * G)
+    for (int64_t t = static_cast<int64_t>(len) + chunk * G + w.part; t < p.T; t += chunks * G)
         static_cast<U *>(p.y)[(t * p.batch + b) * p.C + c] = from_f32<U>(0.0f);
 }
 
@@ -548,7 +548,6 @@ int by_type(int type, F &&f) {
 template <typename U, typename P, int S, int G>
 int forward(const SsmDesc &p, int time_warps, int time_ctas, const DeviceState &ds, cudaStream_t s) {
     using W = Walk<U, P, S, G>;
-    if (p.batch > 65535) return set_error(ISAM_ERR_UNSUPPORTED, "isam_ssm_forward: batch (%d) above 65535", p.batch);
     Scan a{};
     a.T = p.T, a.batch = p.batch, a.C = p.C, a.N = p.N, a.u = p.u, a.dt = p.dt, a.B = p.B, a.Cm = p.Cm, a.z = p.z;
     a.dt_bias = p.dt_bias, a.A = p.A, a.D = p.D, a.h0 = p.state, a.lengths = p.lengths, a.bc_stride = p.bc_stride;

@@ -59,6 +59,7 @@ CONV = dict(T=4, batch=2, C=8, width=4, xt=1, x=P, stride=8, w=P, bias=P, silu=1
     (dict(stride=-8), BAD), (dict(width=1), NO), (dict(width=9), NO), (dict(x=off(1)), NO), (dict(state=off(1)), NO),
     (dict(new=off(1)), NO), (dict(w=off(2)), NO), (dict(bias=off(2)), NO), (dict(lengths=off(1)), NO), (dict(y=off(2)), NO),
     (dict(T=BIG, batch=BIG), NO), (dict(T=2 ** 20, C=2 ** 21, stride=2 ** 21), NO), (dict(stride=2 ** 62), NO),
+    (dict(batch=65536), NO),
 ])
 def test_conv_forward(lib, change, code):
     refused(lib, "isam_conv1d_forward", CONV | dict(state=P, lengths=P, yt=0, y=P, new=P), change, code)
@@ -83,6 +84,7 @@ SSM = dict(ut=1, u=P, pt=0, dt=P, bias=P, A=P, B=P, Cm=P, bc=32, D=P, z=P, zs=16
     (dict(dt=off(2)), NO), (dict(bias=off(1)), NO), (dict(A=off(2)), NO), (dict(B=off(2)), NO), (dict(Cm=off(2)), NO),
     (dict(D=off(2)), NO), (dict(z=off(2)), NO), (dict(h0=off(2)), NO), (dict(lengths=off(2)), NO), (dict(y=off(1)), NO),
     (dict(last=off(2)), NO), (dict(T=BIG, batch=BIG), NO), (dict(bc=2 ** 50), NO), (dict(zs=2 ** 50), NO),
+    (dict(batch=65536), NO),
 ])
 def test_ssm_forward(lib, change, code):
     refused(lib, "isam_ssm_forward", dict(T=4, batch=2, C=8, N=16) | SSM | dict(h0=P, lengths=P, y=P, last=P), change, code)
