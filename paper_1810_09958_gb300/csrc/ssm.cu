@@ -9,10 +9,11 @@
 // pipe (128) bound it: 151 us for 2048 x 8 x 4096 with 16 states, where its bytes take
 // 120.  A warp has 32 / G channels with G lanes each, whose S states stay in
 // registers, in packed pairs (no more products a clock than single ones, but half the
-// issue slots; 105 a step of 32 channels, with its gates).  It works alone: operands come by asynchronous copies
+// issue slots).  It works alone: operands come by asynchronous copies
 // into a ring of its own, some blocks of steps ahead (loaded straight into registers
 // a block ahead they came too late: 460 us; unpacked where they arrive, 715), the gates of a
-// block are formed by all lanes, each a step's of a channel, and the sums over a channel's lanes
+// block are formed by all lanes, each a step's of a channel, beside the states of the block
+// before (four lanes a channel, 2048 x 1 x 2560, uncut: 149 -> 118 us), and the sums over a channel's lanes
 // end in the lane that formed that step's gates.
 //
 // Where channels are few, time is cut into chunks, one to a warp of a CTA and of a
@@ -21,7 +22,7 @@
 // (about 0.8 of a full step), then walked from the state that the folds before it give.
 // Folds pass through (distributed) shared memory in two levels, CTAs then warps
 // (all chunks read by all: 4.6 MB of remote reads a cluster, 1.25 ms where this takes 0.18).
-// Nothing depends on timing.  2048 x 8 x 4096, 16 states: 412 us; 65536 x 1 x 1024: 630 us.
+// Nothing depends on timing.  2048 x 8 x 4096, 16 states: 401 us; 65536 x 1 x 1024: 627 us.
 #include <algorithm>
 #include <cmath>
 
@@ -136,7 +137,7 @@ struct Lane16 {
 template <typename U, typename P, int S, int G>
 struct Walk {
     static constexpr int CH = 32 / G, NP = S * G;
-    static constexpr int TB = S == 4 && G == 4 ? 16 : 8;  // steps a block (16: 2048 x 8 x 4096 416 us, 8: 448)
+    static constexpr int TB = S == 4 && G == 4 ? 16 : 8;  // steps a block (16: 2048 x 8 x 4096 393 us, 8: 450)
     static constexpr int PAIRS = TB / G;           // steps of a block whose gates a lane forms
     static constexpr int kStages = TB == 16 ? 3 : 4;
     static constexpr bool kWiden = sizeof(P) == 2;  // B and C are widened once a block
@@ -145,8 +146,10 @@ struct Walk {
     static constexpr int up16(int n) { return (n + 15) / 16 * 16; }
     static constexpr int kStage = up16(kDt) * 2 + up16(kU) + up16(kBc);
     static constexpr int kWide = kWiden ? TB * 2 * NP * 4 : 0;
-    static constexpr int kGates = G > 1 ? TB * CH * 8 : 0;
-    static constexpr int kBytes = kStages * kStage + kWide + kGates;
+    static constexpr int kGates = TB * CH * 8;
+    // Where registers allow, the next block's gates are formed beside this one's states: a second place for them.
+    static constexpr int AHEAD = S < 16 ? 1 : 0;
+    static constexpr int kBytes = kStages * kStage + (1 + AHEAD) * (kWide + kGates);
 
     using DtLane = Lane16<TB, CH, CH, P>;
     using ULane = Lane16<TB, CH, CH, U>;
@@ -223,30 +226,47 @@ struct Walk {
         return x.x + x.y;
     }
 
-    // The steps of one block: gates, states, outputs.
-    template <bool FOLD, bool FULL>
-    __device__ __forceinline__ float block(int st, const float *bc, float2 *gates, int left, U *py, int64_t py_step) {
+    // The gates of a block, each lane those of its steps; returns the lane's sum of delta.
+    template <bool FULL>
+    __device__ __forceinline__ float form(int st, int left, float2 *gates, float *wide) {
         const int mine = lane % CH;
-        const P *dt = dt_of(st) + mine, *z = z_of(st) + mine;
+        const P *dt = dt_of(st) + mine;
         const U *u = u_of(st) + mine;
-        float delta[PAIRS], in[PAIRS], uv[PAIRS], total = 0.0f;
+        float2 g[PAIRS];
+        float total = 0.0f;
 #pragma unroll
         for (int j = 0; j < PAIRS; ++j) {
             const int i = j * G + part;
-            uv[j] = to_f32(u[i * CH]);
-            delta[j] = softplus(to_f32(dt[i * CH]) + bias);
-            if (!FULL && i >= left) delta[j] = 0.0f;  // (a step past the end keeps the state)
-            in[j] = delta[j] * uv[j];
-            total += delta[j];
-            if (G > 1) gates[i * CH + mine] = make_float2(delta[j], in[j]);
+            g[j].x = softplus(to_f32(dt[i * CH]) + bias);
+            if (!FULL && i >= left) g[j].x = 0.0f;  // (a step past the end keeps the state)
+            g[j].y = g[j].x * to_f32(u[i * CH]);
+            total += g[j].x;
         }
-        if (G > 1 || kWiden) __syncwarp();
+        if constexpr (kWiden) {
+            constexpr int ALL = TB * 2 * NP / 4;
+#pragma unroll
+            for (int i = 0; i < (ALL + 31) / 32; ++i) {
+                const int f = lane + 32 * i;
+                if (ALL % 32 != 0 && f >= ALL) continue;
+                const uint2 q = reinterpret_cast<const uint2 *>(bc_of(st))[f];
+                reinterpret_cast<float4 *>(wide)[f] = make_float4(__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xffff0000u),
+                                                                  __uint_as_float(q.y << 16), __uint_as_float(q.y & 0xffff0000u));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < PAIRS; ++j) gates[(j * G + part) * CH + mine] = g[j];
+        return total;
+    }
+
+    // The states and outputs of a block.
+    template <bool FOLD, bool FULL>
+    __device__ __forceinline__ void walk(int st, const float2 *gates, const float *bc, int left, U *py, int64_t py_step) {
+        const int mine = lane % CH;
+        const P *z = z_of(st) + mine;
+        const U *u = u_of(st) + mine;
         float sums[PAIRS];
-        const auto gate_of = [&](int i) {  // (delta, delta u) of step i
-            return G > 1 ? gates[i * CH + mine] : make_float2(delta[i / G], in[i / G]);
-        };
         // The next step's decays are formed beside a step's products.
-        float2 g = gate_of(0);
+        float2 g = gates[mine];
         Two e[2][S / 2];
         decays(g.x, e[0]);
 #pragma unroll
@@ -257,7 +277,7 @@ struct Walk {
                 const int at = j * G + i;
                 const float now = g.y;
                 if (at + 1 < TB) {
-                    g = gate_of(at + 1);
+                    g = gates[(at + 1) * CH + mine];
                     decays(g.x, e[(at + 1) & 1]);
                 }
                 v[i] = step<FOLD>(e[at & 1], now, bc + at * 2 * NP);
@@ -280,14 +300,13 @@ struct Walk {
 #pragma unroll
             for (int j = 0; j < PAIRS; ++j) {
                 const int i = j * G + part;
-                sums[j] = fmaf(skip, uv[j], sums[j]);
+                sums[j] = fmaf(skip, to_f32(u[i * CH]), sums[j]);
                 if (p.z) sums[j] *= silu(to_f32(z[i * CH]));
             }
 #pragma unroll
             for (int j = 0; j < PAIRS; ++j)
                 if (c_on && (FULL || j * G + part < left)) py[j * py_step] = from_f32<U>(sums[j]);
         }
-        return total;
     }
 
     // Steps t0 to t1.  FOLD: states alone; returns the lane's sum of delta.
@@ -296,7 +315,7 @@ struct Walk {
         float total = 0.0f;
         if (t0 >= t1) return total;
         float *wide = reinterpret_cast<float *>(smem + kStages * kStage);
-        float2 *gates = reinterpret_cast<float2 *>(smem + kStages * kStage + kWide);
+        float2 *gates = reinterpret_cast<float2 *>(smem + kStages * kStage + (1 + AHEAD) * kWide);
         const int64_t r = t0 * p.batch + b, across = static_cast<int64_t>(p.batch) * p.C;
         if (kFast && p.fast) {
             ldt.start(static_cast<const P *>(p.dt) + r * p.C + first, across, p.C - first, lane);
@@ -309,32 +328,38 @@ struct Walk {
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i) bring_block<FOLD>(t0 + i * TB, t1, i);
-        int st = 0;
-        for (int64_t t = t0; t < t1; t += TB) {
+        const auto form_block = [&](int64_t t, int st, int at) {
+            if (t + TB <= t1) total += form<true>(st, TB, gates + at * TB * CH, wide + at * TB * 2 * NP);
+            else if (t < t1) total += form<false>(st, static_cast<int>(t1 - t), gates + at * TB * CH, wide + at * TB * 2 * NP);
+        };
+        if (AHEAD) {
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
             __syncwarp();
+            form_block(t0, 0, 0);
+        }
+        int st = 0, turn = 0;
+        for (int64_t t = t0; t < t1; t += TB) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2 - AHEAD) : "memory");
+            __syncwarp();
             bring_block<FOLD>(t + (kStages - 1) * TB, t1, st == 0 ? kStages - 1 : st - 1);
-            const float *bc;
-            if constexpr (kWiden) {
-                constexpr int ALL = TB * 2 * NP / 4;
-                bc = wide;
-#pragma unroll
-                for (int i = 0; i < (ALL + 31) / 32; ++i) {
-                    const int f = lane + 32 * i;
-                    if (ALL % 32 != 0 && f >= ALL) continue;
-                    const uint2 q = reinterpret_cast<const uint2 *>(bc_of(st))[f];
-                    reinterpret_cast<float4 *>(wide)[f] =
-                        make_float4(__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xffff0000u),
-                                    __uint_as_float(q.y << 16), __uint_as_float(q.y & 0xffff0000u));
-                }
-            } else {
-                bc = reinterpret_cast<const float *>(bc_of(st));
+            const int next = st + 1 == kStages ? 0 : st + 1;
+            if (!AHEAD) {
+                form_block(t, st, 0);
+                __syncwarp();
             }
-            bc += part * S;
-            if (t + TB <= t1) total += block<FOLD, true>(st, bc, gates, TB, py, G * across);
-            else total += block<FOLD, false>(st, bc, gates, static_cast<int>(t1 - t), py, G * across);
+            const float2 *gates_now = gates + turn * TB * CH;
+            const float *bc = (kWiden ? wide + turn * TB * 2 * NP : reinterpret_cast<const float *>(bc_of(st))) + part * S;
+            if (t + (1 + AHEAD) * TB <= t1) {
+                // (one stretch of code without a branch, whose parts fill each other's gaps)
+                walk<FOLD, true>(st, gates_now, bc, TB, py, G * across);
+                if (AHEAD) total += form<true>(next, TB, gates + (turn ^ 1) * TB * CH, wide + (turn ^ 1) * TB * 2 * NP);
+            } else {
+                walk<FOLD, false>(st, gates_now, bc, static_cast<int>(min(t1 - t, static_cast<int64_t>(TB))), py, G * across);
+                if (AHEAD) form_block(t + TB, next, turn ^ 1);
+            }
             py += TB * across;
-            st = st + 1 == kStages ? 0 : st + 1;
+            st = next;
+            turn ^= AHEAD;
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         return total;
@@ -597,15 +622,15 @@ struct Cut {
     int S, time_warps, time_ctas;
 };
 
-// The least time by these figures (clocks, fitted to 140 measured times of seven
-// shapes, whose fastest cut it finds or comes within 9% of): a step takes a warp
-// `alone` on its scheduler, `among` others that many each, and with folds 1.86 times as much; a wave of CTAs takes
+// The least time by these figures (clocks, fitted to 133 measured times of seven
+// shapes, whose fastest cut it finds or comes within 9% of): w warps on a scheduler
+// take alone + w * more for a step of each, and with folds 1.61 times as much; a wave of CTAs takes
 // time to start, more for folds and their exchange in clusters.
 Cut choose(int64_t T, int64_t batch, int64_t C, int N, int u_size, int p_size, const DeviceState &ds) {
     struct Kind {
-        int S, alone, among;
+        int S, alone, more;
     };
-    const Kind kinds[] = {{16, 370, 165}, {8, 316, 86}, {4, 165, 57}};
+    const Kind kinds[] = {{16, 233, 123}, {8, 140, 58}, {4, 105, 31}};
     Cut best{};
     double least = 0.0;
     for (const Kind &k : kinds) {
@@ -616,19 +641,19 @@ Cut choose(int64_t T, int64_t batch, int64_t C, int N, int u_size, int p_size, c
         // Shared memory of a warp (as Walk counts it), and warps that find room on an SM.
         const int CH = 32 / G, TB = k.S == 4 && G == 4 ? 16 : 8;
         const int bytes = (TB == 16 ? 3 : 4) * TB * (CH * (2 * p_size + u_size) + 2 * k.S * G * p_size) +
-                          (p_size == 2 ? TB * 2 * k.S * G * 4 : 0) + (G > 1 ? TB * CH * 8 : 0) + (k.S / 2 + 1) * 288;
+                          (k.S < 16 ? 2 : 1) * ((p_size == 2 ? TB * 2 * k.S * G * 4 : 0) + TB * CH * 8) + (k.S / 2 + 1) * 288;
         for (int tw = 1; tw <= most; tw *= 2)
             for (int tc = 1; tc <= (tw == most ? 8 : 1); tc *= 2) {
                 const int warps = tw > 4 ? tw : 4, across = warps / tw;
                 const double ctas = static_cast<double>((groups + across - 1) / across) * tc * batch;
                 const int resident = std::max(1, std::min(16 / warps, 227 * 1024 / (warps * bytes)));
                 const double room = static_cast<double>(ds.num_sms) * resident;
-                const double waves = ctas <= room ? 1.0 : 0.4 + ctas / room;
+                const double waves = ctas <= room ? 1.0 : 0.29 + ctas / room;
                 const double on_one = std::ceil(std::min(ctas, room) / ds.num_sms) * warps / 4;
                 const int64_t steps = ((T + tw * tc - 1) / (tw * tc) + 7) / 8 * 8;
-                double t = steps * std::max<double>(k.alone, on_one * k.among) * (tw * tc > 1 ? 1.86 : 1.0) + 2500;
-                if (tw * tc > 1) t += 2300 + 250 * tw;
-                if (tc > 1) t += 2500 + 1000 * tc;
+                double t = steps * (k.alone + on_one * k.more) * (tw * tc > 1 ? 1.61 : 1.0) + 4500;
+                if (tw * tc > 1) t += 2900 + 127 * tw;
+                if (tc > 1) t += 1200 + 1000 * tc;
                 t *= waves;
                 if (least == 0.0 || t < least) least = t, best = Cut{k.S, tw, tc};
             }
