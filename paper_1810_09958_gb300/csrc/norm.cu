@@ -12,6 +12,7 @@
 #include <algorithm>
 
 #include "lm_common.cuh"
+#include "two.cuh"
 
 namespace isam {
 
@@ -50,15 +51,6 @@ struct Raw<bf16, 8> {
     }
 };
 template <>
-struct Raw<bf16, 4> {
-    uint2 w;
-    __device__ __forceinline__ void load(const bf16 *p) { w = *reinterpret_cast<const uint2 *>(p); }
-    __device__ __forceinline__ float operator[](int i) const {
-        const uint32_t u = i < 2 ? w.x : w.y;
-        return __uint_as_float(i % 2 ? u & 0xffff0000u : u << 16);
-    }
-};
-template <>
 struct Raw<bf16, 1> {
     uint32_t w;
     __device__ __forceinline__ void load(const bf16 *p) { w = *reinterpret_cast<const uint16_t *>(p); }
@@ -85,6 +77,16 @@ __device__ __forceinline__ void store(T *p, const float (&f)[V]) {
 __device__ __forceinline__ float warp_sum(float s) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+    return s;
+}
+
+// The sums of two values over a warp: of the first in lanes 0 to 15, of the second
+// in the others (each lane keeps one of them from the first exchange on).
+__device__ __forceinline__ float warp_sums(float a, float b) {
+    const bool up = threadIdx.x & 16;
+    float s = (up ? b : a) + __shfl_xor_sync(~0u, up ? a : b, 16);
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
     return s;
 }
 
@@ -232,21 +234,22 @@ __global__ void __launch_bounds__(MODE == kTwice ? 1024 : 512, MODE == kTwice ||
                          const G *dy, const G *dres, G *dx, float *part) {
     extern __shared__ float4 smem_raw[];  // the ring; behind the loop the teams' sums, [teams - 1][D]
     float *smem = reinterpret_cast<float *>(smem_raw);
-    __shared__ float2 sums[2][32];
+    __shared__ float sums[2][2][32];  // [turn][first, second][warp]
     dependent_start();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int team = warp / team_warps, tid = (warp - team * team_warps) * 32 + lane;
     const int step = team_warps * 32 * V;
     constexpr bool HOLD = MODE != kTwice;
     constexpr int HELD = HOLD ? NV : 1;
+    constexpr bool HOLD_W = HOLD && NV * V <= 16;  // else w comes from L1 each time
     // 16-byte words of a thread and row: r, dy, dres.
     constexpr int RW = V * sizeof(R) / 16, GW = V * sizeof(G) / 16, WORDS = NV * (RW + 2 * GW);
-    float acc[NV][V], ww[HELD][V];
+    float acc[NV][V], ww[HOLD_W ? NV : 1][V];
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[j][i] = 0.0f;
-    if constexpr (HOLD)
+    if constexpr (HOLD_W)
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = j * step + tid * V;
@@ -313,7 +316,12 @@ __global__ void __launch_bounds__(MODE == kTwice ? 1024 : 512, MODE == kTwice ||
             const int c = j * step + tid * V;
             if constexpr (HOLD) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) a[i] = rv[j][i], g[i] = gv[j][i], wv[i] = ww[j][i];
+                for (int i = 0; i < V; ++i) a[i] = rv[j][i], g[i] = gv[j][i];
+                if constexpr (HOLD_W)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) wv[i] = ww[j][i];
+                else
+                    load<V>(w + c, wv);
             } else {
                 load<V>(r + base + c, a);
                 load<V>(dy + base + c, g);
@@ -321,28 +329,44 @@ __global__ void __launch_bounds__(MODE == kTwice ? 1024 : 512, MODE == kTwice ||
             }
         };
         float s2 = 0.0f, sd = 0.0f;
+        Two s2_two = two(0.0f, 0.0f), sd_two = s2_two;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (on && j * step + tid * V < D) {
                 float a[V], g[V], wv[V];
                 operands(j, a, g, wv);
+                if constexpr (V > 1) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    s2 = fmaf(a[i], a[i], s2);
-                    sd = fmaf(a[i] * wv[i], g[i], sd);
+                    for (int i = 0; i < V; i += 2) {
+                        const Two aa = two(a[i], a[i + 1]);
+                        s2_two = fma(aa, aa, s2_two);
+                        sd_two = fma(mul(aa, two(wv[i], wv[i + 1])), two(g[i], g[i + 1]), sd_two);
+                    }
+                } else {
+                    s2 = fmaf(a[0], a[0], s2);
+                    sd = fmaf(a[0] * wv[0], g[0], sd);
                 }
             }
-        s2 = warp_sum(s2);
-        sd = warp_sum(sd);
+        if constexpr (V > 1) {
+            const float2 x = apart(s2_two), y = apart(sd_two);
+            s2 = x.x + x.y;
+            sd = y.x + y.y;
+        }
+        float both = warp_sums(s2, sd);
+        const int half = lane / 16;
         if (team_warps > 1) {
-            if (lane == 0) sums[turn][warp] = make_float2(s2, sd);
+            if (lane % 16 == 0) sums[turn][half][warp] = both;
             __syncthreads();
-            // (each warp folds the team's words, lane by lane)
-            const float2 p = lane < team_warps ? sums[turn][team * team_warps + lane] : make_float2(0.0f, 0.0f);
-            s2 = warp_sum(p.x);
-            sd = warp_sum(p.y);
+            // (each warp folds the team's words: of the first sum in lanes 0 to 15, of the second in the others)
+            const float *words = sums[turn][half] + team * team_warps;
+            both = lane % 16 < team_warps ? words[lane % 16] : 0.0f;
+            if (lane % 16 + 16 < team_warps) both += words[lane % 16 + 16];
+#pragma unroll
+            for (int d = 8; d > 0; d >>= 1) both += __shfl_xor_sync(~0u, both, d);
             turn ^= 1;
         }
+        s2 = __shfl_sync(~0u, both, 0);
+        sd = __shfl_sync(~0u, both, 16);
         const float k = rsqrtf(s2 / static_cast<float>(D) + eps);
         const float m = sd * k / static_cast<float>(D);  // mean(d n)
 #pragma unroll
@@ -364,11 +388,21 @@ __global__ void __launch_bounds__(MODE == kTwice ? 1024 : 512, MODE == kTwice ||
                         load<V>(dres + base + c, o);
                     }
                 }
+                if constexpr (V > 1) {
+                    const Two kk = two(k, k), mm = two(-m, -m);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float n = a[i] * k;
-                    acc[j][i] = fmaf(g[i], n, acc[j][i]);
-                    o[i] = fmaf(k, fmaf(-n, m, wv[i] * g[i]), o[i]);
+                    for (int i = 0; i < V; i += 2) {
+                        const Two n = mul(two(a[i], a[i + 1]), kk), gg = two(g[i], g[i + 1]);
+                        const float2 s = apart(fma(gg, n, two(acc[j][i], acc[j][i + 1])));
+                        acc[j][i] = s.x, acc[j][i + 1] = s.y;
+                        const Two d = fma(n, mm, mul(two(wv[i], wv[i + 1]), gg));
+                        const float2 x = apart(fma(kk, d, two(o[i], o[i + 1])));
+                        o[i] = x.x, o[i + 1] = x.y;
+                    }
+                } else {
+                    const float n = a[0] * k;
+                    acc[j][0] = fmaf(g[0], n, acc[j][0]);
+                    o[0] = fmaf(k, fmaf(-n, m, wv[0] * g[0]), o[0]);
                 }
                 if (dx) store<V>(dx + base + c, o);
             }
@@ -514,7 +548,10 @@ int norm_backward_launch(const NormBackDesc &p, DeviceState &ds, cudaStream_t s)
             }
             constexpr int V = sizeof(R) == 4 && sizeof(G) == 4 ? 4 : 8, F = 8 / V;
             if (p.D <= 4096) return backward<R, G, V, F, kRing>(p, ds, s);
-            return p.D <= 8192 ? backward<R, G, V, 2 * F, kRing>(p, ds, s) : backward<R, G, V, 4 * F, kTwice>(p, ds, s);
+            if (p.D <= 8192) return backward<R, G, V, 2 * F, kRing>(p, ds, s);
+            if constexpr (sizeof(R) == 2 && sizeof(G) == 2)
+                if (p.D <= 16384) return backward<R, G, V, 4 * F, kRing>(p, ds, s);  // (two rows of fp32 do not fit)
+            return backward<R, G, V, 4 * F, kTwice>(p, ds, s);
         });
     });
 }

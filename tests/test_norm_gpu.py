@@ -152,7 +152,7 @@ def test_block_scaled_output_is_the_block_scaled_products_operand():
 
 
 @pytest.mark.parametrize("r_kind,g_kind", [("bf16", "bf16"), ("fp32", "bf16"), ("bf16", "fp32"), ("fp32", "fp32")])
-@pytest.mark.parametrize("T,D", SIZES + [(2000, 64), (1300, 520), (400, 4104)])
+@pytest.mark.parametrize("T,D", SIZES + [(2000, 64), (1300, 520), (400, 4104), (320, 12296)])
 def test_backward(T, D, r_kind, g_kind):
     rng = np.random.default_rng(T * 40000 + D)
     r, r64 = tensor(rng, (T, D), r_kind, 2.0)
