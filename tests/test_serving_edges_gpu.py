@@ -183,3 +183,69 @@ def test_rows_of_wider_tensors_are_checked():
         n = normal(3, 6, 4, 16).bfloat16()
         isam.ssm_forward(6, 4, 40, 16, y, normal(4, 6, 4, 40).bfloat16(), None, normal(5, 40, 16), n, x[..., :16], None, None, None,
                          None, y)
+
+
+def room(gigabytes):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gigabytes * 1e9:
+        pytest.skip(f"needs {gigabytes} GB")
+
+
+def test_selection_past_32_bits():
+    """More than 2^31 logits: the last sequence's choice is that of a call of its own."""
+    room(12)
+    batch, beams, V, count = 275, 4, 2_000_003, 5
+    logits = torch.empty(batch, beams, V, dtype=torch.bfloat16, device="cuda")
+    logits.zero_()
+    logits[-1] = normal(1, beams, V).bfloat16()
+    scores = normal(2, batch, beams)
+
+    def call(n, l, s):
+        out = [torch.empty(n, count, dtype=k, device="cuda") for k in (torch.float32, torch.int32, torch.int32)]
+        isam.beam_select(n, beams, V, count, l, s, -1, None, *out)
+        return out
+
+    many, one = call(batch, logits, scores), call(1, logits[-1:].clone(), scores[-1:].clone())
+    assert torch.equal(many[1][-1:], one[1]) and torch.equal(many[2][-1:], one[2])
+    assert float((many[0][-1:] - one[0]).abs().max()) <= 1e-4
+    assert torch.equal(many[2][0], torch.arange(count, dtype=torch.int32, device="cuda"))
+
+
+def test_sequences_past_32_bits():
+    """More than 2^31 values: the last steps are those of a call that goes on from the state before them."""
+    room(40)
+    T, C, N, W, tail = 1_100_000, 2048, 4, 4, 300
+    x = torch.empty(T, 1, C, dtype=torch.bfloat16, device="cuda").normal_()
+    w, bias = normal(1, W, C), normal(2, C)
+    u = torch.empty_like(x)
+    isam.conv1d_forward(T, 1, C, W, x, w, bias, True, None, None, u)
+    few = torch.empty(tail, 1, C, dtype=torch.bfloat16, device="cuda")
+    isam.conv1d_forward(tail, 1, C, W, x[T - tail:], w, bias, True, x[T - tail - W + 1: T - tail].view(1, W - 1, C), None, few)
+    assert torch.equal(u[T - tail:], few)
+    bc, A, y, last = normal(3, T, 1, 2 * N).bfloat16(), -normal(4, C, N).abs() - 0.1, torch.empty_like(x), torch.empty(1, C, N, device="cuda")
+    B, Cm = bc[..., :N], bc[..., N:]
+    isam.ssm_forward(T, 1, C, N, u, x, None, A, B, Cm, bias, None, None, None, y, last)
+    before, end = torch.empty(1, C, N, device="cuda"), torch.empty(1, C, N, device="cuda")
+    isam.ssm_forward(T - tail, 1, C, N, u[:T - tail], x[:T - tail], None, A, B[:T - tail], Cm[:T - tail], bias, None, None, None,
+                     y[:T - tail], before)
+    isam.ssm_forward(tail, 1, C, N, u[T - tail:], x[T - tail:], None, A, B[T - tail:], Cm[T - tail:], bias, None, before, None, few, end)
+    # Other cuts of time: starts differ by roundings of states that decay; y by a rounding to bf16 either way.
+    assert float((end - last).abs().max()) <= 2.0 ** -18 * float(last.abs().max())
+    assert float((few.float() - y[T - tail:].float()).abs().max()) <= 2.0 ** -7 * float(few.abs().max())
+
+
+def test_a_cache_past_32_bits():
+    """Slots above 2^31 states."""
+    room(30)
+    C, N, slots = 4096, 16, 40_000
+    state = torch.empty(slots, C, N, device="cuda")
+    ids = torch.tensor([slots - 1, 3, -1, slots - 2], dtype=torch.int32, device="cuda")
+    state[ids[ids >= 0].long()] = normal(1, 3, C, N)
+    small = torch.stack([state[slots - 1], state[3], state[slots - 2]])
+    u, dt, bc, A = normal(2, 4, C), normal(3, 4, C), normal(4, 4, 2 * N), -normal(5, C, N).abs()
+    y, y2 = torch.empty(4, C, device="cuda"), torch.empty(4, C, device="cuda")
+    isam.ssm_step(4, C, N, slots, u, dt, None, A, bc[:, :N], bc[:, N:], None, None, ids, state, state, y)
+    isam.ssm_step(4, C, N, 3, u, dt, None, A, bc[:, :N], bc[:, N:], None, None,
+                  torch.tensor([0, 1, -1, 2], dtype=torch.int32, device="cuda"), small, small, y2)
+    assert torch.equal(y, y2) and torch.equal(state[slots - 1], small[0]) and torch.equal(state[slots - 2], small[2])
+    del state
