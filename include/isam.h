@@ -11,12 +11,13 @@
  *   - Every tensor pointer is a DEVICE pointer on the current CUDA device,
  *     allocated and owned by the caller.  The library never frees or keeps
  *     them past the call's completion on the stream.
- *   - Tensors are packed row-major (no leading-dimension arguments).
+ *   - Tensors are packed row-major (no leading-dimension arguments, but for the
+ *     pitches of rows that isam_conv1d_* and isam_ssm_* take).
  *   - The library owns small internal workspaces (an error word per device,
  *     the GRU's input-projection buffer, its hidden-state exchange buffer and
  *     step counter).  They are allocated on first use, reused, and released
- *     by isam_shutdown().  isam_glu_backward's workspace grows with the call
- *     and is the caller's.
+ *     by isam_shutdown().  The workspaces of isam_glu_backward,
+ *     isam_rms_norm_backward and isam_beam_select are the caller's.
  *
  * Execution
  *   - Every compute call is asynchronous on the stream set by
