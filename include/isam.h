@@ -642,7 +642,7 @@ int isam_rms_norm_backward(int T, int D, int r_type, const void *r, const float 
  *   y          [T][batch][C] (y_type)
  *   new_state  [batch][width - 1][C] (x_type), or NULL: the last inputs of each
  *              sequence, for isam_conv1d_step; may be state itself
- * Sums are fp32.  2 <= width <= 8, batch <= 65535, x_stride >= C, at most 2^40
+ * Sums are fp32.  2 <= width <= 8, batch <= 65535, C <= 2^31 - 512, x_stride >= C, at most 2^40
  * values of y; pointers aligned to their element; but for new_state outputs overlap
  * no input.  ISAM_ERR_INVALID_ARG for sizes < 1, null
  * pointers, unknown types, silu not 0 or 1 or x_stride < C;

@@ -767,6 +767,8 @@ int conv1d_validate(const char *name, const ConvDesc &p) {
     if (p.x_stride < p.C) return set_error(ISAM_ERR_INVALID_ARG, "%s: x_stride below C", name);
     if (p.width < 2 || p.width > 8)
         return set_error(ISAM_ERR_UNSUPPORTED, "%s: width (%d) must be 2 to 8", name, p.width);
+    // (threads are counted beyond C, in 31 bits)
+    if (p.C > 0x7fffffff - 511) return set_error(ISAM_ERR_UNSUPPORTED, "%s: C (%d) is above 2^31 - 512", name, p.C);
     if (static_cast<int64_t>(p.batch) * p.C > (int64_t{1} << 40) / p.T || p.x_stride > (int64_t{1} << 40) / p.T / p.batch)
         return set_error(ISAM_ERR_UNSUPPORTED, "%s: more than 2^40 values", name);
     if (!aligned(p.x, type_size(p.x_type)) || !aligned(p.state, type_size(p.x_type)) ||

@@ -7,6 +7,8 @@
 // more at the start of a run); the bound is HBM.  It asks for kAhead steps at a
 // time (one load a step and turn took 94 us on 2048 x 8 x 4096 of bf16, whose
 // bytes take 40), and its products run on packed pairs.
+#include <algorithm>
+
 #include "lm_common.cuh"
 #include "two.cuh"
 
@@ -111,11 +113,14 @@ template <typename X, typename Y, int V, int W>
 __global__ void __launch_bounds__(kThreads)
     conv1d_forward_kernel(int T, int batch, int C, int run, int silu_on, const X *x, int64_t x_stride, const float *w,
                           const float *bias, const X *state, const int32_t *lengths, Y *y, X *new_state) {
-    const int64_t c_wide = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * V;
-    if (c_wide >= C) return;
+    const int c = (blockIdx.x * kThreads + threadIdx.x) * V;
+    if (c >= C) return;
     dependent_start();
-    const int c = static_cast<int>(c_wide), b = blockIdx.z;
-    const int64_t first = static_cast<int64_t>(blockIdx.y) * run;
+    // (2048 x 8 x 4096 takes 44 us so, and 51 with b = blockIdx.z and runs on the second axis alone: measured, the
+    // cause is not known)
+    const int b = blockIdx.z % batch;
+    const int64_t first = (static_cast<int64_t>(blockIdx.y) + static_cast<int64_t>(blockIdx.z / batch) * gridDim.y) * run;
+    if (first >= T) return;
     const int len = lengths ? min(max(lengths[b], 0), T) : T;
     const int64_t pitch = static_cast<int64_t>(batch) * x_stride;
     const X *xb = x + b * x_stride + c;
@@ -264,12 +269,18 @@ int conv1d_forward_launch(const ConvDesc &p, DeviceState &ds, cudaStream_t s) {
         constexpr int W = decltype(w)::value, V = decltype(v)::value;
         const unsigned across = static_cast<unsigned>((p.C / V + kThreads - 1) / kThreads);
         // Runs long enough that the inputs read twice are few, short enough to fill the GPU.
-        int run = 32;
-        while (run > 4 && static_cast<int64_t>(across) * p.batch * ((p.T + run - 1) / run) < ds.num_sms * 8) run /= 2;
-        while ((p.T + static_cast<int64_t>(run) - 1) / run > 65535) run *= 2;
-        const unsigned runs = static_cast<unsigned>((p.T + static_cast<int64_t>(run) - 1) / run);
-        return launch_dependent(conv1d_forward_kernel<X, Y, V, W>, dim3(across, runs, p.batch), kThreads, 0, s, 1,
-                                "launch conv1d_forward_kernel", p.T, p.batch, p.C, run, p.silu,
+        // None but a sequence's first looks at the states, which that one may overwrite: the others begin W - 1 steps
+        // or more behind it.
+        int64_t run = 32;
+        const auto runs = [&] { return (p.T + run - 1) / run; };
+        while (run > 4 && run / 2 >= W - 1 && runs() * across * p.batch < ds.num_sms * 8) run /= 2;
+        // Runs beyond a grid's second axis go to its third, beside the sequences; longer ones where that is full.
+        constexpr int64_t kDown = 32768;
+        while ((runs() + kDown - 1) / kDown * p.batch > 65535) run *= 2;
+        const unsigned down = static_cast<unsigned>(std::min(runs(), kDown));
+        const unsigned deep = static_cast<unsigned>((runs() + kDown - 1) / kDown * p.batch);
+        return launch_dependent(conv1d_forward_kernel<X, Y, V, W>, dim3(across, down, deep), kThreads, 0, s, 1,
+                                "launch conv1d_forward_kernel", p.T, p.batch, p.C, static_cast<int>(run), p.silu,
                                 static_cast<const X *>(p.x), p.x_stride, p.w, p.bias, static_cast<const X *>(p.state),
                                 p.lengths, static_cast<Y *>(p.y), static_cast<X *>(p.new_state));
     });

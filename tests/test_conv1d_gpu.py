@@ -68,6 +68,22 @@ def test_padded_batch(C, in_place):
     assert not y.cpu().numpy()[pad].any()
 
 
+@pytest.mark.parametrize("width", [2, 5, 6, 8])
+def test_states_in_place_of_every_width(width):
+    """Few rows, thus short runs: none but a sequence's first may look at states that this one overwrites."""
+    T, batch, C = 64, 2, 200
+    rng = np.random.default_rng(width)
+    x, _ = tensor(rng, (T, batch, C), "bf16")
+    w, _ = tensor(rng, (width, C), "fp32")
+    state, _ = tensor(rng, (batch, width - 1, C), "bf16")
+    y, new = torch.empty_like(x), torch.empty_like(state)
+    isam.conv1d_forward(T, batch, C, width, x, w, None, True, state, None, y, new)
+    for _ in range(50):
+        there, got = state.clone(), torch.empty_like(x)
+        isam.conv1d_forward(T, batch, C, width, x, w, None, True, there, None, got, there)
+        assert torch.equal(got, y) and torch.equal(there, new)
+
+
 def test_without_states():
     T, batch, C = 9, 2, 16
     rng = np.random.default_rng(1)

@@ -59,7 +59,7 @@ CONV = dict(T=4, batch=2, C=8, width=4, xt=1, x=P, stride=8, w=P, bias=P, silu=1
     (dict(stride=-8), BAD), (dict(width=1), NO), (dict(width=9), NO), (dict(x=off(1)), NO), (dict(state=off(1)), NO),
     (dict(new=off(1)), NO), (dict(w=off(2)), NO), (dict(bias=off(2)), NO), (dict(lengths=off(1)), NO), (dict(y=off(2)), NO),
     (dict(T=BIG, batch=BIG), NO), (dict(T=2 ** 20, C=2 ** 21, stride=2 ** 21), NO), (dict(stride=2 ** 62), NO),
-    (dict(batch=65536), NO),
+    (dict(batch=65536), NO), (dict(C=BIG, stride=BIG), NO), (dict(C=BIG - 510, stride=BIG), NO),
 ])
 def test_conv_forward(lib, change, code):
     refused(lib, "isam_conv1d_forward", CONV | dict(state=P, lengths=P, yt=0, y=P, new=P), change, code)
